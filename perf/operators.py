@@ -157,7 +157,7 @@ def _own(s):
         return s["Y"]
     nmf.nmf_lowrank_product(s["dY"], rows, s["A"], not t, n, m, s["offsets"], s["run"], c["segments"], s["H"], s["Wt"], s["koff"], c["runs"],
                             c["kmax"], s["scale"], s["V"], s["dX"])
-    nmf.nmf_lowrank_gradient(s["X"], s["dY"], rows, m, n, s["offsets"], s["run"], c["segments"], s["koff"], c["runs"], c["kmax"], s["scale"],
+    nmf.nmf_lowrank_gradient(s["X"], s["dY"], rows, m, n, s["offsets"], s["run"], c["segments"], s["koff"], c["runs"], c["kmax"],
                              s["U"], s["V"], s["dWt"], s["dH"])
     return s["Y"], s["dX"], s["dWt"], s["dH"]
 
