@@ -20,11 +20,14 @@ EXPORTS = [
     "nmf_mu_dense", "nmf_mu_dense_noalloc", "nmf_mu_dense_profile", "nmf_residual_dense", "nmf_mu_dense_tol", "nmf_mu_dense_monitor", "nmf_mu_csr", "nmf_mu_csr_monitor", "nmf_mu_csr_tol", "nmf_mu_ooc", "nmf_mu_ooc_monitor", "nmf_mu_ooc_hostw", "nmf_mu_csr_ooc", "nmf_mu_dense_batched",
     "nmf_mu_workspace_bytes", "nmf_mu_set_workspace", "nmf_mu_release",
     "nmf_csr_partition", "nmf_split_planes", "nmf_csr_to_csc", "nmf_gram_w", "nmf_wta_dense", "nmf_h_update", "nmf_aht_w_update_dense",
+    "nmf_grouped_product", "nmf_grouped_gradient", "nmf_lowrank_product", "nmf_lowrank_gradient", "nmf_ragged_work_bytes",
 ]
 
 NMF_OK, NMF_EINVAL, NMF_ENOMEM, NMF_EHIP, NMF_EUNSUPPORTED = range(5)
 NMF_MU_MAX_K = 64
 NMF_MU_MAX_K_SLICED = 1024
+NMF_LOWRANK_MAX_K = 256
+NMF_F32, NMF_BF16, NMF_F16 = range(3)
 
 _lib = None
 
@@ -74,6 +77,14 @@ def lib() -> ctypes.CDLL:
     L.nmf_wta_dense.argtypes = [vp, i64, i64, i32, vp, vp, vp]
     L.nmf_h_update.argtypes = [vp, vp, vp, i32, i64, f32, vp, vp]
     L.nmf_aht_w_update_dense.argtypes = [vp, i64, i64, i32, vp, vp, vp, f32, vp]
+    L.nmf_grouped_product.argtypes = [i32, vp, i64, vp, i32, i64, vp, i64, i64, i32, i64, i64, vp, i64, vp, ctypes.c_size_t, vp]
+    L.nmf_grouped_gradient.argtypes = [i32, vp, i64, vp, i64, vp, i32, i64, i64, i64, vp, i64, i64, vp, ctypes.c_size_t, vp]
+    L.nmf_lowrank_product.argtypes = [i32, vp, i64, i64, vp, i64, i32, i64, i64, vp, vp, i32, vp, vp, vp, i32, i32, i64, vp, vp, vp, i64, vp,
+                                      ctypes.c_size_t, vp]
+    L.nmf_lowrank_gradient.argtypes = [i32, vp, i64, vp, i64, i64, i64, i64, vp, vp, i32, vp, i32, i32, i64, vp, vp, vp, vp, vp,
+                                       ctypes.c_size_t, vp]
+    L.nmf_ragged_work_bytes.restype = ctypes.c_size_t
+    L.nmf_ragged_work_bytes.argtypes = [ctypes.c_int, i32, i64, i64, i64, i32, i32, i32, i64]
     for name in EXPORTS:
         fn = getattr(L, name)
         if fn.restype is ctypes.c_int and name not in ("nmf_status_string", "nmf_last_error"):
@@ -289,3 +300,116 @@ def nmf_aht_w_update_dense(A, m, n, k, H, GH, W, eps, stream=None) -> None:
     _check(lib().nmf_aht_w_update_dense(_dev(A, torch.float32, "A"), m, n, k,
                                         _dev(H, torch.float32, "H"), _dev(GH, torch.float32, "GH"),
                                         _dev(W, torch.float32, "W"), eps, _stream(stream)))
+
+
+# ---- products over ragged ranges of rows (include/nmfmu_ragged.h) ------------------
+# Types and leading dimensions are the tensors'; the scratch is torch's unless `work` (a uint8 device tensor) is given.
+
+_TYPES = {torch.float32: NMF_F32, torch.bfloat16: NMF_BF16, torch.float16: NMF_F16}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if not t.is_cuda or t.dtype not in _TYPES:
+        raise ValueError(f"{what}: need a float32, bfloat16 or float16 device tensor")
+    return _TYPES[t.dtype]
+
+
+def _rows_of(t, dtype, rows, cols, what):
+    """(pointer, leading dimension) of a rows x cols matrix whose rows are contiguous."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols
+            and (cols <= 1 or t.stride(1) == 1)):
+        raise ValueError(f"{what}: need a {rows} x {cols} {dtype} device tensor with contiguous rows")
+    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), ld
+
+
+def _stack_of(t, dtype, count, rows, cols, what):
+    """(pointer, leading dimension, stride) of `count` such matrices."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 3 and tuple(t.shape) == (count, rows, cols)
+            and (cols <= 1 or t.stride(2) == 1)):
+        raise ValueError(f"{what}: need a {count} x {rows} x {cols} {dtype} device tensor with contiguous rows")
+    ld = t.stride(1) if rows > 1 else max(cols, t.stride(1))
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), ld, t.stride(0) if count > 1 else max((rows - 1) * ld + cols, t.stride(0))
+
+
+def _list(t, dtype, count, what):
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == count):
+        raise ValueError(f"{what}: need a contiguous {dtype} device tensor of {count} entries")
+    return t.data_ptr()
+
+
+def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, like, stream):
+    """(pointer, bytes, tensor to keep) of the scratch of a call."""
+    if work is not None:
+        if not (work.is_cuda and work.dtype == torch.uint8 and work.is_contiguous()):
+            raise ValueError("work: need a contiguous uint8 device tensor")
+        return work.data_ptr(), work.numel(), work
+    need = lib().nmf_ragged_work_bytes(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
+    if need == 0:
+        return None, 0, None
+    buf = torch.empty(need, dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+        buf.record_stream(on)
+    return buf.data_ptr(), need, buf
+
+
+def nmf_ragged_work_bytes(kind, type, rows, m, n, parts, runs=0, kmax=0, ktotal=0) -> int:
+    return int(lib().nmf_ragged_work_bytes(kind, type, rows, m, n, parts, runs, kmax, ktotal))
+
+
+def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=None, stream=None) -> None:
+    """Y_g = X_g B_g; B: groups x m x n, or groups x n x m if transposed."""
+    typ = _type(X, "X")
+    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
+    b, ldb, stride_b = _stack_of(B, X.dtype, groups, *((n, m) if transposed else (m, n)), "B")
+    y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
+    w, nbytes, _keep = _work(0, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
+    _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
+                                     int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream(stream)))
+
+
+def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, stream=None) -> None:
+    """G_g = X_g^T dY_g (groups x m x n)."""
+    typ = _type(X, "X")
+    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
+    dy, ldy = _rows_of(dY, X.dtype, rows, n, "dY")
+    g, ldg, stride_g = _stack_of(G, X.dtype, groups, m, n, "G")
+    w, nbytes, _keep = _work(1, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
+    _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, m, n,
+                                      g, ldg, stride_g, w, nbytes, _stream(stream)))
+
+
+def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt, H, koff, runs, kmax, scale, U, Y,
+                        work=None, stream=None) -> None:
+    """Y = X A + scale_r (X W_r) H_r; Wt: ktotal x m, H: ktotal x n, contiguous; U: rows x kmax float32, written."""
+    typ = _type(X, "X")
+    ktotal = Wt.shape[0]
+    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
+    a, lda = _rows_of(A, X.dtype, *((n, m) if transposed else (m, n)), "A")
+    y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
+    w, nbytes, _keep = _work(2, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
+    _check(lib().nmf_lowrank_product(
+        typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, segments + 1, "offsets"),
+        _list(run, torch.int32, segments, "run"), segments, _list(Wt, X.dtype, ktotal * m, "Wt"), _list(H, X.dtype, ktotal * n, "H"),
+        _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal,
+        None if scale is None else _list(scale, torch.float32, runs, "scale"), _list(U, torch.float32, rows * kmax, "U"), y, ldy,
+        w, nbytes, _stream(stream)))
+
+
+def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work=None, stream=None) -> None:
+    """dW_r = X^T V and dH_r = U^T dY over the rows of each run; dWt: ktotal x m, dH: ktotal x n, contiguous."""
+    typ = _type(X, "X")
+    ktotal = dWt.shape[0]
+    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
+    dy, ldy = _rows_of(dY, X.dtype, rows, n, "dY")
+    w, nbytes, _keep = _work(3, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
+    _check(lib().nmf_lowrank_gradient(
+        typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, segments + 1, "offsets"), _list(run, torch.int32, segments, "run"),
+        segments, _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, rows * kmax, "U"),
+        _list(V, torch.float32, rows * kmax, "V"), _list(dWt, X.dtype, ktotal * m, "dWt"), _list(dH, X.dtype, ktotal * n, "dH"),
+        w, nbytes, _stream(stream)))

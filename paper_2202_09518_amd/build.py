@@ -8,7 +8,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnmfmu.so")
-SOURCES = ["nmfmu_dense.hip", "nmfmu_pairs.hip", "nmfmu_csr.hip", "nmfmu_api.hip"]
+SOURCES = ["nmfmu_dense.hip", "nmfmu_pairs.hip", "nmfmu_csr.hip", "nmfmu_api.hip",
+           "nmfmu_ragged_bf16.hip", "nmfmu_ragged_f16.hip", "nmfmu_ragged_f32.hip", "nmfmu_ragged_api.hip"]
+HEADERS = [os.path.join(CSRC, h) for h in ("nmfmu_internal.h", "nmfmu_device.h", "nmfmu_ragged_internal.h", "nmfmu_ragged_device.h",
+                                           "nmfmu_ragged_kernels.h")] + \
+          [os.path.join(ROOT, "include", h) for h in ("nmfmu.h", "nmfmu_test.h", "nmfmu_ragged.h")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -24,8 +28,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, "nmfmu_internal.h"), os.path.join(CSRC, "nmfmu_device.h"), os.path.join(ROOT, "include", "nmfmu.h"),
-                        os.path.join(ROOT, "include", "nmfmu_test.h")]
+    deps = sources() + HEADERS
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -24,6 +24,12 @@ int fail(int status, const char *fmt, const char *detail = "")
     return status;
 }
 
+}  // namespace
+
+int nmfmu::set_error(int status, const char *what) { return fail(status, "%s", what); }
+
+namespace {
+
 #define NMF_HIP(call)                                                         \
     do {                                                                      \
         hipError_t e_ = (call);                                               \

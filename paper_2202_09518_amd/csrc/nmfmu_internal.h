@@ -8,6 +8,9 @@
 
 namespace nmfmu {
 
+// Keeps `what` for nmf_last_error of this thread; returns the status.
+int set_error(int status, const char *what);
+
 // ---- launch geometry shared between the host scheduler and the kernels ----
 
 constexpr int kWtaWaves = 4;        // waves per workgroup in the W^T A pass

@@ -1,0 +1,254 @@
+// C ABI of the products over ragged ranges of rows: argument checks and plans.
+// Public contract: include/nmfmu_ragged.h.
+#include "nmfmu_ragged.h"
+#include "nmfmu_internal.h"
+#include "nmfmu_ragged_internal.h"
+
+#include <algorithm>
+
+using namespace nmfmu;
+using namespace nmfmu::ragged;
+
+namespace {
+
+constexpr int64_t kMost = ((int64_t)1 << 31) - 1;
+constexpr int kComputeUnits = 256;
+
+int bytes_of(int32_t type) { return type == NMF_F32 ? 4 : 2; }
+int stage_of(int32_t type) { return 128 / bytes_of(type); }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned(const void *p, int to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+struct Plan {
+    int shape, splits;
+};
+
+// Parts of a contraction of k for `tiles` workgroups: enough of them for two on each compute unit, each at least four
+// stages long.
+int splits_for(int64_t tiles, int64_t k, int stage)
+{
+    const int64_t want = 2 * kComputeUnits / std::max<int64_t>(tiles, 1), have = k / (4 * stage);
+    const int64_t s = std::min<int64_t>(std::min(want, have), kMaxSplits);
+    return s < 2 ? 1 : (int)s;
+}
+
+// Tile shape and parts of a product of `rows` rows in `groups` ranges.
+Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
+{
+    groups = std::max<int64_t>(1, std::min(groups, rows));
+    const int64_t avg = ceil_div(rows, groups);
+    auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
+    Plan p;
+    if (avg >= (groups > 1 ? 400 : 256) && tiles(0) >= 200) p.shape = 0;
+    else if (avg > 64) p.shape = 1;
+    else if (avg > 32) p.shape = 2;
+    else p.shape = 3;
+    p.splits = p.shape == 0 || rows > 4096 ? 1 : splits_for(tiles(p.shape), m, stage_of(type));
+    return p;
+}
+
+Plan gradient_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
+{
+    auto tiles = [&](int shape) { return groups * ceil_div(m, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
+    Plan p;
+    p.shape = tiles(0) >= 200 ? 0 : 1;
+    p.splits = p.shape == 0 ? 1 : splits_for(tiles(1), ceil_div(rows, groups), stage_of(type));
+    return p;
+}
+
+int shrink_plan(int32_t type, int64_t rows, int64_t segments, int64_t m, int kmax)
+{
+    const int64_t tiles = (ceil_div(rows, kShrinkRows) + std::min(segments, rows)) * ceil_div(kmax, kShrinkCols);
+    return rows > 4096 ? 1 : splits_for(tiles, m, stage_of(type));
+}
+
+int factor_plan(int32_t type, int64_t rows, int64_t runs, int64_t m, int64_t n, int kmax)
+{
+    const int64_t tiles = runs * ceil_div(kmax, kmax <= 32 ? 32 : 64) * (ceil_div(m, 128) + ceil_div(n, 128));
+    return splits_for(tiles, ceil_div(rows, runs), stage_of(type));
+}
+
+size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (size_t)splits * rows * up4(n) * 4 : 0; }
+size_t shrink_part(int64_t rows, int kmax, int splits) { return splits > 1 ? (size_t)splits * up4(rows * kmax) * 4 : 0; }
+size_t gradient_part(int64_t groups, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * groups * m * up4(n) * 4 : 0; }
+size_t factor_part(int64_t ktotal, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * ktotal * (up4(m) + up4(n)) * 4 : 0; }
+
+// Splits that a scratch of `have` bytes can hold.
+template <class F> int fit(int splits, size_t have, F bytes)
+{
+    while (splits > 1 && bytes(splits) > have) --splits;
+    return splits;
+}
+
+bool sizes_ok(int64_t rows, int64_t m, int64_t n) { return rows >= 0 && m > 0 && n > 0 && rows <= kMost && m <= kMost && n <= kMost; }
+
+template <class P> int launched(int32_t type, const P &p, void *stream, hipError_t (*f)(const P &, hipStream_t),
+                                hipError_t (*b)(const P &, hipStream_t), hipError_t (*h)(const P &, hipStream_t))
+{
+    const hipError_t e = (type == NMF_F32 ? f : type == NMF_BF16 ? b : h)(p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? NMF_OK : set_error(NMF_EHIP, hipGetErrorString(e));
+}
+
+int check_type(int32_t type) { return type >= NMF_F32 && type <= NMF_F16 ? NMF_OK : set_error(NMF_EINVAL, "unknown type"); }
+
+int check_work(const void *work, size_t bytes)
+{
+    if (bytes && !work) return set_error(NMF_EINVAL, "work is null but work_bytes is not 0");
+    if (!aligned(work, 16)) return set_error(NMF_EINVAL, "work must be 16-byte aligned");
+    return NMF_OK;
+}
+
+int check_grid(int64_t workgroups)
+{
+    return workgroups <= kMost ? NMF_OK : set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
+}
+
+int64_t product_grid(const Product &p)
+{
+    return (ceil_div(p.rows, kTileRows[p.shape]) + (p.offsets ? p.groups : 0)) * ceil_div(p.n, kTileCols[p.shape]) * p.splits;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t *offsets, int32_t groups, int64_t rows, const void *B,
+                        int64_t ldb, int64_t stride_b, int32_t transposed, int64_t m, int64_t n, void *Y, int64_t ldy, void *work,
+                        size_t work_bytes, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!sizes_ok(rows, m, n) || groups < 1) return set_error(NMF_EINVAL, "sizes must be positive and below 2^31");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    if (!offsets || !B || (rows && (!X || !Y))) return set_error(NMF_EINVAL, "null pointer");
+    const int e = bytes_of(type);
+    if (!aligned(X, e) || !aligned(B, e) || !aligned(Y, e) || !aligned(offsets, 8)) return set_error(NMF_EINVAL, "misaligned pointer");
+    if (ldx < m || ldy < n || ldb < (transposed ? m : n) || stride_b < 0) return set_error(NMF_EINVAL, "leading dimension below the row's length");
+    if (rows == 0) return NMF_OK;
+    const Plan plan = product_plan(type, rows, groups, m, n);
+    Product p = {};
+    p.x = X; p.ldx = ldx; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
+    p.b = B; p.ldb = ldb; p.stride_b = stride_b; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
+    p.shape = plan.shape;
+    p.splits = fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); });
+    p.k_split = ceil_div(ceil_div(m, stage_of(type)), p.splits) * stage_of(type);
+    p.part = static_cast<float *>(work);
+    p.shrink_splits = 1;
+    p.vec = aligned(Y, 4 * e) && ldy % 4 == 0;
+    if ((rc = check_grid(product_grid(p)))) return rc;
+    return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
+}
+
+int nmf_grouped_gradient(int32_t type, const void *X, int64_t ldx, const void *dY, int64_t ldy, const int64_t *offsets, int32_t groups,
+                         int64_t rows, int64_t m, int64_t n, void *G, int64_t ldg, int64_t stride_g, void *work, size_t work_bytes,
+                         void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!sizes_ok(rows, m, n) || groups < 1) return set_error(NMF_EINVAL, "sizes must be positive and below 2^31");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    if (!offsets || !G || (rows && (!X || !dY))) return set_error(NMF_EINVAL, "null pointer");
+    const int e = bytes_of(type);
+    if (!aligned(X, e) || !aligned(dY, e) || !aligned(G, e) || !aligned(offsets, 8)) return set_error(NMF_EINVAL, "misaligned pointer");
+    if (ldx < m || ldy < n || ldg < n || (groups > 1 && stride_g < (m - 1) * ldg + n)) return set_error(NMF_EINVAL, "leading dimension below the row's length, or results that overlap");
+    const Plan plan = gradient_plan(type, rows, groups, m, n);
+    Gradient p = {};
+    p.x = X; p.dy = dY; p.ldx = ldx; p.ldy = ldy; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
+    p.g = G; p.ldg = ldg; p.stride_g = stride_g;
+    p.shape = plan.shape;
+    p.splits = fit(plan.splits, work_bytes, [&](int s) { return gradient_part(groups, m, n, s); });
+    p.part = static_cast<float *>(work);
+    p.vec = aligned(G, 4 * e) && ldg % 4 == 0 && stride_g % 4 == 0;
+    if ((rc = check_grid(ceil_div(m, kTileRows[p.shape]) * ceil_div(n, kTileCols[p.shape]) * groups * p.splits))) return rc;
+    return launched(type, p, stream, launch_gradient<float>, launch_gradient<bf16_t>, launch_gradient<f16_t>);
+}
+
+int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, const void *A, int64_t lda, int32_t transposed, int64_t m,
+                        int64_t n, const int64_t *offsets, const int32_t *run, int32_t segments, const void *Wt, const void *H,
+                        const int32_t *koff, int32_t runs, int32_t kmax, int64_t ktotal, const float *scale, float *U, void *Y, int64_t ldy,
+                        void *work, size_t work_bytes, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!sizes_ok(rows, m, n) || segments < 0 || runs < 1 || kmax < 1 || ktotal < 1 || ktotal > kMost)
+        return set_error(NMF_EINVAL, "sizes must be positive and below 2^31");
+    if (kmax > NMF_LOWRANK_MAX_K) return set_error(NMF_EUNSUPPORTED, "kmax exceeds NMF_LOWRANK_MAX_K");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    if (!A || (rows && (!X || !Y)) || (segments && (!offsets || !run || !Wt || !H || !koff || (rows && !U))))
+        return set_error(NMF_EINVAL, "null pointer");
+    const int e = bytes_of(type);
+    if (!aligned(X, e) || !aligned(A, e) || !aligned(Y, e) || !aligned(Wt, e) || !aligned(H, e) || !aligned(offsets, 8) || !aligned(run, 4) ||
+        !aligned(koff, 4) || !aligned(scale, 4) || !aligned(U, 4))
+        return set_error(NMF_EINVAL, "misaligned pointer");
+    if (ldx < m || ldy < n || lda < (transposed ? m : n)) return set_error(NMF_EINVAL, "leading dimension below the row's length");
+    if (rows == 0) return NMF_OK;
+    const Plan plan = product_plan(type, rows, 1, m, n);
+    Product p = {};
+    p.x = X; p.ldx = ldx; p.groups = 1; p.rows = rows; p.m = m; p.n = n;
+    p.b = A; p.ldb = lda; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
+    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, Wt, H, scale, U};
+    p.shape = plan.shape;
+    p.shrink_splits = 1;
+    const int stage = stage_of(type);
+    if (segments) {
+        p.shrink_splits = fit(shrink_plan(type, rows, segments, m, kmax), work_bytes, [&](int s) { return shrink_part(rows, kmax, s); });
+        p.shrink_k = ceil_div(ceil_div(m, stage), p.shrink_splits) * stage;
+        p.upart = static_cast<float *>(work);
+    }
+    const size_t used = segments ? shrink_part(rows, kmax, p.shrink_splits) : 0;
+    p.splits = fit(plan.splits, work_bytes - used, [&](int s) { return product_part(rows, n, s); });
+    p.k_split = ceil_div(ceil_div(m, stage), p.splits) * stage;
+    p.part = reinterpret_cast<float *>(static_cast<char *>(work) + used);
+    p.vec = aligned(Y, 4 * e) && ldy % 4 == 0;
+    const int64_t shrink = segments ? (ceil_div(rows, kShrinkRows) + segments) * ceil_div(kmax, kShrinkCols) * p.shrink_splits : 0;
+    if ((rc = check_grid(product_grid(p) + shrink))) return rc;
+    return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
+}
+
+int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *dY, int64_t ldy, int64_t rows, int64_t m, int64_t n,
+                         const int64_t *offsets, const int32_t *run, int32_t segments, const int32_t *koff, int32_t runs, int32_t kmax,
+                         int64_t ktotal, const float *U, const float *V, void *dWt, void *dH, void *work, size_t work_bytes, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!sizes_ok(rows, m, n) || segments < 0 || runs < 1 || kmax < 1 || ktotal < 1 || ktotal > kMost)
+        return set_error(NMF_EINVAL, "sizes must be positive and below 2^31");
+    if (kmax > NMF_LOWRANK_MAX_K) return set_error(NMF_EUNSUPPORTED, "kmax exceeds NMF_LOWRANK_MAX_K");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    if (!koff || !dWt || !dH || (segments && (!offsets || !run)) || (segments && rows && (!X || !dY || !U || !V)))
+        return set_error(NMF_EINVAL, "null pointer");
+    const int e = bytes_of(type);
+    if (!aligned(X, e) || !aligned(dY, e) || !aligned(dWt, e) || !aligned(dH, e) || !aligned(offsets, 8) || !aligned(run, 4) ||
+        !aligned(koff, 4) || !aligned(U, 4) || !aligned(V, 4))
+        return set_error(NMF_EINVAL, "misaligned pointer");
+    if (ldx < m || ldy < n) return set_error(NMF_EINVAL, "leading dimension below the row's length");
+    if (rows == 0) segments = 0;
+    FactorGradient p = {};
+    p.x = X; p.dy = dY; p.ldx = ldx; p.ldy = ldy; p.rows = rows; p.m = m; p.n = n;
+    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, nullptr, nullptr, nullptr, nullptr};
+    p.u = U; p.v = V; p.ddown = dWt; p.dup = dH;
+    p.splits = fit(factor_plan(type, rows, runs, m, n, kmax), work_bytes, [&](int s) { return factor_part(ktotal, m, n, s); });
+    p.part = static_cast<float *>(work);
+    if ((int64_t)runs * ceil_div(kmax, 32) > 65535) return set_error(NMF_EUNSUPPORTED, "more runs than one launch can have");
+    return launched(type, p, stream, launch_factor_gradient<float>, launch_factor_gradient<bf16_t>, launch_factor_gradient<f16_t>);
+}
+
+size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, int64_t n, int32_t parts, int32_t runs, int32_t kmax,
+                             int64_t ktotal)
+{
+    if (type < NMF_F32 || type > NMF_F16 || !sizes_ok(rows, m, n) || rows == 0) return 0;
+    switch (kind) {
+    case 0: return parts < 1 ? 0 : product_part(rows, n, product_plan(type, rows, parts, m, n).splits);
+    case 1: return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits);
+    case 2:
+        if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K) return 0;
+        return product_part(rows, n, product_plan(type, rows, 1, m, n).splits) +
+               (parts ? shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax)) : 0);
+    case 3:
+        if (runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
+        return factor_part(ktotal, m, n, factor_plan(type, rows, runs, m, n, kmax));
+    }
+    return 0;
+}
+
+}  // extern "C"

@@ -1,0 +1,87 @@
+// Launchers of the products over ragged ranges of rows (grouped products, low-rank adapters), one set per type.
+// Not part of the public ABI (that is include/nmfmu_ragged.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace nmfmu {
+namespace ragged {
+
+// Tile shapes of the product kernels, largest first.
+constexpr int kShapes = 4;
+constexpr int kTileRows[kShapes] = {256, 128, 64, 32}, kTileCols[kShapes] = {256, 128, 128, 128};
+constexpr int kShrinkRows = 64, kShrinkCols = 64;
+constexpr int kMaxSplits = 16, kMaxRank = 256;
+
+// Factor pairs of segments of rows.
+struct Adapters {
+    const int64_t *offsets;      // segments + 1
+    const int32_t *run;          // segments
+    int32_t segments;
+    const int32_t *koff;         // runs + 1
+    int32_t runs, kmax;
+    int64_t ktotal;              // rows of down and up
+    const void *down, *up;       // ktotal x m and ktotal x n
+    const float *scale;          // runs, or null
+    float *u;                    // rows x kmax
+};
+
+struct Product {
+    const void *x;
+    int64_t ldx;
+    const int64_t *offsets;      // groups + 1, or null: one group of all rows
+    int32_t groups;
+    int64_t rows, m, n;
+    const void *b;
+    int64_t ldb, stride_b;
+    int32_t transposed;
+    void *y;
+    int64_t ldy;
+    Adapters ad;                 // ad.segments == 0: none
+    // plan
+    int shape, splits;
+    int64_t k_split;             // k of a split, whole stages
+    float *part;                 // splits x rows x (n rounded up to 4); 
+    int shrink_splits;           // parts of u
+    int64_t shrink_k;
+    float *upart;                // shrink_splits x rows x kmax, where there are several
+    bool vec;                    // rows of y can take four entries at once
+};
+
+struct Gradient {
+    const void *x, *dy;
+    int64_t ldx, ldy;
+    const int64_t *offsets;
+    int32_t groups;
+    int64_t rows, m, n;
+    void *g;
+    int64_t ldg, stride_g;
+    int shape, splits;
+    float *part;                 // splits x groups x m x (n rounded up to 4)
+    bool vec;
+};
+
+struct FactorGradient {
+    const void *x, *dy;
+    int64_t ldx, ldy, rows, m, n;
+    Adapters ad;                 // its u, down, up and scale are not used
+    const float *u, *v;          // rows x kmax
+    void *ddown, *dup;           // ktotal x m, ktotal x n
+    int splits;
+    float *part;                 // splits x ktotal x (m rounded up to 4 + n rounded up to 4)
+};
+
+// Types by their bits (float as it is).
+struct bf16_t { unsigned short bits; };
+struct f16_t { unsigned short bits; };
+
+template <class T> hipError_t launch_product(const Product &p, hipStream_t st);
+template <class T> hipError_t launch_gradient(const Gradient &p, hipStream_t st);
+template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hipStream_t st);
+
+__host__ __device__ inline int64_t up4(int64_t n) { return (n + 3) / 4 * 4; }
+
+}  // namespace ragged
+}  // namespace nmfmu
