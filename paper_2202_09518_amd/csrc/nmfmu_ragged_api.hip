@@ -134,7 +134,7 @@ int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t 
     p.k_split = ceil_div(ceil_div(m, stage_of(type)), p.splits) * stage_of(type);
     p.part = static_cast<float *>(work);
     p.shrink_splits = 1;
-    p.vec = aligned(Y, 4 * e) && ldy % 4 == 0;
+    p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
     if ((rc = check_grid(product_grid(p)))) return rc;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
 }
@@ -158,7 +158,7 @@ int nmf_grouped_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     p.shape = plan.shape;
     p.splits = fit(plan.splits, work_bytes, [&](int s) { return gradient_part(groups, m, n, s); });
     p.part = static_cast<float *>(work);
-    p.vec = aligned(G, 4 * e) && ldg % 4 == 0 && stride_g % 4 == 0;
+    p.vec = aligned(G, 16) && ldg * e % 16 == 0 && stride_g * e % 16 == 0;
     if ((rc = check_grid(ceil_div(m, kTileRows[p.shape]) * ceil_div(n, kTileCols[p.shape]) * groups * p.splits))) return rc;
     return launched(type, p, stream, launch_gradient<float>, launch_gradient<bf16_t>, launch_gradient<f16_t>);
 }
@@ -199,7 +199,7 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
     p.splits = fit(plan.splits, work_bytes - used, [&](int s) { return product_part(rows, n, s); });
     p.k_split = ceil_div(ceil_div(m, stage), p.splits) * stage;
     p.part = reinterpret_cast<float *>(static_cast<char *>(work) + used);
-    p.vec = aligned(Y, 4 * e) && ldy % 4 == 0;
+    p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
     const int64_t shrink = segments ? (ceil_div(rows, kShrinkRows) + segments) * ceil_div(kmax, kShrinkCols) * p.shrink_splits : 0;
     if ((rc = check_grid(product_grid(p) + shrink))) return rc;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);

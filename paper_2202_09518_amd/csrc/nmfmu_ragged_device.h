@@ -58,12 +58,12 @@ template <> struct Type<float> {
     static __device__ __forceinline__ float round(float x) { return x; }
 };
 
-constexpr int kStageBytes = 128;      // bytes of k in a stage
+constexpr int kStageBytes = 128;      // bytes of k in a stage, if not said otherwise
 constexpr unsigned kOutside = 0xfffffff0u;
 constexpr int kBufferFlags = 0x00020000;
 
 // k of a stage.
-template <class T> constexpr int stage_k() { return kStageBytes / Type<T>::kBytes; }
+template <class T, int SB = kStageBytes> constexpr int stage_k() { return SB / Type<T>::kBytes; }
 // Entries of a chunk.
 template <class T> constexpr int chunk_n() { return 16 / Type<T>::kBytes; }
 
@@ -76,6 +76,9 @@ template <class T, int R> __device__ __forceinline__ int rc_shift(int k)
     if (pitch == 128) return ((k >> 1) & 1) * 4;
     return 0;
 }
+
+// The same for row `row` of a KC operand.
+template <int SB> __device__ __forceinline__ int kc_shift(int row) { return SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
 // One operand of a tile as it lies in memory.
 struct Operand {
@@ -122,12 +125,11 @@ template <class T> __device__ __forceinline__ u32x4 keep_first(u32x4 v, int64_t 
 // Brings stages of an operand (R rows or columns) into LDS with THREADS threads.
 // DMA: base, ld and the extents are multiples of 16 bytes: the chunks go to LDS without passing registers; a chunk that is
 // not there is asked for outside the descriptor's range, which delivers zeros.  Else: any alignment, through registers.
-template <class T, int R, bool RC, int THREADS, bool DMA> struct Loader {
-    static constexpr int kBytesLds = R * kStageBytes;
-    static constexpr int kJobs = R * 8 / THREADS;                    // chunks of a thread
-    static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : 8;
+template <class T, int R, bool RC, int THREADS, bool DMA, int SB> struct Loader {
+    static constexpr int kJobs = R * (SB / 16) / THREADS;            // chunks of a thread
+    static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : SB / 16;
     static constexpr int kRowStep = THREADS / kRowChunks;            // rows from job to job
-    static_assert(R * 8 % THREADS == 0 && THREADS % kRowChunks == 0, "whole jobs");
+    static_assert(R * (SB / 16) % THREADS == 0 && THREADS % kRowChunks == 0, "whole jobs");
     static_assert(RC ? kRowStep % (Type<T>::kBytes == 4 ? 8 : 4) == 0 : kRowStep % 16 == 0, "places repeat from job to job");
 
     const char *base;
@@ -146,7 +148,7 @@ template <class T, int R, bool RC, int THREADS, bool DMA> struct Loader {
         const int tid = threadIdx.x;
         line = tid / kRowChunks;
         const int place = tid % kRowChunks;
-        chunk = RC ? place ^ rc_shift<T, R>(line) : place ^ ((line >> 1) & 7);
+        chunk = RC ? place ^ rc_shift<T, R>(line) : place ^ kc_shift<SB>(line);
         if (DMA) {
 #pragma unroll
             for (int j = 0; j < kJobs; ++j) {
@@ -156,8 +158,8 @@ template <class T, int R, bool RC, int THREADS, bool DMA> struct Loader {
             }
         }
     }
-    // The stage at k0 (of K in all) to `lds`, or to registers.
-    __device__ __forceinline__ void fetch(int64_t k0, int64_t K, char *lds)
+    // Chunk j of the stage at k0 (of K in all) to `lds`, or to a register.
+    __device__ __forceinline__ void fetch_job(int j, int64_t k0, int64_t K, char *lds)
     {
         const int64_t left = K - k0;
         const char *at = base + (RC ? k0 * ld : k0 * Type<T>::kBytes);
@@ -166,31 +168,30 @@ template <class T, int R, bool RC, int THREADS, bool DMA> struct Loader {
                 __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, 0x7fffffff, kBufferFlags);
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
             typedef __attribute__((address_space(3))) void lds_void;
-#pragma unroll
-            for (int j = 0; j < kJobs; ++j) {
-                unsigned o = off[j];
-                if (left < stage_k<T>()) {
-                    const int64_t k = RC ? line + j * kRowStep : chunk * chunk_n<T>();
-                    if (k >= left) o = kOutside;
-                }
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + j * THREADS * 16 + wave * 1024), 16, o, 0, 0, 0);
+            unsigned o = off[j];
+            if (left < stage_k<T, SB>()) {
+                const int64_t k = RC ? line + j * kRowStep : chunk * chunk_n<T>();
+                if (k >= left) o = kOutside;
             }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + j * THREADS * 16 + wave * 1024), 16, o, 0, 0, 0);
         } else {
-#pragma unroll
-            for (int j = 0; j < kJobs; ++j) {
-                const int row = line + j * kRowStep;
-                u32x4 v = {0, 0, 0, 0};
-                const int64_t where = (int64_t)row * ld + chunk * 16;
-                const int64_t avail = bytes - (at - base) - where;
-                if (RC) {
-                    if (row < left && chunk * chunk_n<T>() < count) v = chunk_at<T>(at + where, avail);
-                } else if (row < count && chunk * chunk_n<T>() < left) {
-                    v = chunk_at<T>(at + where, avail);
-                    v = keep_first<T>(v, left - chunk * chunk_n<T>());
-                }
-                reg[j] = v;
+            const int row = line + j * kRowStep;
+            u32x4 v = {0, 0, 0, 0};
+            const int64_t where = (int64_t)row * ld + chunk * 16;
+            const int64_t avail = bytes - (at - base) - where;
+            if (RC) {
+                if (row < left && chunk * chunk_n<T>() < count) v = chunk_at<T>(at + where, avail);
+            } else if (row < count && chunk * chunk_n<T>() < left) {
+                v = chunk_at<T>(at + where, avail);
+                v = keep_first<T>(v, left - chunk * chunk_n<T>());
             }
+            reg[j] = v;
         }
+    }
+    __device__ __forceinline__ void fetch(int64_t k0, int64_t K, char *lds)
+    {
+#pragma unroll
+        for (int j = 0; j < kJobs; ++j) fetch_job(j, k0, K, lds);
     }
     __device__ __forceinline__ void put(char *lds)
     {
@@ -200,8 +201,8 @@ template <class T, int R, bool RC, int THREADS, bool DMA> struct Loader {
 };
 
 // Reads operands of the matrix instruction from a stage: block of 32 rows or columns at 32 * t + first, step kk of 4.
-template <class T, int R, bool RC> struct Reader {
-    int at[4];              // KC: by kk; RC: unused
+template <class T, int R, bool RC, int SB = kStageBytes> struct Reader {
+    int at[SB / 32];        // KC: by kk; RC: unused
     int lane, first;
 
     __device__ __forceinline__ void open(int first_)
@@ -211,13 +212,12 @@ template <class T, int R, bool RC> struct Reader {
         if (!RC) {
             const int row = first + (lane & 31);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-                at[kk] = row * kStageBytes + (((2 * kk + (lane >> 5)) ^ ((row >> 1) & 7)) << 4);
+            for (int kk = 0; kk < SB / 32; ++kk) at[kk] = row * SB + (((2 * kk + (lane >> 5)) ^ kc_shift<SB>(row)) << 4);
         }
     }
     __device__ __forceinline__ u32x4 read(const char *lds, int t, int kk) const
     {
-        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * 32 * kStageBytes);
+        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * 32 * SB);
         constexpr int pitch = R * Type<T>::kBytes;
         u32x4 v;
         if (Type<T>::kBytes == 2) {
@@ -251,16 +251,19 @@ template <int N> __device__ __forceinline__ void wait_loads()      // until at m
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A tile of BM x BN by WM x WN waves.
-template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_> struct Tile {
+template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_, int SB_ = kStageBytes> struct Tile {
     using T = T_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = DMA_ ? STAGES_ : 2, THREADS = 64 * WM * WN;
     static constexpr bool PRC = PRC_, QRC = QRC_, DMA = DMA_;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;      // 32 x 32 tiles of a wave
-    static constexpr int kLdsP = BM * kStageBytes, kLdsQ = BN * kStageBytes, kLdsStage = kLdsP + kLdsQ;
+    static constexpr int SB = SB_, SK = stage_k<T, SB>();          // bytes of k in a stage, and k
+    static constexpr int kLdsP = BM * SB, kLdsQ = BN * SB, kLdsStage = kLdsP + kLdsQ;
     static constexpr int kLds = STAGES * kLdsStage;
     using Acc = f32x16[TM][TN];
-    using LoadP = Loader<T, BM, PRC, THREADS, DMA>;
-    using LoadQ = Loader<T, BN, QRC, THREADS, DMA>;
+    using LoadP = Loader<T, BM, PRC, THREADS, DMA, SB>;
+    using LoadQ = Loader<T, BN, QRC, THREADS, DMA, SB>;
+    using ReadP = Reader<T, BM, PRC, SB>;
+    using ReadQ = Reader<T, BN, QRC, SB>;
 
     static __device__ __forceinline__ void clear(Acc &acc)
     {
@@ -272,19 +275,41 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
     }
 
-    static __device__ __forceinline__ void step(const char *lds, const Reader<T, BM, PRC> &rp, const Reader<T, BN, QRC> &rq, Acc &acc)
+    // One stage.  The operands of a matrix step are read while the one before runs; load(n) asks for chunk n of the next
+    // stage.  A chunk of all lanes keeps the load unit busy for 16 cycles, so the large tile spreads them over its products,
+    // one after every second (256 x 256, 8192 x 8192 x 4096, bf16: 443 us, all at the start 478; 448 after every fourth); a
+    // tile with few products asks first (32 x 128 over 64 groups of 4096 x 2048: 165 us, spread 242).
+    template <class F>
+    static __device__ __forceinline__ void step(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc, F load)
     {
+        constexpr int KK = SB / 32, L = LoadP::kJobs + LoadQ::kJobs;
+        constexpr bool spread = KK * TM * TN >= 4 * L;
+        u32x4 p[2][TM], q[2][TN];
+        auto get = [&](int kk) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            u32x4 p[TM], q[TN];
+            for (int j = 0; j < TN; ++j) q[kk & 1][j] = rq.read(lds + kLdsP, j, kk);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) p[i] = rp.read(lds, i, kk);
+            for (int i = 0; i < TM; ++i) p[kk & 1][i] = rp.read(lds, i, kk);
+        };
+        int done = 0;
+        if (!spread)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) q[j] = rq.read(lds + kLdsP, j, kk);
+            for (; done < L; ++done) load(done);
+        get(0);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kk + 1 < KK) get(kk + 1);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[j], p[i], acc[i][j]);
+                for (int j = 0; j < TN; ++j) {
+                    acc[i][j] = Type<T>::mac(q[kk & 1][j], p[kk & 1][i], acc[i][j]);
+                    if (spread && ((kk * TM + i) * TN + j) % 2 == 0 && done < L) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        load(done++);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
         }
     }
 
@@ -296,26 +321,27 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
         LoadQ lq;
         lp.open(P);
         lq.open(Q);
-        Reader<T, BM, PRC> rp;
-        Reader<T, BN, QRC> rq;
+        ReadP rp;
+        ReadQ rq;
         rp.open(wave / WN * (BM / WM));
         rq.open(wave % WN * (BN / WN));
-        const int steps = (int)((k1 - k0 + stage_k<T>() - 1) / stage_k<T>());
+        const int steps = (int)((k1 - k0 + SK - 1) / SK);
         if (DMA) {
             constexpr int L = LoadP::kJobs + LoadQ::kJobs;
 #pragma unroll
             for (int s = 0; s < STAGES - 1; ++s) {
-                lp.fetch(k0 + (int64_t)s * stage_k<T>(), k1, lds + s * kLdsStage);
-                lq.fetch(k0 + (int64_t)s * stage_k<T>(), k1, lds + s * kLdsStage + kLdsP);
+                lp.fetch(k0 + (int64_t)s * SK, k1, lds + s * kLdsStage);
+                lq.fetch(k0 + (int64_t)s * SK, k1, lds + s * kLdsStage + kLdsP);
             }
             int from = 0, to = STAGES - 1;
             for (int s = 0; s < steps; ++s) {
                 wait_loads<(STAGES - 2) * L>();
                 meet();
-                const int64_t k = k0 + (int64_t)(s + STAGES - 1) * stage_k<T>();
-                lp.fetch(k, k1, lds + to * kLdsStage);
-                lq.fetch(k, k1, lds + to * kLdsStage + kLdsP);
-                step(lds + from * kLdsStage, rp, rq, acc);
+                const int64_t k = k0 + (int64_t)(s + STAGES - 1) * SK;
+                step(lds + from * kLdsStage, rp, rq, acc, [&](int n) {
+                    if (n < LoadQ::kJobs) lq.fetch_job(n, k, k1, lds + to * kLdsStage + kLdsP);
+                    else lp.fetch_job(n - LoadQ::kJobs, k, k1, lds + to * kLdsStage);
+                });
                 from = from + 1 == STAGES ? 0 : from + 1;
                 to = to + 1 == STAGES ? 0 : to + 1;
             }
@@ -329,10 +355,10 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 meet();
                 const bool more = s + 1 < steps;
                 if (more) {
-                    lp.fetch(k0 + (int64_t)(s + 1) * stage_k<T>(), k1, nullptr);
-                    lq.fetch(k0 + (int64_t)(s + 1) * stage_k<T>(), k1, nullptr);
+                    lp.fetch(k0 + (int64_t)(s + 1) * SK, k1, nullptr);
+                    lq.fetch(k0 + (int64_t)(s + 1) * SK, k1, nullptr);
                 }
-                step(lds + (s & 1) * kLdsStage, rp, rq, acc);
+                step(lds + (s & 1) * kLdsStage, rp, rq, acc, [](int) {});
                 if (more) {
                     lp.put(lds + ((s + 1) & 1) * kLdsStage);
                     lq.put(lds + ((s + 1) & 1) * kLdsStage + kLdsP);
@@ -342,37 +368,52 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
         meet();
     }
 
-    // Entries (row, column) of the tile inside rows x cols to out (ld entries from row to row), four columns at a time;
-    // vec: out + row * ld is a multiple of four entries' bytes for each row.
+    // Entries (row, column) of the tile inside rows x cols to out (ld entries from row to row).  A lane's accumulators are
+    // four columns at a time of one row; through LDS, 32 rows of a wave at a time, whole lines leave together.
+    // vec: rows of out begin on 16-byte borders.  lds: as much as multiply had, free.
     template <class O>
-    static __device__ __forceinline__ void store(const Acc &acc, O *out, int64_t ld, int64_t rows, int64_t cols, bool vec, float scale = 1.f)
+    static __device__ __forceinline__ void store(const Acc &acc, O *out, int64_t ld, int64_t rows, int64_t cols, bool vec, char *lds,
+                                                 float scale = 1.f)
     {
+        constexpr int W = TN * 32, N = 16 / (int)sizeof(O), kPitch = W * (int)sizeof(O) + 16, kLanes = W / N, kAtOnce = 64 / kLanes;
+        static_assert(32 * kPitch * WM * WN <= kLds, "the waves' rows fit");
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-        const int r0 = wave / WN * (BM / WM) + (lane & 31), c0 = wave % WN * (BN / WN) + 4 * (lane >> 5);
+        char *mine = lds + wave * (32 * kPitch);
+        const int first = wave / WN * (BM / WM), col = wave % WN * (BN / WN) + lane % kLanes * N, up = lane / kLanes;
+        const int have = cols - col < N ? (int)(cols - col) : N;
+        O *at = out + (int64_t)(first + up) * ld + col;
+        const int64_t step = ld * kAtOnce;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int row = r0 + 32 * i;
-            if (row >= rows) continue;
-            O *line = out + (int64_t)row * ld;
+            if (first + 32 * i >= rows) break;
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const int col = c0 + 32 * j + 8 * v;
-                    float x[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * v + e] * scale;
-                    if (vec && col + 4 <= cols) {
-                        if constexpr (sizeof(O) == 4)
-                            *reinterpret_cast<f32x4 *>(line + col) = f32x4{x[0], x[1], x[2], x[3]};
-                        else
-                            *reinterpret_cast<u32x2 *>(line + col) = u32x2{Type<O>::round2(x[0], x[1]), Type<O>::round2(x[2], x[3])};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < cols) line[col + e] = Type<O>::round(x[e]);
-                    }
+                    const f32x4 x = {acc[i][j][4 * v] * scale, acc[i][j][4 * v + 1] * scale, acc[i][j][4 * v + 2] * scale,
+                                     acc[i][j][4 * v + 3] * scale};
+                    char *to = mine + (lane & 31) * kPitch + (32 * j + 8 * v + 4 * (lane >> 5)) * (int)sizeof(O);
+                    if constexpr (sizeof(O) == 4) *reinterpret_cast<f32x4 *>(to) = x;
+                    else *reinterpret_cast<u32x2 *>(to) = u32x2{Type<O>::round2(x[0], x[1]), Type<O>::round2(x[2], x[3])};
                 }
+            u32x4 w[32 / kAtOnce];
+#pragma unroll
+            for (int r = 0; r < 32 / kAtOnce; ++r)
+                w[r] = *reinterpret_cast<const u32x4 *>(mine + (up + r * kAtOnce) * kPitch + lane % kLanes * 16);
+#pragma unroll
+            for (int r = 0; r < 32 / kAtOnce; ++r, at += step) {
+                if (first + 32 * i + up + r * kAtOnce >= rows) continue;
+                if (vec && have == N) {
+                    *reinterpret_cast<u32x4 *>(at) = w[r];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e < have) {
+                            if constexpr (sizeof(O) == 4) at[e] = __uint_as_float(w[r][e]);
+                            else at[e] = O{(unsigned short)(w[r][e >> 1] >> (16 * (e & 1)))};
+                        }
+                }
+            }
         }
     }
 };
@@ -388,60 +429,70 @@ __device__ __forceinline__ void range_of(const int64_t *offsets, int g, int64_t 
     hi = hi < lo ? lo : (hi > rows ? rows : hi);
 }
 
-// Row tiles of BM rows of all ranges, in order; every wave looks by itself, 64 ranges at a time.  Returns how many there are;
-// where `want` is one of them, its range g and rows [r0, r1).
+// Row tiles of BM rows of all ranges, in order; every wave looks by itself, 64 ranges at a time.
 struct Found {
-    int g;
-    int64_t r0, r1;
+    int g;              // range
+    int64_t r0, r1;     // its rows [r0, r1)
 };
-__device__ __forceinline__ int count_tiles(const int64_t *offsets, int groups, int64_t rows, int BM)
-{
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int base = 0; base < groups; base += 64) {
-        int nt = 0;
-        if (base + lane < groups) {
-            int64_t lo, hi;
-            range_of(offsets, base + lane, rows, lo, hi);
-            nt = (int)((hi - lo + BM - 1) / BM);
-        }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) nt += __shfl_xor(nt, d);
-        total += nt;
-    }
-    return __builtin_amdgcn_readfirstlane(total);
-}
-__device__ __forceinline__ bool find_tile(const int64_t *offsets, int groups, int64_t rows, int BM, int want, Found &f)
-{
-    const int lane = threadIdx.x & 63;
-    for (int base = 0; base < groups; base += 64) {
-        int nt = 0;
-        int64_t lo = 0, hi = 0;
-        if (base + lane < groups) {
-            range_of(offsets, base + lane, rows, lo, hi);
-            nt = (int)((hi - lo + BM - 1) / BM);
-        }
-        int sum = nt;
+struct Ranges {
+    const int64_t *offsets;
+    int groups, BM;
+    int64_t rows, lo, hi;        // of the lane's range
+    int count, sum, base;        // its tiles, and those up to and with it among the 64 from `base` on
+
+    __device__ __forceinline__ void look(int base_)
+    {
+        const int lane = threadIdx.x & 63;
+        base = base_;
+        lo = hi = 0;
+        if (base + lane < groups) range_of(offsets, base + lane, rows, lo, hi);
+        count = (int)((hi - lo + BM - 1) / BM);
+        sum = count;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int o = __shfl_up(sum, d);
             if (lane >= d) sum += o;
         }
-        const unsigned long long past = __ballot(sum > want);
-        if (past) {
-            const int l = __ffsll(past) - 1;
-            const int before = __shfl(sum - nt, l);
-            const int64_t l0 = __shfl(lo, l), h0 = __shfl(hi, l);
-            f.g = __builtin_amdgcn_readfirstlane(base + l);
-            const int64_t r0 = l0 + (int64_t)(want - before) * BM;
-            f.r0 = r0;
-            f.r1 = h0 < r0 + BM ? h0 : r0 + BM;
-            return true;
-        }
-        want -= __shfl(sum, 63);
     }
-    return false;
-}
+    __device__ __forceinline__ int open(const int64_t *offsets_, int groups_, int64_t rows_, int BM_)      // returns how many tiles there are
+    {
+        offsets = offsets_;
+        groups = groups_;
+        rows = rows_;
+        BM = BM_;
+        int total = 0;
+        for (int b = groups > 0 ? (groups - 1) / 64 * 64 : 0; b >= 0; b -= 64) {
+            look(b);
+            total += __builtin_amdgcn_readlane(sum, 63);
+        }
+        return total;
+    }
+    // Tile `want`, counted from the ranges looked at now (the first 64 after open).
+    __device__ __forceinline__ bool find(int want, Found &f)
+    {
+        if (base != 0) look(0);
+        for (;;) {
+            const unsigned long long past = __ballot(sum > want);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                f.g = base + l;
+                const int before = __builtin_amdgcn_readlane(sum - count, l);
+                const int64_t l0 = lane_value(lo, l), h0 = lane_value(hi, l);
+                f.r0 = l0 + (int64_t)(want - before) * BM;
+                f.r1 = h0 < f.r0 + BM ? h0 : f.r0 + BM;
+                return true;
+            }
+            want -= __builtin_amdgcn_readlane(sum, 63);
+            if (base + 64 >= groups) return false;
+            look(base + 64);
+        }
+    }
+    static __device__ __forceinline__ int64_t lane_value(int64_t x, int l)
+    {
+        return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)x, l) |
+                         (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32);
+    }
+};
 // First range that ends behind row r (ranges in order), or `groups`.
 __device__ __forceinline__ int first_range(const int64_t *offsets, int groups, int64_t r)
 {

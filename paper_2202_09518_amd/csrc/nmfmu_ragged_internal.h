@@ -47,7 +47,7 @@ struct Product {
     int shrink_splits;           // parts of u
     int64_t shrink_k;
     float *upart;                // shrink_splits x rows x kmax, where there are several
-    bool vec;                    // rows of y can take four entries at once
+    bool vec;                    // rows of y begin on 16-byte borders
 };
 
 struct Gradient {

@@ -92,7 +92,7 @@ __device__ __forceinline__ void add_adapters(const Product &a, int64_t r0, int64
     const int first = wave / C::WN * (C::BM / C::WM);
     rp.open(first);
     rq.open(wave % C::WN * (C::BN / C::WN));
-    char *lq = lds + C::kLdsP;
+    char *lq = lds + C::BM * kStageBytes;
     for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
         int64_t lo, hi;
         range_of(a.ad.offsets, s, a.rows, lo, hi);
@@ -196,7 +196,9 @@ template <class C> __device__ __forceinline__ void shrink_tile(const Product &a,
     const int split = id % a.shrink_splits;
     id /= a.shrink_splits;
     Found f;
-    if (!find_tile(a.ad.offsets, a.ad.segments, a.rows, C::BM, id / ct, f)) return;
+    Ranges ranges;
+    ranges.open(a.ad.offsets, a.ad.segments, a.rows, C::BM);
+    if (!ranges.find(id / ct, f)) return;
     const Run run = run_of(a.ad, f.g);
     const int c0 = id % ct * C::BN;
     if (c0 >= run.k) return;
@@ -209,7 +211,7 @@ template <class C> __device__ __forceinline__ void shrink_tile(const Product &a,
     float *out = a.ad.u;
     if (a.shrink_splits > 1) out = a.upart + (int64_t)split * a.rows * a.ad.kmax;
     const float scale = a.ad.scale ? a.ad.scale[a.ad.run[f.g]] : 1.f;
-    C::store(acc, out + f.r0 * a.ad.kmax + c0, a.ad.kmax, f.r1 - f.r0, run.k - c0, false, scale);
+    C::store(acc, out + f.r0 * a.ad.kmax + c0, a.ad.kmax, f.r1 - f.r0, run.k - c0, false, lds, scale);
 }
 
 template <class S> __global__ __launch_bounds__(S::THREADS) void shrink_kernel(Product a)
@@ -230,7 +232,8 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
             return;
         }
     }
-    const int rt = a.offsets ? count_tiles(a.offsets, a.groups, a.rows, C::BM) : (int)((a.rows + C::BM - 1) / C::BM);
+    Ranges ranges;
+    const int rt = a.offsets ? ranges.open(a.offsets, a.groups, a.rows, C::BM) : (int)((a.rows + C::BM - 1) / C::BM);
     const int ct = (int)((a.n + C::BN - 1) / C::BN);
     const int each = rt * ct, total = each * a.splits, mine = blockIdx.x - shrink;
     if (mine >= total) return;
@@ -243,7 +246,7 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
     const int64_t c0 = (int64_t)(in / high) * C::BN;
     Found f = {0, (int64_t)r * C::BM, 0};
     if (a.offsets) {
-        if (!find_tile(a.offsets, a.groups, a.rows, C::BM, r, f)) return;
+        if (!ranges.find(r, f)) return;
     } else {
         f.r1 = f.r0 + C::BM < a.rows ? f.r0 + C::BM : a.rows;
     }
@@ -256,11 +259,11 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
     C::multiply(P, Q, k0, k1, lds, acc);
     if (a.splits > 1) {
         const int64_t n4 = up4(a.n);
-        C::store(acc, a.part + ((int64_t)split * a.rows + f.r0) * n4 + c0, n4, f.r1 - f.r0, a.n - c0, true);
+        C::store(acc, a.part + ((int64_t)split * a.rows + f.r0) * n4 + c0, n4, f.r1 - f.r0, a.n - c0, true, lds);
         return;
     }
     if constexpr (ADAPTERS) add_adapters<C>(a, f.r0, f.r1, c0, lds, acc);
-    C::store(acc, (T *)a.y + f.r0 * a.ldy + c0, a.ldy, f.r1 - f.r0, a.n - c0, a.vec);
+    C::store(acc, (T *)a.y + f.r0 * a.ldy + c0, a.ldy, f.r1 - f.r0, a.n - c0, a.vec, lds);
 }
 
 // Y of one row and 1024 columns from the parts, in order, and its adapter.
@@ -336,9 +339,9 @@ template <class C> __global__ __launch_bounds__(C::THREADS) void gradient_kernel
     if (k1 > k0) C::multiply(P, Q, k0, k1, lds, acc);
     if (a.splits > 1) {
         const int64_t n4 = up4(a.n);
-        C::store(acc, a.part + (((int64_t)split * a.groups + g) * a.m + r0) * n4 + c0, n4, a.m - r0, a.n - c0, true);
+        C::store(acc, a.part + (((int64_t)split * a.groups + g) * a.m + r0) * n4 + c0, n4, a.m - r0, a.n - c0, true, lds);
     } else {
-        C::store(acc, (T *)a.g + g * a.stride_g + r0 * a.ldg + c0, a.ldg, a.m - r0, a.n - c0, a.vec);
+        C::store(acc, (T *)a.g + g * a.stride_g + r0 * a.ldg + c0, a.ldg, a.m - r0, a.n - c0, a.vec, lds);
     }
 }
 
