@@ -59,8 +59,12 @@ Plan gradient_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_
 int shrink_plan(int32_t type, int64_t rows, int64_t segments, int64_t m, int kmax)
 {
     const int64_t tiles = (ceil_div(rows, kShrinkRows) + std::min(segments, rows)) * ceil_div(kmax, kShrinkCols);
-    return rows > 4096 ? 1 : splits_for(tiles, m, stage_of(type));
+    return splits_for(tiles, m, stage_of(type));
 }
+
+// A tile runs its segments' adapters one after the other, 2.5 us each; where segments are short, the launch that joins parts
+// adds the adapters row by row, for the price of the product's floats written and read once (26 us for a tile of 256 x 256).
+bool joined_plan(int64_t rows, int64_t segments, int splits) { return splits > 1 || rows < 24 * segments; }
 
 int factor_plan(int32_t type, int64_t rows, int64_t runs, int64_t m, int64_t n, int kmax)
 {
@@ -68,8 +72,9 @@ int factor_plan(int32_t type, int64_t rows, int64_t runs, int64_t m, int64_t n, 
     return splits_for(tiles, ceil_div(rows, runs), stage_of(type));
 }
 
-size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (size_t)splits * rows * up4(n) * 4 : 0; }
+size_t product_part(int64_t rows, int64_t n, int splits) { return (size_t)splits * rows * up4(n) * 4; }
 size_t shrink_part(int64_t rows, int kmax, int splits) { return splits > 1 ? (size_t)splits * up4(rows * kmax) * 4 : 0; }
+size_t pack_part(int64_t rows, int kmax) { return (size_t)rows * (4 * ceil_div(kmax, 32) * 32) + (size_t)up4(rows) * 4; }
 size_t gradient_part(int64_t groups, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * groups * m * up4(n) * 4 : 0; }
 size_t factor_part(int64_t ktotal, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * ktotal * (up4(m) + up4(n)) * 4 : 0; }
 
@@ -131,11 +136,12 @@ int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t 
     p.b = B; p.ldb = ldb; p.stride_b = stride_b; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
     p.shape = plan.shape;
     p.splits = fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); });
+    p.joined = p.splits > 1;
     p.k_split = ceil_div(ceil_div(m, stage_of(type)), p.splits) * stage_of(type);
     p.part = static_cast<float *>(work);
     p.shrink_splits = 1;
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
-    if ((rc = check_grid(product_grid(p)))) return rc;
+    if ((rc = check_grid(std::max(product_grid(p), p.joined ? rows * ceil_div(n, 256) : 0)))) return rc;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
 }
 
@@ -190,18 +196,29 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
     p.shape = plan.shape;
     p.shrink_splits = 1;
     const int stage = stage_of(type);
-    if (segments) {
-        p.shrink_splits = fit(shrink_plan(type, rows, segments, m, kmax), work_bytes, [&](int s) { return shrink_part(rows, kmax, s); });
-        p.shrink_k = ceil_div(ceil_div(m, stage), p.shrink_splits) * stage;
-        p.upart = static_cast<float *>(work);
+    char *at = static_cast<char *>(work), *end = at + work_bytes;
+    p.joined = joined_plan(rows, segments, plan.splits) && product_part(rows, n, 1) <= work_bytes;
+    p.splits = p.joined ? fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); }) : 1;
+    if (p.joined && p.splits == 1 && !segments) p.joined = false;
+    if (p.joined) {
+        p.part = reinterpret_cast<float *>(at);
+        at += product_part(rows, n, p.splits);
+    } else if (segments && pack_part(rows, kmax) <= work_bytes) {
+        p.pack = at;
+        at += pack_part(rows, kmax);
+        p.row_scale = reinterpret_cast<float *>(at) - up4(rows);
     }
-    const size_t used = segments ? shrink_part(rows, kmax, p.shrink_splits) : 0;
-    p.splits = fit(plan.splits, work_bytes - used, [&](int s) { return product_part(rows, n, s); });
     p.k_split = ceil_div(ceil_div(m, stage), p.splits) * stage;
-    p.part = reinterpret_cast<float *>(static_cast<char *>(work) + used);
+    if (segments) {
+        // parts of u are added up by the launch that joins y or that packs u
+        if (p.joined || p.pack)
+            p.shrink_splits = fit(shrink_plan(type, rows, segments, m, kmax), end - at, [&](int s) { return shrink_part(rows, kmax, s); });
+        p.shrink_k = ceil_div(ceil_div(m, stage), p.shrink_splits) * stage;
+        p.upart = reinterpret_cast<float *>(at);
+    }
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
     const int64_t shrink = segments ? (ceil_div(rows, kShrinkRows) + segments) * ceil_div(kmax, kShrinkCols) * p.shrink_splits : 0;
-    if ((rc = check_grid(product_grid(p) + shrink))) return rc;
+    if ((rc = check_grid(std::max(product_grid(p) + shrink, p.joined ? rows * ceil_div(n, 256) : 0)))) return rc;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
 }
 
@@ -238,12 +255,19 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
 {
     if (type < NMF_F32 || type > NMF_F16 || !sizes_ok(rows, m, n) || rows == 0) return 0;
     switch (kind) {
-    case 0: return parts < 1 ? 0 : product_part(rows, n, product_plan(type, rows, parts, m, n).splits);
+    case 0: {
+        if (parts < 1) return 0;
+        const int splits = product_plan(type, rows, parts, m, n).splits;
+        return splits > 1 ? product_part(rows, n, splits) : 0;
+    }
     case 1: return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits);
-    case 2:
+    case 2: {
         if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K) return 0;
-        return product_part(rows, n, product_plan(type, rows, 1, m, n).splits) +
-               (parts ? shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax)) : 0);
+        const int splits = product_plan(type, rows, 1, m, n).splits;
+        if (parts == 0) return splits > 1 ? product_part(rows, n, splits) : 0;
+        return (joined_plan(rows, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
+               shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax));
+    }
     case 3:
         if (runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
         return factor_part(ktotal, m, n, factor_plan(type, rows, runs, m, n, kmax));

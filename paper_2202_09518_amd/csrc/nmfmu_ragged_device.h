@@ -86,6 +86,8 @@ struct Operand {
     int64_t ld;              // bytes from row to row (KC) or from k to k (RC)
     int64_t count;           // rows (KC) or columns (RC) of the tile that exist; may be 0 or less
     int64_t bytes;           // from base to the end of the array: nothing is read from there on
+    int first = 0;           // KC: rows before this one are zero
+    int64_t plane = 0;       // operands in two planes: bytes from the first to the second
 };
 
 // 16 bytes of which only those before `bytes` may be read; the others are zero.
@@ -123,9 +125,10 @@ template <class T> __device__ __forceinline__ u32x4 keep_first(u32x4 v, int64_t 
 }
 
 // Brings stages of an operand (R rows or columns) into LDS with THREADS threads.
+// PLANES 2: half a stage is k of the first plane, the other half the same k of the second.
 // DMA: base, ld and the extents are multiples of 16 bytes: the chunks go to LDS without passing registers; a chunk that is
 // not there is asked for outside the descriptor's range, which delivers zeros.  Else: any alignment, through registers.
-template <class T, int R, bool RC, int THREADS, bool DMA, int SB> struct Loader {
+template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> struct Loader {
     static constexpr int kJobs = R * (SB / 16) / THREADS;            // chunks of a thread
     static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : SB / 16;
     static constexpr int kRowStep = THREADS / kRowChunks;            // rows from job to job
@@ -134,29 +137,43 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB> struct Loader 
 
     const char *base;
     int64_t ld, bytes;
-    int line, chunk;           // LDS line (row or k) and source chunk of job 0
-    int count;
+    int line, chunk;           // LDS line (row or k) and chunk of job 0
+    int first, count;
+    int64_t plane;
     unsigned off[kJobs];
     u32x4 reg[DMA ? 1 : kJobs];
 
+    // k of job j within its plane's part of a stage, and where its chunk lies from the stage's first k on.
+    __device__ __forceinline__ int k_of(int j) const
+    {
+        return RC ? (line + j * kRowStep) % (stage_k<T, SB>() / PLANES) : chunk % (SB / 16 / PLANES) * chunk_n<T>();
+    }
+    __device__ __forceinline__ int64_t where(int j) const
+    {
+        const int row = line + j * kRowStep;
+        if (RC) return k_of(j) * ld + chunk * 16 + (PLANES == 2 && row >= stage_k<T, SB>() / 2 ? plane : 0);
+        return (int64_t)row * ld + k_of(j) * Type<T>::kBytes + (PLANES == 2 && chunk >= SB / 32 ? plane : 0);
+    }
+    __device__ __forceinline__ bool there(int j) const
+    {
+        const int row = line + j * kRowStep;
+        return RC ? chunk * chunk_n<T>() < count : row >= first && row < count;
+    }
     __device__ __forceinline__ void open(const Operand &o)
     {
         base = o.base;
         ld = o.ld;
         bytes = o.bytes;
+        first = o.first;
+        plane = o.plane;
         count = (int)(o.count < 0 ? 0 : (o.count > R ? R : o.count));
         const int tid = threadIdx.x;
         line = tid / kRowChunks;
         const int place = tid % kRowChunks;
         chunk = RC ? place ^ rc_shift<T, R>(line) : place ^ kc_shift<SB>(line);
-        if (DMA) {
+        if (DMA)
 #pragma unroll
-            for (int j = 0; j < kJobs; ++j) {
-                const int row = line + j * kRowStep;
-                const bool there = RC ? chunk * chunk_n<T>() < count : row < count;
-                off[j] = there ? (unsigned)(row * ld) + (unsigned)chunk * 16u : kOutside;
-            }
-        }
+            for (int j = 0; j < kJobs; ++j) off[j] = there(j) ? (unsigned)where(j) : kOutside;
     }
     // Chunk j of the stage at k0 (of K in all) to `lds`, or to a register.
     __device__ __forceinline__ void fetch_job(int j, int64_t k0, int64_t K, char *lds)
@@ -169,21 +186,13 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB> struct Loader 
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
             typedef __attribute__((address_space(3))) void lds_void;
             unsigned o = off[j];
-            if (left < stage_k<T, SB>()) {
-                const int64_t k = RC ? line + j * kRowStep : chunk * chunk_n<T>();
-                if (k >= left) o = kOutside;
-            }
+            if (left < stage_k<T, SB>() / PLANES && k_of(j) >= left) o = kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + j * THREADS * 16 + wave * 1024), 16, o, 0, 0, 0);
         } else {
-            const int row = line + j * kRowStep;
             u32x4 v = {0, 0, 0, 0};
-            const int64_t where = (int64_t)row * ld + chunk * 16;
-            const int64_t avail = bytes - (at - base) - where;
-            if (RC) {
-                if (row < left && chunk * chunk_n<T>() < count) v = chunk_at<T>(at + where, avail);
-            } else if (row < count && chunk * chunk_n<T>() < left) {
-                v = chunk_at<T>(at + where, avail);
-                v = keep_first<T>(v, left - chunk * chunk_n<T>());
+            if (there(j) && k_of(j) < left) {
+                v = chunk_at<T>(at + where(j), bytes - (at - base) - where(j));
+                v = keep_first<T>(v, RC ? count - chunk * chunk_n<T>() : left - k_of(j));
             }
             reg[j] = v;
         }
@@ -251,17 +260,17 @@ template <int N> __device__ __forceinline__ void wait_loads()      // until at m
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A tile of BM x BN by WM x WN waves.
-template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_, int SB_ = kStageBytes> struct Tile {
+template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_, int SB_ = kStageBytes, int PLANES_ = 1> struct Tile {
     using T = T_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = DMA_ ? STAGES_ : 2, THREADS = 64 * WM * WN;
     static constexpr bool PRC = PRC_, QRC = QRC_, DMA = DMA_;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;      // 32 x 32 tiles of a wave
-    static constexpr int SB = SB_, SK = stage_k<T, SB>();          // bytes of k in a stage, and k
+    static constexpr int SB = SB_, PLANES = PLANES_, SK = stage_k<T, SB>() / PLANES;      // bytes of k in a stage; its k
     static constexpr int kLdsP = BM * SB, kLdsQ = BN * SB, kLdsStage = kLdsP + kLdsQ;
     static constexpr int kLds = STAGES * kLdsStage;
     using Acc = f32x16[TM][TN];
-    using LoadP = Loader<T, BM, PRC, THREADS, DMA, SB>;
-    using LoadQ = Loader<T, BN, QRC, THREADS, DMA, SB>;
+    using LoadP = Loader<T, BM, PRC, THREADS, DMA, SB, PLANES>;
+    using LoadQ = Loader<T, BN, QRC, THREADS, DMA, SB, PLANES>;
     using ReadP = Reader<T, BM, PRC, SB>;
     using ReadQ = Reader<T, BN, QRC, SB>;
 
@@ -505,6 +514,17 @@ __device__ __forceinline__ int first_range(const int64_t *offsets, int groups, i
     return groups;
 }
 
+// The same for a lane's own row.
+__device__ __forceinline__ int range_at(const int64_t *offsets, int groups, int64_t r)
+{
+    int lo = 0, hi = groups;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (offsets[mid + 1] > r) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
 // Workgroups are dealt to the eight dies in turn, each with a cache of its own: a die gets neighbouring tiles.
 __device__ __forceinline__ int by_die(int id, int total)
 {

@@ -42,11 +42,14 @@ struct Product {
     Adapters ad;                 // ad.segments == 0: none
     // plan
     int shape, splits;
+    bool joined;                 // y comes from parts (one at least), which a second launch joins; needs part
     int64_t k_split;             // k of a split, whole stages
-    float *part;                 // splits x rows x (n rounded up to 4); 
+    float *part;                 // splits x rows x (n rounded up to 4)
     int shrink_splits;           // parts of u
     int64_t shrink_k;
     float *upart;                // shrink_splits x rows x kmax, where there are several
+    void *pack;                  // u as an operand, rows x 4 bytes x kmax in whole 32s, and for f16 a scale of each row;
+    float *row_scale;            // null: none (slow)
     bool vec;                    // rows of y begin on 16-byte borders
 };
 

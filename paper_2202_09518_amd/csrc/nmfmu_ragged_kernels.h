@@ -4,6 +4,8 @@
 #include "nmfmu_ragged_internal.h"
 #include "nmfmu_ragged_device.h"
 
+#include <type_traits>
+
 namespace nmfmu {
 namespace ragged {
 
@@ -77,115 +79,199 @@ __device__ __forceinline__ Run run_of(const Adapters &a, int segment)
     return r;
 }
 
-// acc += u H_r for the rows of a tile, segment by segment, 32 factors at a time; u lies scaled in memory.
-// A segment's product is formed on its own and added in its rows only: factors that are not finite reach no other
-// request's rows.
-template <class C>
-__device__ __forceinline__ void add_adapters(const Product &a, int64_t r0, int64_t r1, int64_t c0, char *lds, typename C::Acc &acc)
-{
-    using T = typename C::T;
-    using E = typename Cut<T>::E;
-    constexpr int EN = chunk_n<E>();
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    Reader<E, C::BM, false> rp;
-    Reader<E, C::BN, true> rq;
-    const int first = wave / C::WN * (C::BM / C::WM);
-    rp.open(first);
-    rq.open(wave % C::WN * (C::BN / C::WN));
-    char *lq = lds + C::BM * kStageBytes;
-    for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
-        int64_t lo, hi;
-        range_of(a.ad.offsets, s, a.rows, lo, hi);
-        if (lo >= r1) break;
-        const int from = (int)((lo > r0 ? lo : r0) - r0), to = (int)((hi < r1 ? hi : r1) - r0);
-        const Run run = run_of(a.ad, s);
-        if (run.k == 0 || to <= from) continue;
-        for (int kc = 0; kc < run.k; kc += 32) {
-            for (int q = threadIdx.x; q < C::BM * 32 / EN; q += C::THREADS) {
-                const int row = q / (32 / EN), c = q % (32 / EN), swz = (row >> 1) & 7;
-                const bool in = row >= from && row < to;
-                const int64_t line = (r0 + (in ? row : from)) * a.ad.kmax;
-                float x[EN];
-                if (a.shrink_splits == 1) {
-                    floats_at<EN>(a.ad.u + line, kc + c * EN, in ? run.k : 0, x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < EN; ++e) x[e] = 0.f;
-                    for (int s2 = 0; s2 < a.shrink_splits; ++s2) {
-                        float y[EN];
-                        floats_at<EN>(a.upart + s2 * a.rows * a.ad.kmax + line, kc + c * EN, in ? run.k : 0, y);
-#pragma unroll
-                        for (int e = 0; e < EN; ++e) x[e] += y[e];
-                    }
-                    if (c0 == 0 && in)
-#pragma unroll
-                        for (int e = 0; e < EN; ++e)
-                            if (kc + c * EN + e < run.k) a.ad.u[line + kc + c * EN + e] = x[e];
-                }
-                char *at = lds + row * kStageBytes;
-                if constexpr (sizeof(E) == 2) {
-                    u32x4 h, l;
-                    cut_chunk(x, h, l);
-                    *reinterpret_cast<u32x4 *>(at + ((c ^ swz) << 4)) = h;
-                    *reinterpret_cast<u32x4 *>(at + (((c + 4) ^ swz) << 4)) = l;
-                } else {
-                    *reinterpret_cast<f32x4 *>(at + ((c ^ swz) << 4)) = f32x4{x[0], x[1], x[2], x[3]};
-                }
-            }
-            constexpr int TN = chunk_n<T>(), chunks = C::BN / TN;
-            for (int q = threadIdx.x; q < 32 * chunks; q += C::THREADS) {
-                const int k = q / chunks, c = q % chunks;
-                u32x4 v = {0, 0, 0, 0};
-                if (kc + k < run.k && c0 + c * TN < a.n) {
-                    const int64_t e = (int64_t)(run.ko + kc + k) * a.n + c0 + c * TN;
-                    v = chunk_at<T>((const char *)a.ad.up + e * (int64_t)sizeof(T), (a.ad.ktotal * a.n - e) * (int64_t)sizeof(T));
-                }
-                char *at = lq + k * (C::BN * (int)sizeof(E)) + ((c ^ rc_shift<E, C::BN>(k)) << 4);
-                if constexpr (two_piece_matrix<T>()) {
-                    float x[8];
-                    u32x4 h, l;
-                    floats_of(v, x, T{});
-                    cut_chunk(x, h, l);
-                    *reinterpret_cast<u32x4 *>(at) = h;
-                    *reinterpret_cast<u32x4 *>(at + 32 * (C::BN * (int)sizeof(E))) = l;
-                } else {
-                    *reinterpret_cast<u32x4 *>(at) = v;
-                }
-            }
-            meet();
-            constexpr int KK = 32 / (2 * EN);         // matrix steps of 32 factors
-#pragma unroll
-            for (int i = 0; i < C::TM; ++i) {
-                const int row = first + 32 * i + (lane & 31);
-                const bool in = row >= from && row < to;
-#pragma unroll
-                for (int j = 0; j < C::TN; ++j) {
-                    f32x16 d, low;                    // products of the first pieces, and of the others
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) d[v] = low[v] = 0.f;
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        const u32x4 p = rp.read(lds, i, kk), q = rq.read(lq, j, kk);
-                        if constexpr (Cut<T>::kBoth) {
-                            if constexpr (two_piece_matrix<T>()) low = Type<E>::mac(rq.read(lq, j, kk + KK), p, low);
-                            low = Type<E>::mac(q, rp.read(lds, i, kk + KK), low);
-                        }
-                        d = Type<E>::mac(q, p, d);
-                    }
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[i][j][v] += in ? both_pieces<Cut<T>::kBoth>(d[v], low[v]) : 0.f;
-                    __builtin_amdgcn_sched_barrier(0);      // one product's registers at a time
-                }
-            }
-            meet();
-        }
-    }
-}
-
 template <class T> __device__ __forceinline__ Operand operand(const void *base, int64_t entry, int64_t ld, int64_t count, int64_t last)
 {
     constexpr int E = sizeof(T);
     return Operand{(const char *)base + entry * E, ld * E, count, last * E};
+}
+
+// ---- adapters in a tile's accumulators --------------------------------------------
+// u as an operand of the matrix instructions: rows of `planes` x kp entries, kp = kmax in whole 32s, zero behind a run's
+// rank and in rows without a run.  Floats: as they are.  Halves and bf16: u = hi + lo in two planes; the products with hi and
+// with lo both run over H's rows.  A half has too small a range for u, so f16 rows are scaled by a power of two that brings
+// their largest entry to [1/2, 1), held to 2^24 at most so that sums stay in range; row_scale undoes it.
+// One row per 16 lanes; adds up the parts of u on the way.
+template <class T> __global__ __launch_bounds__(256) void pack_kernel(Product a)
+{
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int l = threadIdx.x & 15, kp = (a.ad.kmax + 31) / 32 * 32;
+    if (row >= a.rows) return;
+    Run run = {0, 0};
+    const int s = range_at(a.ad.offsets, a.ad.segments, row);
+    if (s < a.ad.segments && a.ad.offsets[s] <= row) run = run_of(a.ad, s);
+    constexpr int N = kMaxRank / 16;
+    float u[N];
+    float most = 0.f;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const int k = 16 * t + l;
+        u[t] = 0.f;
+        if (k < run.k) {
+            if (a.shrink_splits == 1) {
+                u[t] = a.ad.u[row * a.ad.kmax + k];
+            } else {
+                for (int p = 0; p < a.shrink_splits; ++p) u[t] += a.upart[(p * a.rows + row) * a.ad.kmax + k];
+                a.ad.u[row * a.ad.kmax + k] = u[t];
+            }
+        }
+        most = __builtin_fmaxf(most, __builtin_fabsf(u[t]));
+    }
+    float up = 1.f;
+    if constexpr (sizeof(T) == 2 && !std::is_same<T, bf16_t>::value) {
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+        int e = half_exponent(__float_as_uint(most)) + 1;
+        e = e < -24 ? -24 : (e > 126 ? 126 : e);
+        up = power_of_two(-e);
+        if (l == 0) a.row_scale[row] = power_of_two(e);
+    }
+    T *out = (T *)a.pack + row * ((int64_t)kp * (4 / (int)sizeof(T)));
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const int k = 16 * t + l;
+        if (k >= kp) break;
+        const float x = u[t] * up;
+        const T hi = Type<T>::round(x);
+        out[k] = hi;
+        if constexpr (sizeof(T) == 2) out[kp + k] = Type<T>::round(__builtin_isfinite(Type<T>::load(hi)) ? x - Type<T>::load(hi) : 0.f);
+    }
+}
+
+template <class T> __device__ __forceinline__ bool all_finite(u32x4 v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            bad |= (v[i] & 0x7f800000u) == 0x7f800000u;
+        } else {
+            constexpr unsigned e = std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
+            bad |= (v[i] & e) == e || (v[i] & e << 16) == e << 16;
+        }
+    }
+    return !bad;
+}
+
+// acc += u H_r by plain sums, in the rows of their segments alone: for factors H that are not finite, which would reach other
+// rows through the zeros of a matrix product, and for calls without scratch (packed false: all factors).  Slow.
+// Takes groups of `group` factors that have such an entry in the tile's columns.
+template <class C>
+__device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_t r1, int64_t c0, bool packed, int group, typename C::Acc &acc)
+{
+    using T = typename C::T;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const int64_t row0 = r0 + wave / C::WN * (C::BM / C::WM) + (lane & 31), col0 = c0 + wave % C::WN * (C::BN / C::WN);
+    for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
+        int64_t lo, hi;
+        range_of(a.ad.offsets, s, a.rows, lo, hi);
+        if (lo >= r1) break;
+        const Run run = run_of(a.ad, s);
+        if (hi <= lo || hi <= r0) continue;
+        bool use = !packed;
+        for (int k = 0; k < run.k; ++k) {
+            const T *h = (const T *)a.ad.up + (int64_t)(run.ko + k) * a.n;
+            if (packed && k % group == 0) {
+                bool bad = false;
+                for (int64_t q = threadIdx.x; q < (int64_t)group * C::BN; q += C::THREADS) {
+                    const int64_t kk = k + q / C::BN, col = c0 + q % C::BN;
+                    if (kk < run.k && col < a.n) bad |= !__builtin_isfinite(Type<T>::load(h[q / C::BN * a.n + col]));
+                }
+                use = __syncthreads_or(bad);
+            }
+            if (!use) continue;
+            float u[C::TM];
+            bool in[C::TM];
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) {
+                const int64_t row = row0 + 32 * i;
+                in[i] = row >= lo && row < hi && row < r1;
+                u[i] = in[i] ? a.ad.u[row * a.ad.kmax + k] : 0.f;
+                if constexpr (std::is_same<T, f16_t>::value)
+                    if (packed && in[i]) u[i] /= a.row_scale[row];
+            }
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int64_t col = col0 + 32 * j + acc_row(v, lane >> 5);
+                    const float x = Type<T>::load(h[col < a.n ? col : a.n - 1]);
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i) acc[i][j][v] = in[i] ? __builtin_fmaf(u[i], x, acc[i][j][v]) : acc[i][j][v];
+                }
+        }
+    }
+}
+
+// acc (cleared) += s_r x W_r H_r from the packed u, segment by segment, 64 factors at a time in two stages: the tile's
+// product with H_r, in which the rows of other segments are zeros.  H is looked at first; what has entries that are not
+// finite is left out.  (A row of u that is not finite is a row of the result.)  Returns whether something was.
+template <class C, class X>
+__device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t r1, int64_t c0, char *lds, typename C::Acc &acc)
+{
+    using T = typename C::T;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int kp = (a.ad.kmax + 31) / 32 * 32;
+    const int64_t row_n = kp * (4 / (int)sizeof(T));
+    bool left_out = false;
+    typename X::ReadP rp;
+    typename X::ReadQ rq;
+    rp.open(wave / C::WN * (C::BM / C::WM));
+    rq.open(wave % C::WN * (C::BN / C::WN));
+    for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
+        int64_t lo, hi;
+        range_of(a.ad.offsets, s, a.rows, lo, hi);
+        if (lo >= r1) break;
+        const Run run = run_of(a.ad, s);
+        if (run.k == 0 || hi <= lo || hi <= r0) continue;
+        Operand P = operand<T>(a.pack, r0 * row_n, row_n, (hi < r1 ? hi : r1) - r0, (a.rows - r0) * row_n);
+        P.first = (int)((lo > r0 ? lo : r0) - r0);
+        P.plane = kp * (int)sizeof(T);
+        const Operand Q = operand<T>(a.ad.up, (int64_t)run.ko * a.n + c0, a.n, a.n - c0, (a.ad.ktotal - run.ko) * a.n - c0);
+        typename X::LoadP lp;
+        typename X::LoadQ lq;
+        lp.open(P);
+        lq.open(Q);
+        for (int k = 0; k < run.k; k += 2 * X::SK) {
+            bool bad = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                char *stage = lds + h * X::kLdsStage;
+                lp.fetch(k + h * X::SK, run.k, stage);
+                lq.fetch(k + h * X::SK, run.k, stage + X::kLdsP);
+                if constexpr (!X::DMA) {
+                    lp.put(stage);
+                    lq.put(stage + X::kLdsP);
+                }
+            }
+            wait_loads<0>();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < X::LoadQ::kJobs; ++j)      // a thread looks at the chunks that it brought
+                    bad |= !all_finite<T>(*reinterpret_cast<const u32x4 *>(lds + h * X::kLdsStage + X::kLdsP + (threadIdx.x + j * X::THREADS) * 16));
+            bad = __syncthreads_or(bad);
+            left_out |= bad;
+            const int stages = bad ? 0 : (k + X::SK < run.k ? 2 : 1);
+            for (int h = 0; h < stages; ++h) X::step(lds + h * X::kLdsStage, rp, rq, acc, [](int) {});
+            meet();
+        }
+    }
+    return left_out;
+}
+
+// Accumulators of f16 tiles out of the rows' scales.
+template <class C> __device__ __forceinline__ void unscale(const Product &a, int64_t r0, int64_t r1, typename C::Acc &acc)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+        const int64_t row = r0 + wave / C::WN * (C::BM / C::WM) + 32 * i + (lane & 31);
+        const float up = a.row_scale[row < r1 ? row : r0];
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] *= up;
+    }
 }
 
 // u (or a part of it) for one tile of a segment's rows: s_r x W_r.
@@ -256,61 +342,93 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
     const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.m ? k0 + a.k_split : a.m;
     typename C::Acc acc;
     C::clear(acc);
+    if constexpr (ADAPTERS) {
+        using X = Tile<T, C::BM, C::BN, C::WM, C::WN, 2, false, true, C::DMA, C::SB, (sizeof(T) == 2 ? 2 : 1)>;
+        if (!a.joined) {
+            const bool packed = a.pack != nullptr;
+            if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_plainly<C>(a, f.r0, f.r1, c0, packed, 2 * X::SK, acc);
+            if constexpr (std::is_same<T, f16_t>::value)
+                if (packed) unscale<C>(a, f.r0, f.r1, acc);
+        }
+    }
     C::multiply(P, Q, k0, k1, lds, acc);
-    if (a.splits > 1) {
+    if (a.joined) {
         const int64_t n4 = up4(a.n);
         C::store(acc, a.part + ((int64_t)split * a.rows + f.r0) * n4 + c0, n4, f.r1 - f.r0, a.n - c0, true, lds);
         return;
     }
-    if constexpr (ADAPTERS) add_adapters<C>(a, f.r0, f.r1, c0, lds, acc);
     C::store(acc, (T *)a.y + f.r0 * a.ldy + c0, a.ldy, f.r1 - f.r0, a.n - c0, a.vec, lds);
 }
 
-// Y of one row and 1024 columns from the parts, in order, and its adapter.
+// Y of one row and 256 columns from the parts, and its adapter: wave w adds parts and factors w, w + 4, ..., and the four
+// sums meet in order.
 template <class T> __global__ __launch_bounds__(256) void join_product_kernel(Product a)
 {
-    const int64_t row = blockIdx.y;
-    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    const int64_t n4 = up4(a.n);
+    const int ct = (int)((a.n + 255) / 256);
+    const int64_t row = blockIdx.x / ct;
+    const int c = blockIdx.x % ct, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const int64_t col = (int64_t)c * 256 + lane * 4, n4 = up4(a.n), at = col < a.n ? col : 0;
     __shared__ float us[kMaxRank];
-    Run run = {0, 0};
-    bool in = !a.offsets;
+    __shared__ f32x4 sums[4][64];
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    {
+        f32x4 t[kMaxSplits / 4];
+#pragma unroll
+        for (int i = 0; i < kMaxSplits / 4; ++i) {
+            const int s = w + 4 * i;
+            t[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (s < a.splits) t[i] = *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)s * a.rows + row) * n4 + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kMaxSplits / 4; ++i) y += t[i];
+    }
     if (a.offsets) {
         const int g = first_range(a.offsets, a.groups, row);
-        if (g < a.groups) in = a.offsets[g] <= row;
-        if (!in) return;
+        if (g == a.groups || a.offsets[g] > row) return;
     }
     if (a.ad.segments) {
+        Run run = {0, 0};
         const int s = first_range(a.ad.offsets, a.ad.segments, row);
         if (s < a.ad.segments && a.ad.offsets[s] <= row) run = run_of(a.ad, s);
         for (int k = threadIdx.x; k < run.k; k += 256) {
-            float u;
+            float u = 0.f;
             if (a.shrink_splits > 1) {
-                u = 0.f;
-                for (int s2 = 0; s2 < a.shrink_splits; ++s2) u += a.upart[((int64_t)s2 * a.rows + row) * a.ad.kmax + k];
-                if (blockIdx.x == 0) a.ad.u[row * a.ad.kmax + k] = u;
+                float t[kMaxSplits];
+#pragma unroll
+                for (int p = 0; p < kMaxSplits; ++p) t[p] = p < a.shrink_splits ? a.upart[(p * a.rows + row) * a.ad.kmax + k] : 0.f;
+#pragma unroll
+                for (int p = 0; p < kMaxSplits; ++p) u += t[p];
+                if (c == 0) a.ad.u[row * a.ad.kmax + k] = u;
             } else {
                 u = a.ad.u[row * a.ad.kmax + k];
             }
             us[k] = u;
         }
         __syncthreads();
-    }
-    if (col >= a.n) return;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) y += *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)s * a.rows + row) * n4 + col);
-    const int have = a.n - col < 4 ? (int)(a.n - col) : 4;
-    for (int k = 0; k < run.k; ++k) {
-        const T *h = (const T *)a.ad.up + (int64_t)(run.ko + k) * a.n + col;
-        const float u = us[k];
+        const T *h = (const T *)a.ad.up + (int64_t)run.ko * a.n;
+        for (int k0 = w; k0 < run.k; k0 += 16) {
+            float x[4][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < have) y[e] = __builtin_fmaf(u, Type<T>::load(h[e]), y[e]);
+            for (int i = 0; i < 4; ++i) {
+                const int k = k0 + 4 * i < run.k ? k0 + 4 * i : run.k - 1;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][e] = Type<T>::load(h[(int64_t)k * a.n + (col + e < a.n ? col + e : a.n - 1)]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k0 + 4 * i < run.k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(us[k0 + 4 * i], x[i][e], y[e]);
+        }
     }
+    sums[w][lane] = y;
+    __syncthreads();
+    if (w || col >= a.n) return;
+    y = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
     T *out = (T *)a.y + row * a.ldy + col;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (e < have) out[e] = Type<T>::round(y[e]);
+        if (col + e < a.n) out[e] = Type<T>::round(y[e]);
 }
 
 // dB_g = X_g^T dY_g, or parts of it over the group's rows.
@@ -528,17 +646,18 @@ template <class T> hipError_t launch_product(const Product &p, hipStream_t st)
     const int64_t far = (int64_t)1 << 30;
     bool dma = by16(p.x, p.ldx * E, p.m * E) && by16(p.b, p.ldb * E, p.stride_b * E) && p.ldx * E * 256 < far && p.ldb * E * 256 < far;
     if (p.transposed == 0) dma = dma && p.n * E % 16 == 0;
-    if (p.ad.segments) dma = dma && by16(p.ad.down);
+    if (p.ad.segments) dma = dma && by16(p.ad.down) && by16(p.ad.up, p.n * E);
     using ShrinkDma = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, true>;
     using Shrink = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, false>;
     int shrink = 0;
     if (p.ad.segments) {
         const int64_t rt = (p.rows + kShrinkRows - 1) / kShrinkRows + p.ad.segments, ct = (p.ad.kmax + kShrinkCols - 1) / kShrinkCols;
         shrink = (int)(rt * ct * p.shrink_splits);
-        if (p.splits == 1) {
+        if (!p.joined) {
             if (dma) hipLaunchKernelGGL((shrink_kernel<ShrinkDma>), dim3(shrink), dim3(ShrinkDma::THREADS), 0, st, p);
             else hipLaunchKernelGGL((shrink_kernel<Shrink>), dim3(shrink), dim3(Shrink::THREADS), 0, st, p);
             shrink = 0;
+            if (p.pack) hipLaunchKernelGGL((pack_kernel<T>), dim3((unsigned)((p.rows + 15) / 16)), dim3(256), 0, st, p);
         }
     }
     if (p.transposed) {
@@ -548,8 +667,7 @@ template <class T> hipError_t launch_product(const Product &p, hipStream_t st)
         if (dma) launch_shape<T, true, true>(p, shrink, st);
         else launch_shape<T, true, false>(p, shrink, st);
     }
-    if (p.splits > 1)
-        hipLaunchKernelGGL((join_product_kernel<T>), dim3((unsigned)((p.n + 1023) / 1024), (unsigned)p.rows), dim3(256), 0, st, p);
+    if (p.joined) hipLaunchKernelGGL((join_product_kernel<T>), dim3((unsigned)((p.n + 255) / 256 * p.rows)), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
