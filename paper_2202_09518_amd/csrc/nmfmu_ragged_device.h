@@ -17,6 +17,8 @@
 #include "nmfmu_device.h"
 #include "nmfmu_ragged_internal.h"
 
+#include <type_traits>
+
 namespace nmfmu {
 namespace ragged {
 
@@ -250,6 +252,13 @@ template <class T, int R, bool RC, int SB = kStageBytes> struct Reader {
         }
         return v;
     }
+    // The same for a kk known at run time only (floats).
+    __device__ __forceinline__ u32x4 read_at(const char *lds, int t, int kk) const
+    {
+        if (RC) return read(lds + kk * 8 * R * Type<T>::kBytes, t, 0);          // eight k further; their places repeat
+        const int row = first + (lane & 31);
+        return *reinterpret_cast<const u32x4 *>(lds + (row + 32 * t) * SB + (((2 * kk + (lane >> 5)) ^ kc_shift<SB>(row)) << 4));
+    }
 };
 
 template <int N> __device__ __forceinline__ void wait_loads()      // until at most N of a wave's loads are under way
@@ -288,37 +297,56 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
     // stage.  A chunk of all lanes keeps the load unit busy for 16 cycles, so the large tile spreads them over its products,
     // one after every second (256 x 256, 8192 x 8192 x 4096, bf16: 443 us, all at the start 478; 448 after every fourth); a
     // tile with few products asks first (32 x 128 over 64 groups of 4096 x 2048: 165 us, spread 242).
-    template <class F>
+    // KK: matrix steps of the stage; LIVE: blocks of 32 rows that take part.
+    template <int KK = SB / 32, int LIVE = TM, class F>
     static __device__ __forceinline__ void step(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc, F load)
     {
-        constexpr int KK = SB / 32, L = LoadP::kJobs + LoadQ::kJobs;
-        constexpr bool spread = KK * TM * TN >= 4 * L;
+        constexpr int L = LoadP::kJobs + LoadQ::kJobs;
+        constexpr bool spread = KK * LIVE * TN >= 4 * L;
         u32x4 p[2][TM], q[2][TN];
         auto get = [&](int kk) {
 #pragma unroll
             for (int j = 0; j < TN; ++j) q[kk & 1][j] = rq.read(lds + kLdsP, j, kk);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) p[kk & 1][i] = rp.read(lds, i, kk);
+            for (int i = 0; i < LIVE; ++i) p[kk & 1][i] = rp.read(lds, i, kk);
         };
         int done = 0;
         if (!spread)
 #pragma unroll
             for (; done < L; ++done) load(done);
+        if (LIVE == 0) return;
         get(0);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             if (kk + 1 < KK) get(kk + 1);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < LIVE; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     acc[i][j] = Type<T>::mac(q[kk & 1][j], p[kk & 1][i], acc[i][j]);
-                    if (spread && ((kk * TM + i) * TN + j) % 2 == 0 && done < L) {
+                    if (spread && ((kk * LIVE + i) * TN + j) % 2 == 0 && done < L) {
                         __builtin_amdgcn_sched_barrier(0);
                         load(done++);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
+        }
+    }
+
+    // The first kks matrix steps of a stage, one by one.
+    static __device__ __forceinline__ void first_steps(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc, int kks)
+    {
+#pragma unroll 1
+        for (int kk = 0; kk < kks; ++kk) {
+            u32x4 p[TM], q[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) q[j] = rq.read_at(lds + kLdsP, j, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) p[i] = rp.read_at(lds, i, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[j], p[i], acc[i][j]);
         }
     }
 
@@ -343,17 +371,24 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 lq.fetch(k0 + (int64_t)s * SK, k1, lds + s * kLdsStage + kLdsP);
             }
             int from = 0, to = STAGES - 1;
-            for (int s = 0; s < steps; ++s) {
-                wait_loads<(STAGES - 2) * L>();
-                meet();
-                const int64_t k = k0 + (int64_t)(s + STAGES - 1) * SK;
-                step(lds + from * kLdsStage, rp, rq, acc, [&](int n) {
-                    if (n < LoadQ::kJobs) lq.fetch_job(n, k, k1, lds + to * kLdsStage + kLdsP);
-                    else lp.fetch_job(n - LoadQ::kJobs, k, k1, lds + to * kLdsStage);
-                });
-                from = from + 1 == STAGES ? 0 : from + 1;
-                to = to + 1 == STAGES ? 0 : to + 1;
-            }
+            auto run = [&](auto live) {
+                for (int s = 0; s < steps; ++s) {
+                    wait_loads<(STAGES - 2) * L>();
+                    meet();
+                    const int64_t k = k0 + (int64_t)(s + STAGES - 1) * SK;
+                    step<SB / 32, live.value>(lds + from * kLdsStage, rp, rq, acc, [&](int n) {
+                        if (n < LoadQ::kJobs) lq.fetch_job(n, k, k1, lds + to * kLdsStage + kLdsP);
+                        else lp.fetch_job(n - LoadQ::kJobs, k, k1, lds + to * kLdsStage);
+                    });
+                    from = from + 1 == STAGES ? 0 : from + 1;
+                    to = to + 1 == STAGES ? 0 : to + 1;
+                }
+            };
+            // Waves whose rows are not there leave out their products: all of them, or half.
+            const int have = (int)(P.count < BM ? P.count : BM) - wave / WN * (BM / WM);
+            if (PRC || TM < 4 || have > TM * 16) run(std::integral_constant<int, TM>{});
+            else if (have > 0) run(std::integral_constant<int, TM / 2>{});
+            else run(std::integral_constant<int, 0>{});
             wait_loads<0>();
         } else if (steps > 0) {
             lp.fetch(k0, k1, nullptr);
@@ -525,6 +560,23 @@ __device__ __forceinline__ int range_at(const int64_t *offsets, int groups, int6
     }
     return lo;
 }
+// The range with `want` longer ones (or as long and before it), where there are up to 64; else range `want`.
+__device__ __forceinline__ int nth_longest(const int64_t *offsets, int groups, int64_t rows, int want)
+{
+    if (groups > 64) return want;
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = 0;
+    if (lane < groups) range_of(offsets, lane, rows, lo, hi);
+    const int len = lane < groups ? (int)(hi - lo) : -1;
+    int longer = 0;
+    for (int i = 0; i < groups; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        longer += other > len || (other == len && i < lane);
+    }
+    const unsigned long long at = __ballot(lane < groups && longer == want);
+    return __builtin_ctzll(at);
+}
+
 // Workgroups are dealt to the eight dies in turn, each with a cache of its own: a die gets neighbouring tiles.
 __device__ __forceinline__ int by_die(int id, int total)
 {

@@ -252,7 +252,12 @@ __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t
             bad = __syncthreads_or(bad);
             left_out |= bad;
             const int stages = bad ? 0 : (k + X::SK < run.k ? 2 : 1);
-            for (int h = 0; h < stages; ++h) X::step(lds + h * X::kLdsStage, rp, rq, acc, [](int) {});
+            for (int h = 0; h < stages; ++h) {
+                const char *stage = lds + h * X::kLdsStage;
+                [[maybe_unused]] const int left = run.k - k - h * X::SK;      // steps without factors: left out where they take long
+                if constexpr (sizeof(T) == 4) X::first_steps(stage, rp, rq, acc, left > 24 ? 4 : (left + 7) / 8);
+                else X::step(stage, rp, rq, acc, [](int) {});
+            }
             meet();
         }
     }
@@ -437,11 +442,13 @@ template <class C> __global__ __launch_bounds__(C::THREADS) void gradient_kernel
     using T = typename C::T;
     __shared__ __align__(1024) char lds[C::kLds];
     const int mt = (int)((a.m + C::BM - 1) / C::BM), nt = (int)((a.n + C::BN - 1) / C::BN);
-    int id = by_die(blockIdx.x, gridDim.x);
+    // Every die has its share of each group's tiles, the longest groups first: a tile takes as long as its group.
+    const int tiles = mt * nt * a.splits, per = (tiles + 7) / 8, nth = blockIdx.x / 8;
+    int id = blockIdx.x % 8 * per + nth % per;
+    if (id >= tiles) return;
+    const int g = nth_longest(a.offsets, a.groups, a.rows, nth / per);
     const int split = id % a.splits;
     id /= a.splits;
-    const int g = id / (mt * nt);
-    id -= g * mt * nt;
     const int block = id / (4 * nt), in = id - block * 4 * nt, high = mt - 4 * block < 4 ? mt - 4 * block : 4;
     const int64_t r0 = (int64_t)(4 * block + in % high) * C::BM, c0 = (int64_t)(in / high) * C::BN;
     int64_t lo, hi;
@@ -489,8 +496,8 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     constexpr bool two = two_piece_matrix<T>(), both = Cut<T>::kBoth;
     constexpr int kP = SK * BM * (int)sizeof(E), kQ = SK * BN * (int)sizeof(E);
     constexpr int TM = BM / 32;
-    __shared__ __align__(1024) char lds[kP * (both ? 2 : 1) + kQ * (two ? 2 : 1)];
-    char *lp = lds, *lq = lds + kP * (both ? 2 : 1);
+    constexpr int kAllP = kP * (both ? 2 : 1), kStage = kAllP + kQ * (two ? 2 : 1);
+    __shared__ __align__(1024) char lds[2 * kStage];
 
     const int mt = (int)((a.m + BN - 1) / BN);
     const bool down = (int)blockIdx.x < mt;                // dW: from v and X; dH: from u and dY
@@ -521,79 +528,104 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 
     constexpr int EN = chunk_n<E>(), TE = chunk_n<T>();
     constexpr int pc = BM / EN, PJ = SK * pc / 256, qc = BN / TE, QJ = SK * qc / 256;
-    int turn = 0;
-    for (int base = 0; base < a.ad.segments; base += 64) {
-        int64_t lo = 0, hi = 0;
-        bool is = false;
-        if (base + lane < a.ad.segments) {
-            range_of(a.ad.offsets, base + lane, a.rows, lo, hi);
-            is = a.ad.run[base + lane] == id && hi > lo;
+
+    // The run's rows in blocks of SK within its segments; every a.splits-th is this workgroup's.
+    int base = -64, turn = -1;
+    unsigned long long todo = 0;
+    int64_t lo = 0, hi = 0, r = 0, shi = 0;
+    auto advance = [&]() {
+        for (;;) {
+            r += SK;
+            while (r >= shi) {
+                while (!todo) {
+                    base += 64;
+                    if (base >= a.ad.segments) return false;
+                    lo = hi = 0;
+                    bool is = false;
+                    if (base + lane < a.ad.segments) {
+                        range_of(a.ad.offsets, base + lane, a.rows, lo, hi);
+                        is = a.ad.run[base + lane] == id && hi > lo;
+                    }
+                    todo = __ballot(is);
+                }
+                const int l = __builtin_ctzll(todo);
+                todo &= todo - 1;
+                r = Ranges::lane_value(lo, l);
+                shi = Ranges::lane_value(hi, l);
+            }
+            if (++turn % a.splits == split) return true;
         }
-        unsigned long long todo = __ballot(is);
-        while (todo) {
-            const int l = __ffsll(todo) - 1;
-            todo &= todo - 1;
-            const int64_t slo = __shfl(lo, l), shi = __shfl(hi, l);
-            for (int64_t r = slo; r < shi; r += SK) {
-                if (turn++ % a.splits != split) continue;
-                const int64_t left = shi - r;
-                u32x4 ph[PJ], pl[PJ], qv[QJ];
+    };
+    u32x4 ph[PJ], pl[PJ], qv[QJ];
+    auto get = [&]() {
+        const int64_t left = shi - r;
 #pragma unroll
-                for (int j = 0; j < PJ; ++j) {
-                    const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
-                    float x[EN];
-                    floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, x);
-                    if constexpr (both) cut_chunk(x, ph[j], pl[j]);
-                    else ph[j] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
-                }
-#pragma unroll
-                for (int j = 0; j < QJ; ++j) {
-                    const int q = threadIdx.x + 256 * j, kr = q / qc, c = q % qc;
-                    qv[j] = u32x4{0, 0, 0, 0};
-                    if (kr < left && c0 + c * TE < width) {
-                        const int64_t e = (r + kr) * ld + c0 + c * TE;
-                        qv[j] = chunk_at<T>(src + e * (int64_t)sizeof(T), ((a.rows - 1) * ld + width - e) * (int64_t)sizeof(T));
-                    }
-                }
-                meet();                 // the last stage has been read
-#pragma unroll
-                for (int j = 0; j < PJ; ++j) {
-                    const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
-                    char *at = lp + kr * (BM * (int)sizeof(E)) + ((c ^ rc_shift<E, BM>(kr)) << 4);
-                    *reinterpret_cast<u32x4 *>(at) = ph[j];
-                    if constexpr (both) *reinterpret_cast<u32x4 *>(at + kP) = pl[j];
-                }
-#pragma unroll
-                for (int j = 0; j < QJ; ++j) {
-                    const int q = threadIdx.x + 256 * j, kr = q / qc, c = q % qc;
-                    char *at = lq + kr * (BN * (int)sizeof(E)) + ((c ^ rc_shift<E, BN>(kr)) << 4);
-                    if constexpr (two) {
-                        float x[8];
-                        u32x4 h, w;
-                        floats_of(qv[j], x, T{});
-                        cut_chunk(x, h, w);
-                        *reinterpret_cast<u32x4 *>(at) = h;
-                        *reinterpret_cast<u32x4 *>(at + kQ) = w;
-                    } else {
-                        *reinterpret_cast<u32x4 *>(at) = qv[j];
-                    }
-                }
-                meet();
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    const u32x4 q = rq.read(lq, 0, kk);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) {
-                        const u32x4 p = rp.read(lp, i, kk);
-                        if constexpr (both) {
-                            if constexpr (two) low[i] = Type<E>::mac(rq.read(lq + kQ, 0, kk), p, low[i]);
-                            low[i] = Type<E>::mac(q, rp.read(lp + kP, i, kk), low[i]);
-                        }
-                        acc[i] = Type<E>::mac(q, p, acc[i]);
-                    }
-                }
+        for (int j = 0; j < QJ; ++j) {
+            const int q = threadIdx.x + 256 * j, kr = q / qc, c = q % qc;
+            qv[j] = u32x4{0, 0, 0, 0};
+            if (kr < left && c0 + c * TE < width) {
+                const int64_t e = (r + kr) * ld + c0 + c * TE;
+                qv[j] = chunk_at<T>(src + e * (int64_t)sizeof(T), ((a.rows - 1) * ld + width - e) * (int64_t)sizeof(T));
             }
         }
+#pragma unroll
+        for (int j = 0; j < PJ; ++j) {
+            const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
+            float x[EN];
+            floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, x);
+            if constexpr (both) cut_chunk(x, ph[j], pl[j]);
+            else ph[j] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
+        }
+    };
+    auto put = [&](char *to) {
+#pragma unroll
+        for (int j = 0; j < PJ; ++j) {
+            const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
+            char *at = to + kr * (BM * (int)sizeof(E)) + ((c ^ rc_shift<E, BM>(kr)) << 4);
+            *reinterpret_cast<u32x4 *>(at) = ph[j];
+            if constexpr (both) *reinterpret_cast<u32x4 *>(at + kP) = pl[j];
+        }
+#pragma unroll
+        for (int j = 0; j < QJ; ++j) {
+            const int q = threadIdx.x + 256 * j, kr = q / qc, c = q % qc;
+            char *at = to + kAllP + kr * (BN * (int)sizeof(E)) + ((c ^ rc_shift<E, BN>(kr)) << 4);
+            if constexpr (two) {
+                float x[8];
+                u32x4 h, w;
+                floats_of(qv[j], x, T{});
+                cut_chunk(x, h, w);
+                *reinterpret_cast<u32x4 *>(at) = h;
+                *reinterpret_cast<u32x4 *>(at + kQ) = w;
+            } else {
+                *reinterpret_cast<u32x4 *>(at) = qv[j];
+            }
+        }
+    };
+    // the next block is on its way while one is multiplied
+    bool more = advance();
+    if (more) {
+        get();
+        put(lds);
+    }
+    for (int n = 0; more; ++n) {
+        meet();
+        more = advance();
+        if (more) get();
+        const char *lp = lds + (n & 1) * kStage, *lq = lp + kAllP;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const u32x4 q = rq.read(lq, 0, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const u32x4 p = rp.read(lp, i, kk);
+                if constexpr (both) {
+                    if constexpr (two) low[i] = Type<E>::mac(rq.read(lq + kQ, 0, kk), p, low[i]);
+                    low[i] = Type<E>::mac(q, rp.read(lp + kP, i, kk), low[i]);
+                }
+                acc[i] = Type<E>::mac(q, p, acc[i]);
+            }
+        }
+        if (more) put(lds + ((n + 1) & 1) * kStage);
     }
     const int64_t m4 = up4(a.m), n4 = up4(a.n);
 #pragma unroll
@@ -686,7 +718,7 @@ template <class T> hipError_t launch_gradient(const Gradient &p, hipStream_t st)
     const bool dma = by16(p.x, p.ldx * E, p.m * E) && by16(p.dy, p.ldy * E, p.n * E) && p.ldx * E * 64 < far && p.ldy * E * 64 < far;
     auto go = [&](auto tile) {
         using C = decltype(tile);
-        const int64_t tiles = (p.m + C::BM - 1) / C::BM * ((p.n + C::BN - 1) / C::BN) * p.groups * p.splits;
+        const int64_t tiles = ((p.m + C::BM - 1) / C::BM * ((p.n + C::BN - 1) / C::BN) * p.splits + 7) / 8 * 8 * p.groups;
         hipLaunchKernelGGL((gradient_kernel<C>), dim3((unsigned)tiles), dim3(C::THREADS), 0, st, p);
     };
     if (p.shape == 0) {
