@@ -6,12 +6,13 @@
 //   RC: [k][chunks of columns], chunk c at place c ^ f(k).
 // Both permutations keep the matrix instructions' reads free of bank conflicts: 16 lanes that a 16-byte read serves at
 // once cover 16 rows, two rows fill the 256 bytes of all banks, so a place changes with every second row; the transposing
-// 8-byte reads of an RC half operand serve 32 lanes on 4 values of k x 64 bytes, which f spreads over the banks; single
-// floats of an RC operand are read on two k four apart, 128 bytes of each.
+// 8-byte reads of an RC half operand serve 32 lanes on 8 values of k x 32 bytes, which f spreads over the banks; single
+// floats of an RC operand are read on four k four apart, 64 bytes of each.
 //
-// Matrix instructions: v_mfma_f32_32x32x16 on halves, v_mfma_f32_32x32x2_f32 on floats (its k are taken in the order that
-// a 16-byte read of a KC operand delivers them, on both operands alike).  Q is the first operand, so a lane ends with four
-// neighbouring columns of one row in its accumulators, which it stores together.
+// Matrix instructions: v_mfma_f32_16x16x32 on halves, v_mfma_f32_16x16x4_f32 on floats (its k are taken in the order that
+// a 16-byte read of a KC operand delivers them, on both operands alike).  On normal random bf16 the 16 x 16 form holds
+// 2040 TFLOP/s in registers where the 32 x 32 form holds 1830: it moves half as much of the accumulators.  Q is the
+// first operand, so a lane ends with four neighbouring columns of one row in its accumulators, which it stores together.
 #pragma once
 
 #include "nmfmu_device.h"
@@ -27,7 +28,10 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 template <class T> struct Type;
 template <> struct Type<bf16_t> {
     static constexpr int kBytes = 2;
-    static __device__ __forceinline__ f32x16 mac(u32x4 q, u32x4 p, f32x16 c) { return mfma_bf16(q, p, c); }
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float load(bf16_t x) { return __uint_as_float((unsigned)x.bits << 16); }
     static __device__ __forceinline__ bf16_t round(float x)
     {
@@ -37,7 +41,10 @@ template <> struct Type<bf16_t> {
 };
 template <> struct Type<f16_t> {
     static constexpr int kBytes = 2;
-    static __device__ __forceinline__ f32x16 mac(u32x4 q, u32x4 p, f32x16 c) { return mfma_f16(q, p, c); }
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, q), __builtin_bit_cast(f16x8, p), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float load(f16_t x) { return (float)__builtin_bit_cast(_Float16, x.bits); }
     static __device__ __forceinline__ f16_t round(float x)
     {
@@ -50,10 +57,10 @@ template <> struct Type<f16_t> {
 };
 template <> struct Type<float> {
     static constexpr int kBytes = 4;
-    static __device__ __forceinline__ f32x16 mac(u32x4 q, u32x4 p, f32x16 c)
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c = mfma32(__uint_as_float(q[j]), __uint_as_float(p[j]), c);
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[j]), __uint_as_float(p[j]), c, 0, 0, 0);
         return c;
     }
     static __device__ __forceinline__ float load(float x) { return x; }
@@ -73,10 +80,9 @@ template <class T> constexpr int chunk_n() { return 16 / Type<T>::kBytes; }
 template <class T, int R> __device__ __forceinline__ int rc_shift(int k)
 {
     constexpr int pitch = R * Type<T>::kBytes;                // bytes of a row
-    if (Type<T>::kBytes == 4) return pitch >= 256 ? ((k >> 2) & 1) * 8 : 0;
-    if (pitch >= 256) return (k & 3) * 4;
-    if (pitch == 128) return ((k >> 1) & 1) * 4;
-    return 0;
+    if (Type<T>::kBytes == 4) return pitch >= 256 ? ((k >> 2) & 1) * 4 : 0;
+    constexpr int b = pitch >= 256 ? 0 : (pitch == 128 ? 1 : 2);      // bits of k that choose a part of the 256 bytes
+    return 2 * (((k & 3) >> b) | ((k >> 3) & 1) << (2 - b));
 }
 
 // The same for row `row` of a KC operand.
@@ -135,31 +141,35 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
     static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : SB / 16;
     static constexpr int kRowStep = THREADS / kRowChunks;            // rows from job to job
     static_assert(R * (SB / 16) % THREADS == 0 && THREADS % kRowChunks == 0, "whole jobs");
-    static_assert(RC ? kRowStep % (Type<T>::kBytes == 4 ? 8 : 4) == 0 : kRowStep % 16 == 0, "places repeat from job to job");
+    static_assert(RC || kRowStep % 16 == 0, "places repeat from job to job");
 
     const char *base;
     int64_t ld, bytes;
-    int line, chunk;           // LDS line (row or k) and chunk of job 0
+    int line, place;           // LDS line (row or k) of job 0, and place of its chunks
     int first, count;
     int64_t plane;
     unsigned off[kJobs];
     u32x4 reg[DMA ? 1 : kJobs];
 
+    __device__ __forceinline__ int chunk(int j) const
+    {
+        return RC ? place ^ rc_shift<T, R>(line + j * kRowStep) : place ^ kc_shift<SB>(line);
+    }
     // k of job j within its plane's part of a stage, and where its chunk lies from the stage's first k on.
     __device__ __forceinline__ int k_of(int j) const
     {
-        return RC ? (line + j * kRowStep) % (stage_k<T, SB>() / PLANES) : chunk % (SB / 16 / PLANES) * chunk_n<T>();
+        return RC ? (line + j * kRowStep) % (stage_k<T, SB>() / PLANES) : chunk(j) % (SB / 16 / PLANES) * chunk_n<T>();
     }
     __device__ __forceinline__ int64_t where(int j) const
     {
         const int row = line + j * kRowStep;
-        if (RC) return k_of(j) * ld + chunk * 16 + (PLANES == 2 && row >= stage_k<T, SB>() / 2 ? plane : 0);
-        return (int64_t)row * ld + k_of(j) * Type<T>::kBytes + (PLANES == 2 && chunk >= SB / 32 ? plane : 0);
+        if (RC) return k_of(j) * ld + chunk(j) * 16 + (PLANES == 2 && row >= stage_k<T, SB>() / 2 ? plane : 0);
+        return (int64_t)row * ld + k_of(j) * Type<T>::kBytes + (PLANES == 2 && chunk(j) >= SB / 32 ? plane : 0);
     }
     __device__ __forceinline__ bool there(int j) const
     {
         const int row = line + j * kRowStep;
-        return RC ? chunk * chunk_n<T>() < count : row >= first && row < count;
+        return RC ? chunk(j) * chunk_n<T>() < count : row >= first && row < count;
     }
     __device__ __forceinline__ void open(const Operand &o)
     {
@@ -171,8 +181,7 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
         count = (int)(o.count < 0 ? 0 : (o.count > R ? R : o.count));
         const int tid = threadIdx.x;
         line = tid / kRowChunks;
-        const int place = tid % kRowChunks;
-        chunk = RC ? place ^ rc_shift<T, R>(line) : place ^ kc_shift<SB>(line);
+        place = tid % kRowChunks;
         if (DMA)
 #pragma unroll
             for (int j = 0; j < kJobs; ++j) off[j] = there(j) ? (unsigned)where(j) : kOutside;
@@ -183,18 +192,21 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
         const int64_t left = K - k0;
         const char *at = base + (RC ? k0 * ld : k0 * Type<T>::kBytes);
         if (DMA) {
-            const __amdgpu_buffer_rsrc_t r =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, 0x7fffffff, kBufferFlags);
+            // Written out, as the builtin makes the compiler wait for all loads before the next transposing read of LDS; the
+            // load has no destination register, and wait_loads orders what it brings.
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-            typedef __attribute__((address_space(3))) void lds_void;
+            typedef __attribute__((address_space(3))) char lds_char;
+            const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)(lds + j * THREADS * 16)) + wave * 1024;
+            const u32x4 r = {(unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)at),
+                             (unsigned)__builtin_amdgcn_readfirstlane((int)((uintptr_t)at >> 32)) & 0xffffu, 0x7fffffffu, (unsigned)kBufferFlags};
             unsigned o = off[j];
             if (left < stage_k<T, SB>() / PLANES && k_of(j) >= left) o = kOutside;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + j * THREADS * 16 + wave * 1024), 16, o, 0, 0, 0);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(r) : "memory", "m0");
         } else {
             u32x4 v = {0, 0, 0, 0};
             if (there(j) && k_of(j) < left) {
                 v = chunk_at<T>(at + where(j), bytes - (at - base) - where(j));
-                v = keep_first<T>(v, RC ? count - chunk * chunk_n<T>() : left - k_of(j));
+                v = keep_first<T>(v, RC ? count - chunk(j) * chunk_n<T>() : left - k_of(j));
             }
             reg[j] = v;
         }
@@ -211,9 +223,9 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
     }
 };
 
-// Reads operands of the matrix instruction from a stage: block of 32 rows or columns at 32 * t + first, step kk of 4.
-template <class T, int R, bool RC, int SB = kStageBytes> struct Reader {
-    int at[SB / 32];        // KC: by kk; RC: unused
+// Reads operands of the matrix instruction from a stage: block of 16 rows or columns at first + t * STEP, matrix step kk.
+template <class T, int R, bool RC, int STEP, int SB = kStageBytes> struct Reader {
+    int at[SB / 64];        // KC: by kk; RC: unused
     int lane, first;
 
     __device__ __forceinline__ void open(int first_)
@@ -221,43 +233,39 @@ template <class T, int R, bool RC, int SB = kStageBytes> struct Reader {
         lane = threadIdx.x & 63;
         first = first_;
         if (!RC) {
-            const int row = first + (lane & 31);
 #pragma unroll
-            for (int kk = 0; kk < SB / 32; ++kk) at[kk] = row * SB + (((2 * kk + (lane >> 5)) ^ kc_shift<SB>(row)) << 4);
+            for (int kk = 0; kk < SB / 64; ++kk) at[kk] = kc_at(kk);
         }
+    }
+    __device__ __forceinline__ int kc_at(int kk) const
+    {
+        const int row = first + (lane & 15);
+        return row * SB + (((4 * kk + (lane >> 4)) ^ kc_shift<SB>(row)) << 4);
     }
     __device__ __forceinline__ u32x4 read(const char *lds, int t, int kk) const
     {
-        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * 32 * SB);
+        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * STEP * SB);
         constexpr int pitch = R * Type<T>::kBytes;
         u32x4 v;
         if (Type<T>::kBytes == 2) {
             // 16 lanes read 4 values of k x 16 columns, and each leaves with the 4 k of one column
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const int i = lane & 15, k = 8 * (lane >> 5) + (i >> 2);
-            const int col = first + 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-            const char *p = lds + (16 * kk + k) * pitch + (((col >> 3) ^ rc_shift<T, R>(k)) << 4) + (col & 7) * 2;
+            const int i = lane & 15, k = 8 * (lane >> 4) + (i >> 2);
+            const int col = first + t * STEP + 4 * (i & 3);
+            const char *p = lds + (32 * kk + k) * pitch + (((col >> 3) ^ rc_shift<T, R>(k)) << 4) + (col & 7) * 2;
             const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-            const char *p4 = lds + (16 * kk + k + 4) * pitch + (((col >> 3) ^ rc_shift<T, R>(k + 4)) << 4) + (col & 7) * 2;
-            const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p4));
+            const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * pitch)));
             v = u32x4{a[0], a[1], b[0], b[1]};
         } else {
-            const int col = first + 32 * t + (lane & 31);
+            const int col = first + t * STEP + (lane & 15);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int k = 8 * kk + 4 * (lane >> 5) + j;
+                const int k = 16 * kk + 4 * (lane >> 4) + j;
                 v[j] = *reinterpret_cast<const unsigned *>(lds + k * pitch + (((col >> 2) ^ rc_shift<T, R>(k)) << 4) + (col & 3) * 4);
             }
         }
         return v;
-    }
-    // The same for a kk known at run time only (floats).
-    __device__ __forceinline__ u32x4 read_at(const char *lds, int t, int kk) const
-    {
-        if (RC) return read(lds + kk * 8 * R * Type<T>::kBytes, t, 0);          // eight k further; their places repeat
-        const int row = first + (lane & 31);
-        return *reinterpret_cast<const u32x4 *>(lds + (row + 32 * t) * SB + (((2 * kk + (lane >> 5)) ^ kc_shift<SB>(row)) << 4));
     }
 };
 
@@ -273,97 +281,150 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
     using T = T_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = DMA_ ? STAGES_ : 2, THREADS = 64 * WM * WN;
     static constexpr bool PRC = PRC_, QRC = QRC_, DMA = DMA_;
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;      // 32 x 32 tiles of a wave
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;      // 16 x 16 blocks of a wave: every WM-th of the rows, neighbouring columns
+    static constexpr int KK = SB_ / 64;                             // matrix steps of a stage
     static constexpr int SB = SB_, PLANES = PLANES_, SK = stage_k<T, SB>() / PLANES;      // bytes of k in a stage; its k
     static constexpr int kLdsP = BM * SB, kLdsQ = BN * SB, kLdsStage = kLdsP + kLdsQ;
     static constexpr int kLds = STAGES * kLdsStage;
-    using Acc = f32x16[TM][TN];
+    using Acc = f32x4[TM][TN];
     using LoadP = Loader<T, BM, PRC, THREADS, DMA, SB, PLANES>;
     using LoadQ = Loader<T, BN, QRC, THREADS, DMA, SB, PLANES>;
-    using ReadP = Reader<T, BM, PRC, SB>;
-    using ReadQ = Reader<T, BN, QRC, SB>;
+    using ReadP = Reader<T, BM, PRC, 16 * WM, SB>;
+    using ReadQ = Reader<T, BN, QRC, 16, SB>;
 
     static __device__ __forceinline__ void clear(Acc &acc)
     {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+            for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    // First row and column of a wave; row and column of a lane's first entry in block (i, j), which has four columns.
+    static __device__ __forceinline__ int wave_row() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / WN * 16; }
+    static __device__ __forceinline__ int wave_col() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % WN * (BN / WN); }
+    static __device__ __forceinline__ int row_of(int i) { return wave_row() + 16 * WM * i + (threadIdx.x & 15); }
+    static __device__ __forceinline__ int col_of(int j) { return wave_col() + 16 * j + 4 * (threadIdx.x >> 4 & 3); }
 
     // One stage.  The operands of a matrix step are read while the one before runs; load(n) asks for chunk n of the next
-    // stage.  A chunk of all lanes keeps the load unit busy for 16 cycles, so the large tile spreads them over its products,
-    // one after every second (256 x 256, 8192 x 8192 x 4096, bf16: 443 us, all at the start 478; 448 after every fourth); a
-    // tile with few products asks first (32 x 128 over 64 groups of 4096 x 2048: 165 us, spread 242).
-    // KK: matrix steps of the stage; LIVE: blocks of 32 rows that take part.
-    template <int KK = SB / 32, int LIVE = TM, class F>
+    // stage, first of all (32 x 128 over 64 groups of 4096 x 2048: 165 us; spread over the products 242).
+    template <class F>
     static __device__ __forceinline__ void step(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc, F load)
     {
         constexpr int L = LoadP::kJobs + LoadQ::kJobs;
-        constexpr bool spread = KK * LIVE * TN >= 4 * L;
-        u32x4 p[2][TM], q[2][TN];
+#pragma unroll
+        for (int n = 0; n < L; ++n) load(n);
+        constexpr int D = TM * TN < 32 ? 2 : 1;      // the large tile's registers hold one step's operands
+        u32x4 p[D][TM], q[D][TN];
         auto get = [&](int kk) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) q[kk & 1][j] = rq.read(lds + kLdsP, j, kk);
+            for (int j = 0; j < TN; ++j) q[kk % D][j] = rq.read(lds + kLdsP, j, kk);
 #pragma unroll
-            for (int i = 0; i < LIVE; ++i) p[kk & 1][i] = rp.read(lds, i, kk);
+            for (int i = 0; i < TM; ++i) p[kk % D][i] = rp.read(lds, i, kk);
         };
-        int done = 0;
-        if (!spread)
-#pragma unroll
-            for (; done < L; ++done) load(done);
-        if (LIVE == 0) return;
         get(0);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            if (kk + 1 < KK) get(kk + 1);
-#pragma unroll
-            for (int i = 0; i < LIVE; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    acc[i][j] = Type<T>::mac(q[kk & 1][j], p[kk & 1][i], acc[i][j]);
-                    if (spread && ((kk * LIVE + i) * TN + j) % 2 == 0 && done < L) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        load(done++);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
-        }
-    }
-
-    // The first kks matrix steps of a stage, one by one.
-    static __device__ __forceinline__ void first_steps(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc, int kks)
-    {
-#pragma unroll 1
-        for (int kk = 0; kk < kks; ++kk) {
-            u32x4 p[TM], q[TN];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) q[j] = rq.read_at(lds + kLdsP, j, kk);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) p[i] = rp.read_at(lds, i, kk);
+            if (D == 1 && kk) {
+                __builtin_amdgcn_sched_barrier(0);
+                get(kk);
+            } else if (D == 2 && kk + 1 < KK) {
+                get(kk + 1);
+            }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[j], p[i], acc[i][j]);
+                for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[kk % D][j], p[kk % D][i], acc[i][j]);
         }
+    }
+
+    // Stages of the large tile, two matrix steps each.  While the first step's products run, the second's operands are read;
+    // then the stage's buffer is free, and the next stage has arrived.  While the second step's run, the next stage's first
+    // operands are read, and the buffer is loaded again for the stage after it.  Reads and loads are dealt out between the
+    // products: a load of all lanes keeps its unit busy for 16 cycles, and products wait behind what is issued before them.
+    static constexpr bool kAhead = DMA && STAGES == 2 && TM * TN >= 32;
+    static __device__ __forceinline__ void ahead(LoadP &lp, LoadQ &lq, const ReadP &rp, const ReadQ &rq, int64_t k0, int64_t k1, int steps, int64_t rows,
+                                                 char *lds, Acc &acc)
+    {
+        static_assert(KK == 2, "two matrix steps");
+        constexpr int L = LoadP::kJobs + LoadQ::kJobs;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            lp.fetch(k0 + s * SK, k1, lds + s * kLdsStage);
+            lq.fetch(k0 + s * SK, k1, lds + s * kLdsStage + kLdsP);
+        }
+        wait_loads<L>();
+        meet();
+        auto run = [&](auto live) {
+            constexpr int LIVE = live.value, N = LIVE * TN, R = LIVE + TN;
+            u32x4 p[2][TM], q[2][TN];
+            auto get = [&](int n, int kk, const char *stage) {      // operand n of a step
+                if (n < TN) q[kk][n] = rq.read(stage + kLdsP, n, kk);
+                else p[kk][n - TN] = rp.read(stage, n - TN, kk);
+            };
+            // products of step kk, and `jobs` jobs between them
+            auto products = [&](int kk, int jobs, auto job) {
+                int done = 0;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    acc[n / TN][n % TN] = Type<T>::mac(q[kk][n % TN], p[kk][n / TN], acc[n / TN][n % TN]);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (; done < jobs && done * (N - 4) <= n * jobs; ++done) job(done);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+#pragma unroll
+            for (int n = 0; n < R; ++n) get(n, 0, lds);
+            for (int s = 0; s < steps; ++s) {
+                char *now = lds + (s & 1) * kLdsStage, *next = lds + (~s & 1) * kLdsStage;
+                const int64_t k = k0 + (int64_t)(s + 2) * SK;
+                products(0, R, [&](int n) { get(n, 1, now); });
+                wait_loads<0>();
+                meet();
+                __builtin_amdgcn_sched_barrier(0);
+                products(1, R + L, [&](int n) {
+                    // loads and reads in turn while there are both
+                    const int r = n < 2 * (R < L ? R : L) ? (n & 1 ? n / 2 : -1 - n / 2) : (R > L ? n - L : -1 - (n - R));
+                    if (r >= 0) get(r, 0, next);
+                    else if (-1 - r < LoadQ::kJobs) lq.fetch_job(-1 - r, k, k1, now + kLdsP);
+                    else lp.fetch_job(-1 - r - LoadQ::kJobs, k, k1, now);
+                });
+            }
+        };
+        if (PRC || rows > BM / 2) run(std::integral_constant<int, TM>{});
+        else run(std::integral_constant<int, TM / 2>{});      // the waves' rows lie in turn: half of each one's
+        wait_loads<0>();
+    }
+
+    // The first matrix step of a stage alone.
+    static __device__ __forceinline__ void first_step(const char *lds, const ReadP &rp, const ReadQ &rq, Acc &acc)
+    {
+        u32x4 p[TM], q[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) q[j] = rq.read(lds + kLdsP, j, 0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) p[i] = rp.read(lds, i, 0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[j], p[i], acc[i][j]);
     }
 
     // acc += the product over k in [k0, k1) of K.  Leaves LDS free for other use.
     static __device__ __forceinline__ void multiply(const Operand &P, const Operand &Q, int64_t k0, int64_t k1, char *lds, Acc &acc)
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         LoadP lp;
         LoadQ lq;
         lp.open(P);
         lq.open(Q);
         ReadP rp;
         ReadQ rq;
-        rp.open(wave / WN * (BM / WM));
-        rq.open(wave % WN * (BN / WN));
+        rp.open(wave_row());
+        rq.open(wave_col());
         const int steps = (int)((k1 - k0 + SK - 1) / SK);
-        if (DMA) {
+        if constexpr (kAhead) {
+            ahead(lp, lq, rp, rq, k0, k1, steps, P.count, lds, acc);
+        } else if (DMA) {
             constexpr int L = LoadP::kJobs + LoadQ::kJobs;
 #pragma unroll
             for (int s = 0; s < STAGES - 1; ++s) {
@@ -371,24 +432,17 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 lq.fetch(k0 + (int64_t)s * SK, k1, lds + s * kLdsStage + kLdsP);
             }
             int from = 0, to = STAGES - 1;
-            auto run = [&](auto live) {
-                for (int s = 0; s < steps; ++s) {
-                    wait_loads<(STAGES - 2) * L>();
-                    meet();
-                    const int64_t k = k0 + (int64_t)(s + STAGES - 1) * SK;
-                    step<SB / 32, live.value>(lds + from * kLdsStage, rp, rq, acc, [&](int n) {
-                        if (n < LoadQ::kJobs) lq.fetch_job(n, k, k1, lds + to * kLdsStage + kLdsP);
-                        else lp.fetch_job(n - LoadQ::kJobs, k, k1, lds + to * kLdsStage);
-                    });
-                    from = from + 1 == STAGES ? 0 : from + 1;
-                    to = to + 1 == STAGES ? 0 : to + 1;
-                }
-            };
-            // Waves whose rows are not there leave out their products: all of them, or half.
-            const int have = (int)(P.count < BM ? P.count : BM) - wave / WN * (BM / WM);
-            if (PRC || TM < 4 || have > TM * 16) run(std::integral_constant<int, TM>{});
-            else if (have > 0) run(std::integral_constant<int, TM / 2>{});
-            else run(std::integral_constant<int, 0>{});
+            for (int s = 0; s < steps; ++s) {
+                wait_loads<(STAGES - 2) * L>();
+                meet();
+                const int64_t k = k0 + (int64_t)(s + STAGES - 1) * SK;
+                step(lds + from * kLdsStage, rp, rq, acc, [&](int n) {
+                    if (n < LoadQ::kJobs) lq.fetch_job(n, k, k1, lds + to * kLdsStage + kLdsP);
+                    else lp.fetch_job(n - LoadQ::kJobs, k, k1, lds + to * kLdsStage);
+                });
+                from = from + 1 == STAGES ? 0 : from + 1;
+                to = to + 1 == STAGES ? 0 : to + 1;
+            }
             wait_loads<0>();
         } else if (steps > 0) {
             lp.fetch(k0, k1, nullptr);
@@ -413,40 +467,40 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
     }
 
     // Entries (row, column) of the tile inside rows x cols to out (ld entries from row to row).  A lane's accumulators are
-    // four columns at a time of one row; through LDS, 32 rows of a wave at a time, whole lines leave together.
+    // four columns at a time of one row; through LDS, two blocks' rows of a wave at a time, whole lines leave together.
     // vec: rows of out begin on 16-byte borders.  lds: as much as multiply had, free.
     template <class O>
     static __device__ __forceinline__ void store(const Acc &acc, O *out, int64_t ld, int64_t rows, int64_t cols, bool vec, char *lds,
                                                  float scale = 1.f)
     {
-        constexpr int W = TN * 32, N = 16 / (int)sizeof(O), kPitch = W * (int)sizeof(O) + 16, kLanes = W / N, kAtOnce = 64 / kLanes;
-        static_assert(32 * kPitch * WM * WN <= kLds, "the waves' rows fit");
+        constexpr int B = TM < 2 ? 1 : 2, H = 16 * B;           // blocks and rows at once
+        constexpr int W = TN * 16, N = 16 / (int)sizeof(O), kPitch = W * (int)sizeof(O) + 16, kLanes = W / N, kAtOnce = 64 / kLanes;
+        static_assert(H * kPitch * WM * WN <= kLds && H % kAtOnce == 0, "the waves' rows fit");
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-        char *mine = lds + wave * (32 * kPitch);
-        const int first = wave / WN * (BM / WM), col = wave % WN * (BN / WN) + lane % kLanes * N, up = lane / kLanes;
+        char *mine = lds + wave * (H * kPitch);
+        const int first = wave_row(), col = wave_col() + lane % kLanes * N, up = lane / kLanes;
         const int have = cols - col < N ? (int)(cols - col) : N;
-        O *at = out + (int64_t)(first + up) * ld + col;
-        const int64_t step = ld * kAtOnce;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            if (first + 32 * i >= rows) break;
+        for (int i = 0; i < TM; i += B) {
+            if (first + 16 * WM * i >= rows) break;
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const f32x4 x = {acc[i][j][4 * v] * scale, acc[i][j][4 * v + 1] * scale, acc[i][j][4 * v + 2] * scale,
-                                     acc[i][j][4 * v + 3] * scale};
-                    char *to = mine + (lane & 31) * kPitch + (32 * j + 8 * v + 4 * (lane >> 5)) * (int)sizeof(O);
+                for (int j = 0; j < TN; ++j) {
+                    const f32x4 x = acc[i + b][j] * scale;
+                    char *to = mine + (16 * b + (lane & 15)) * kPitch + (16 * j + 4 * (lane >> 4)) * (int)sizeof(O);
                     if constexpr (sizeof(O) == 4) *reinterpret_cast<f32x4 *>(to) = x;
                     else *reinterpret_cast<u32x2 *>(to) = u32x2{Type<O>::round2(x[0], x[1]), Type<O>::round2(x[2], x[3])};
                 }
-            u32x4 w[32 / kAtOnce];
+            u32x4 w[H / kAtOnce];
 #pragma unroll
-            for (int r = 0; r < 32 / kAtOnce; ++r)
+            for (int r = 0; r < H / kAtOnce; ++r)
                 w[r] = *reinterpret_cast<const u32x4 *>(mine + (up + r * kAtOnce) * kPitch + lane % kLanes * 16);
 #pragma unroll
-            for (int r = 0; r < 32 / kAtOnce; ++r, at += step) {
-                if (first + 32 * i + up + r * kAtOnce >= rows) continue;
+            for (int r = 0; r < H / kAtOnce; ++r) {
+                const int in = up + r * kAtOnce, row = first + 16 * WM * (i + in / 16) + in % 16;
+                if (row >= rows) continue;
+                O *at = out + (int64_t)row * ld + col;
                 if (vec && have == N) {
                     *reinterpret_cast<u32x4 *>(at) = w[r];
                 } else {

@@ -159,8 +159,6 @@ template <class C>
 __device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_t r1, int64_t c0, bool packed, int group, typename C::Acc &acc)
 {
     using T = typename C::T;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    const int64_t row0 = r0 + wave / C::WN * (C::BM / C::WM) + (lane & 31), col0 = c0 + wave % C::WN * (C::BN / C::WN);
     for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
         int64_t lo, hi;
         range_of(a.ad.offsets, s, a.rows, lo, hi);
@@ -183,7 +181,7 @@ __device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_
             bool in[C::TM];
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
-                const int64_t row = row0 + 32 * i;
+                const int64_t row = r0 + C::row_of(i);
                 in[i] = row >= lo && row < hi && row < r1;
                 u[i] = in[i] ? a.ad.u[row * a.ad.kmax + k] : 0.f;
                 if constexpr (std::is_same<T, f16_t>::value)
@@ -192,8 +190,8 @@ __device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_
 #pragma unroll
             for (int j = 0; j < C::TN; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int64_t col = col0 + 32 * j + acc_row(v, lane >> 5);
+                for (int v = 0; v < 4; ++v) {
+                    const int64_t col = c0 + C::col_of(j) + v;
                     const float x = Type<T>::load(h[col < a.n ? col : a.n - 1]);
 #pragma unroll
                     for (int i = 0; i < C::TM; ++i) acc[i][j][v] = in[i] ? __builtin_fmaf(u[i], x, acc[i][j][v]) : acc[i][j][v];
@@ -209,14 +207,13 @@ template <class C, class X>
 __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t r1, int64_t c0, char *lds, typename C::Acc &acc)
 {
     using T = typename C::T;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int kp = (a.ad.kmax + 31) / 32 * 32;
     const int64_t row_n = kp * (4 / (int)sizeof(T));
     bool left_out = false;
     typename X::ReadP rp;
     typename X::ReadQ rq;
-    rp.open(wave / C::WN * (C::BM / C::WM));
-    rq.open(wave % C::WN * (C::BN / C::WN));
+    rp.open(X::wave_row());
+    rq.open(X::wave_col());
     for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
         int64_t lo, hi;
         range_of(a.ad.offsets, s, a.rows, lo, hi);
@@ -254,8 +251,8 @@ __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t
             const int stages = bad ? 0 : (k + X::SK < run.k ? 2 : 1);
             for (int h = 0; h < stages; ++h) {
                 const char *stage = lds + h * X::kLdsStage;
-                [[maybe_unused]] const int left = run.k - k - h * X::SK;      // steps without factors: left out where they take long
-                if constexpr (sizeof(T) == 4) X::first_steps(stage, rp, rq, acc, left > 24 ? 4 : (left + 7) / 8);
+                // floats: a matrix step without factors is left out, it takes long
+                if (sizeof(T) == 4 && run.k - k - h * X::SK <= X::SK / 2) X::first_step(stage, rp, rq, acc);
                 else X::step(stage, rp, rq, acc, [](int) {});
             }
             meet();
@@ -267,15 +264,12 @@ __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t
 // Accumulators of f16 tiles out of the rows' scales.
 template <class C> __device__ __forceinline__ void unscale(const Product &a, int64_t r0, int64_t r1, typename C::Acc &acc)
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < C::TM; ++i) {
-        const int64_t row = r0 + wave / C::WN * (C::BM / C::WM) + 32 * i + (lane & 31);
+        const int64_t row = r0 + C::row_of(i);
         const float up = a.row_scale[row < r1 ? row : r0];
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] *= up;
+        for (int j = 0; j < C::TN; ++j) acc[i][j] *= up;
     }
 }
 
@@ -495,7 +489,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     constexpr int BN = 128, SK = stage_k<E>();
     constexpr bool two = two_piece_matrix<T>(), both = Cut<T>::kBoth;
     constexpr int kP = SK * BM * (int)sizeof(E), kQ = SK * BN * (int)sizeof(E);
-    constexpr int TM = BM / 32;
+    constexpr int TM = BM / 16, TN = 2;
     constexpr int kAllP = kP * (both ? 2 : 1), kStage = kAllP + kQ * (two ? 2 : 1);
     __shared__ __align__(1024) char lds[2 * kStage];
 
@@ -516,15 +510,15 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     if (k > a.ad.kmax) k = a.ad.kmax;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    Reader<E, BM, true> rp;
-    Reader<E, BN, true> rq;
+    Reader<E, BM, true, 16> rp;
+    Reader<E, BN, true, 16> rq;
     rp.open(0);
     rq.open(wave * 32);
-    f32x16 acc[TM], low[TM];                               // products of the first pieces, and of the others
+    f32x4 acc[TM][TN], low[TM][TN];                        // products of the first pieces, and of the others
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][v] = low[i][v] = 0.f;
+        for (int j = 0; j < TN; ++j) acc[i][j] = low[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     constexpr int EN = chunk_n<E>(), TE = chunk_n<T>();
     constexpr int pc = BM / EN, PJ = SK * pc / 256, qc = BN / TE, QJ = SK * qc / 256;
@@ -613,16 +607,26 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         if (more) get();
         const char *lp = lds + (n & 1) * kStage, *lq = lp + kAllP;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const u32x4 q = rq.read(lq, 0, kk);
+        for (int kk = 0; kk < kStageBytes / 64; ++kk) {
+            u32x4 q[TN], ql[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                q[j] = rq.read(lq, j, kk);
+                if constexpr (two) ql[j] = rq.read(lq + kQ, j, kk);
+            }
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
                 const u32x4 p = rp.read(lp, i, kk);
-                if constexpr (both) {
-                    if constexpr (two) low[i] = Type<E>::mac(rq.read(lq + kQ, 0, kk), p, low[i]);
-                    low[i] = Type<E>::mac(q, rp.read(lp + kP, i, kk), low[i]);
+                u32x4 pl2;
+                if constexpr (both) pl2 = rp.read(lp + kP, i, kk);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    if constexpr (both) {
+                        if constexpr (two) low[i][j] = Type<E>::mac(ql[j], p, low[i][j]);
+                        low[i][j] = Type<E>::mac(q[j], pl2, low[i][j]);
+                    }
+                    acc[i][j] = Type<E>::mac(q[j], p, acc[i][j]);
                 }
-                acc[i] = Type<E>::mac(q, p, acc[i]);
             }
         }
         if (more) put(lds + ((n + 1) & 1) * kStage);
@@ -630,23 +634,24 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     const int64_t m4 = up4(a.m), n4 = up4(a.n);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int row = 32 * i + (lane & 31);
+        const int row = 16 * i + (lane & 15);
         if (row >= mine) continue;
         const bool real = f0 + row < k;                     // factors beyond kmax take no part: zero
+        const int64_t line = klo + f0 + row;
+        float *part = nullptr;
+        if (a.splits > 1)
+            part = down ? a.part + ((int64_t)split * a.ad.ktotal + line) * m4
+                        : a.part + (int64_t)a.splits * a.ad.ktotal * m4 + ((int64_t)split * a.ad.ktotal + line) * n4;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int64_t col = c0 + 32 * wave + acc_row(v, lane >> 5);
-            if (col >= width) continue;
-            const float x = real ? both_pieces<both>(acc[i][v], low[i][v]) : 0.f;
-            const int64_t line = klo + f0 + row;
-            if (a.splits > 1) {
-                float *o = down ? a.part + ((int64_t)split * a.ad.ktotal + line) * m4
-                                : a.part + (int64_t)a.splits * a.ad.ktotal * m4 + ((int64_t)split * a.ad.ktotal + line) * n4;
-                o[col] = x;
-            } else {
-                ((T *)(down ? a.ddown : a.dup))[line * width + col] = Type<T>::round(x);
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t col = c0 + 32 * wave + 16 * j + 4 * (lane >> 4) + v;
+                if (col >= width) continue;
+                const float x = real ? both_pieces<both>(acc[i][j][v], low[i][j][v]) : 0.f;
+                if (part) part[col] = x;
+                else ((T *)(down ? a.ddown : a.dup))[line * width + col] = Type<T>::round(x);
             }
-        }
     }
 }
 
