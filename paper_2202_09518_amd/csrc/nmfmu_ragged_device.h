@@ -19,6 +19,7 @@
 #include "nmfmu_ragged_internal.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace nmfmu {
 namespace ragged {
@@ -28,7 +29,8 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 template <class T> struct Type;
 template <> struct Type<bf16_t> {
     static constexpr int kBytes = 2;
-    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
+    static constexpr int kParts = 1;      // matrix instructions of a step
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c, int)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), c, 0, 0, 0);
     }
@@ -41,7 +43,8 @@ template <> struct Type<bf16_t> {
 };
 template <> struct Type<f16_t> {
     static constexpr int kBytes = 2;
-    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c, int)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, q), __builtin_bit_cast(f16x8, p), c, 0, 0, 0);
     }
@@ -57,11 +60,10 @@ template <> struct Type<f16_t> {
 };
 template <> struct Type<float> {
     static constexpr int kBytes = 4;
-    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c)
+    static constexpr int kParts = 4;
+    static __device__ __forceinline__ f32x4 mac(u32x4 q, u32x4 p, f32x4 c, int part)
     {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[j]), __uint_as_float(p[j]), c, 0, 0, 0);
-        return c;
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[part]), __uint_as_float(p[part]), c, 0, 0, 0);
     }
     static __device__ __forceinline__ float load(float x) { return x; }
     static __device__ __forceinline__ float round(float x) { return x; }
@@ -70,6 +72,24 @@ template <> struct Type<float> {
 constexpr int kStageBytes = 128;      // bytes of k in a stage, if not said otherwise
 constexpr unsigned kOutside = 0xfffffff0u;
 constexpr int kBufferFlags = 0x00020000;
+
+// c[i] += q[j] p for the columns' blocks j: parts outside, so that no instruction waits for the one before it.
+template <class T, int N> __device__ __forceinline__ void mac_row(const u32x4 (&q)[N], u32x4 p, f32x4 (&c)[N])
+{
+#pragma unroll
+    for (int part = 0; part < Type<T>::kParts; ++part)
+#pragma unroll
+        for (int j = 0; j < N; ++j) c[j] = Type<T>::mac(q[j], p, c[j], part);
+}
+
+// f(0), ..., f(N - 1) with constants.
+template <class F, int... I> __device__ __forceinline__ void each_of(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F &&f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+// How many of `jobs` jobs dealt out over `slots` slots are due by the end of slot n.
+constexpr int jobs_due(int n, int jobs, int slots) { return n * jobs / slots + 1 < jobs ? n * jobs / slots + 1 : jobs; }
 
 // k of a stage.
 template <class T, int SB = kStageBytes> constexpr int stage_k() { return SB / Type<T>::kBytes; }
@@ -331,9 +351,7 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 get(kk + 1);
             }
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[kk % D][j], p[kk % D][i], acc[i][j]);
+            for (int i = 0; i < TM; ++i) mac_row<T>(q[kk % D], p[kk % D][i], acc[i]);
         }
     }
 
@@ -357,37 +375,42 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
         auto run = [&](auto live) {
             constexpr int LIVE = live.value, N = LIVE * TN, R = LIVE + TN;
             u32x4 p[2][TM], q[2][TN];
-            auto get = [&](int n, int kk, const char *stage) {      // operand n of a step
-                if (n < TN) q[kk][n] = rq.read(stage + kLdsP, n, kk);
-                else p[kk][n - TN] = rp.read(stage, n - TN, kk);
+            auto get = [&](auto n, auto kk, const char *stage) {      // operand n of a step
+                if constexpr (n.value < TN) q[kk.value][n.value] = rq.read(stage + kLdsP, n.value, kk.value);
+                else p[kk.value][n.value - TN] = rp.read(stage, n.value - TN, kk.value);
             };
-            // products of step kk, and `jobs` jobs between them
-            auto products = [&](int kk, int jobs, auto job) {
-                int done = 0;
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    acc[n / TN][n % TN] = Type<T>::mac(q[kk][n % TN], p[kk][n / TN], acc[n / TN][n % TN]);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (; done < jobs && done * (N - 4) <= n * jobs; ++done) job(done);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            // products of step kk, and jobs between them
+            auto products = [&](auto kk, auto jobs, auto job) {
+                constexpr int parts = Type<T>::kParts, J = jobs.value, all = N * parts;
+                each<all>([&](auto n) {
+                    constexpr int i = n.value / (TN * parts), part = n.value / TN % parts, j = n.value % TN;
+                    acc[i][j] = Type<T>::mac(q[kk.value][j], p[kk.value][i], acc[i][j], part);
+                    constexpr int past = n.value ? jobs_due(n.value - 1, J, all - 4) : 0, due = jobs_due(n.value, J, all - 4);
+                    if constexpr (due > past) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        each<due - past>([&](auto t) { job(std::integral_constant<int, past + t.value>{}); });
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
             };
-#pragma unroll
-            for (int n = 0; n < R; ++n) get(n, 0, lds);
+            using First = std::integral_constant<int, 0>;
+            using Second = std::integral_constant<int, 1>;
+            each<R>([&](auto n) { get(n, First{}, lds); });
             for (int s = 0; s < steps; ++s) {
                 char *now = lds + (s & 1) * kLdsStage, *next = lds + (~s & 1) * kLdsStage;
                 const int64_t k = k0 + (int64_t)(s + 2) * SK;
-                products(0, R, [&](int n) { get(n, 1, now); });
+                products(First{}, std::integral_constant<int, R>{}, [&](auto n) { get(n, Second{}, now); });
                 wait_loads<0>();
                 meet();
                 __builtin_amdgcn_sched_barrier(0);
-                products(1, R + L, [&](int n) {
+                products(Second{}, std::integral_constant<int, R + L>{}, [&](auto n) {
                     // loads and reads in turn while there are both
-                    const int r = n < 2 * (R < L ? R : L) ? (n & 1 ? n / 2 : -1 - n / 2) : (R > L ? n - L : -1 - (n - R));
-                    if (r >= 0) get(r, 0, next);
-                    else if (-1 - r < LoadQ::kJobs) lq.fetch_job(-1 - r, k, k1, now + kLdsP);
-                    else lp.fetch_job(-1 - r - LoadQ::kJobs, k, k1, now);
+                    constexpr int both = 2 * (R < L ? R : L), m = n.value;
+                    constexpr bool reads = m < both ? m % 2 == 1 : R > L;
+                    constexpr int nth = m < both ? m / 2 : m - both / 2;
+                    if constexpr (reads) get(std::integral_constant<int, nth>{}, First{}, next);
+                    else if constexpr (nth < LoadQ::kJobs) lq.fetch_job(nth, k, k1, now + kLdsP);
+                    else lp.fetch_job(nth - LoadQ::kJobs, k, k1, now);
                 });
             }
         };
@@ -405,9 +428,7 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
 #pragma unroll
         for (int i = 0; i < TM; ++i) p[i] = rp.read(lds, i, 0);
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = Type<T>::mac(q[j], p[i], acc[i][j]);
+        for (int i = 0; i < TM; ++i) mac_row<T>(q, p[i], acc[i]);
     }
 
     // acc += the product over k in [k0, k1) of K.  Leaves LDS free for other use.

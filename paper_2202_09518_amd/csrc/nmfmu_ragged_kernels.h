@@ -619,14 +619,9 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
                 const u32x4 p = rp.read(lp, i, kk);
                 u32x4 pl2;
                 if constexpr (both) pl2 = rp.read(lp + kP, i, kk);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    if constexpr (both) {
-                        if constexpr (two) low[i][j] = Type<E>::mac(ql[j], p, low[i][j]);
-                        low[i][j] = Type<E>::mac(q[j], pl2, low[i][j]);
-                    }
-                    acc[i][j] = Type<E>::mac(q[j], p, acc[i][j]);
-                }
+                if constexpr (two) mac_row<E>(ql, p, low[i]);
+                if constexpr (both) mac_row<E>(q, pl2, low[i]);
+                mac_row<E>(q, p, acc[i]);
             }
         }
         if (more) put(lds + ((n + 1) & 1) * kStage);
