@@ -8,6 +8,7 @@ has not been built, importing the symbols raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -309,37 +310,55 @@ _TYPES = {torch.float32: NMF_F32, torch.bfloat16: NMF_BF16, torch.float16: NMF_F
 
 
 def _type(t: torch.Tensor, what: str) -> int:
-    if not t.is_cuda or t.dtype not in _TYPES:
+    typ = _TYPES.get(t.dtype)
+    if typ is None or not t.is_cuda:
         raise ValueError(f"{what}: need a float32, bfloat16 or float16 device tensor")
-    return _TYPES[t.dtype]
+    return typ
 
 
 def _rows_of(t, dtype, rows, cols, what):
     """(pointer, leading dimension) of a rows x cols matrix whose rows are contiguous."""
-    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols
-            and (cols <= 1 or t.stride(1) == 1)):
-        raise ValueError(f"{what}: need a {rows} x {cols} {dtype} device tensor with contiguous rows")
-    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
-    if ld < cols:
-        raise ValueError(f"{what}: rows overlap")
-    return t.data_ptr(), ld
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+        ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            if ld >= cols:
+                return t.data_ptr(), ld
+            if rows <= 1:
+                return t.data_ptr(), cols
+    raise ValueError(f"{what}: need a {rows} x {cols} {dtype} device tensor with contiguous rows that do not overlap")
 
 
 def _stack_of(t, dtype, count, rows, cols, what):
     """(pointer, leading dimension, stride) of `count` such matrices."""
-    if not (t.is_cuda and t.dtype == dtype and t.dim() == 3 and tuple(t.shape) == (count, rows, cols)
-            and (cols <= 1 or t.stride(2) == 1)):
-        raise ValueError(f"{what}: need a {count} x {rows} x {cols} {dtype} device tensor with contiguous rows")
-    ld = t.stride(1) if rows > 1 else max(cols, t.stride(1))
-    if ld < cols:
-        raise ValueError(f"{what}: rows overlap")
-    return t.data_ptr(), ld, t.stride(0) if count > 1 else max((rows - 1) * ld + cols, t.stride(0))
+    if t.dtype is dtype and t.is_cuda and t.shape == (count, rows, cols):
+        stride, ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            if rows <= 1 and ld < cols:
+                ld = cols
+            if ld >= cols:
+                return t.data_ptr(), ld, stride if count > 1 else max((rows - 1) * ld + cols, stride)
+    raise ValueError(f"{what}: need a {count} x {rows} x {cols} {dtype} device tensor with contiguous rows that do not overlap")
 
 
 def _list(t, dtype, count, what):
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == count):
-        raise ValueError(f"{what}: need a contiguous {dtype} device tensor of {count} entries")
-    return t.data_ptr()
+    if t.dtype is dtype and t.is_cuda and t.numel() == count and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{what}: need a contiguous {dtype} device tensor of {count} entries")
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less a call than the stream object
+
+
+def _stream_at(t, stream) -> int:
+    """The stream of a call: the current one of the tensor's device if none is given."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(t.get_device())
+    return _stream(stream)
+
+
+@functools.lru_cache(maxsize=1024)
+def _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal) -> int:
+    return int(lib().nmf_ragged_work_bytes(kind, typ, rows, m, n, parts, runs, kmax, ktotal))
 
 
 def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, like, stream):
@@ -348,7 +367,7 @@ def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, like, stream):
         if not (work.is_cuda and work.dtype == torch.uint8 and work.is_contiguous()):
             raise ValueError("work: need a contiguous uint8 device tensor")
         return work.data_ptr(), work.numel(), work
-    need = lib().nmf_ragged_work_bytes(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
+    need = _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
     if need == 0:
         return None, 0, None
     buf = torch.empty(need, dtype=torch.uint8, device=like.device)
@@ -370,7 +389,7 @@ def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=N
     y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
     w, nbytes, _keep = _work(0, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
     _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
-                                     int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream(stream)))
+                                     int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(X, stream)))
 
 
 def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, stream=None) -> None:
@@ -381,7 +400,7 @@ def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, strea
     g, ldg, stride_g = _stack_of(G, X.dtype, groups, m, n, "G")
     w, nbytes, _keep = _work(1, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
     _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, m, n,
-                                      g, ldg, stride_g, w, nbytes, _stream(stream)))
+                                      g, ldg, stride_g, w, nbytes, _stream_at(X, stream)))
 
 
 def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt, H, koff, runs, kmax, scale, U, Y,
@@ -398,7 +417,7 @@ def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt
         _list(run, torch.int32, segments, "run"), segments, _list(Wt, X.dtype, ktotal * m, "Wt"), _list(H, X.dtype, ktotal * n, "H"),
         _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal,
         None if scale is None else _list(scale, torch.float32, runs, "scale"), _list(U, torch.float32, rows * kmax, "U"), y, ldy,
-        w, nbytes, _stream(stream)))
+        w, nbytes, _stream_at(X, stream)))
 
 
 def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work=None, stream=None) -> None:
@@ -412,4 +431,4 @@ def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, 
         typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, segments + 1, "offsets"), _list(run, torch.int32, segments, "run"),
         segments, _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, rows * kmax, "U"),
         _list(V, torch.float32, rows * kmax, "V"), _list(dWt, X.dtype, ktotal * m, "dWt"), _list(dH, X.dtype, ktotal * n, "dH"),
-        w, nbytes, _stream(stream)))
+        w, nbytes, _stream_at(X, stream)))

@@ -23,43 +23,56 @@ struct Plan {
     int shape, splits;
 };
 
-// Parts of a contraction of k for `tiles` workgroups: enough of them for two on each compute unit, each at least four
-// stages long.
-int splits_for(int64_t tiles, int64_t k, int stage)
+// Parts of a contraction of k for `tiles` workgroups, so that there are about `workgroups`, each at least four stages long.
+int splits_for(int64_t tiles, int64_t workgroups, int64_t k, int stage)
 {
-    const int64_t want = 2 * kComputeUnits / std::max<int64_t>(tiles, 1), have = k / (4 * stage);
+    const int64_t want = workgroups / std::max<int64_t>(tiles, 1), have = k / (4 * stage);
     const int64_t s = std::min<int64_t>(std::min(want, have), kMaxSplits);
     return s < 2 ? 1 : (int)s;
 }
 
-// Tile shape and parts of a product of `rows` rows in `groups` ranges.
+// Tile shape and parts of a product of `rows` rows in `groups` ranges.  us, bf16 unless said otherwise:
+//   256 x 256 where that gives most compute units a tile: 8192 x 4096 x 4096 takes 207; 128 x 128 of 2000 x 4096 x 2048
+//   takes 56, 64 x 64 63.  Of 1000 x 2048 x 1024, 64 tiles of 128 x 128, 64 x 64 takes 14.6 and 128 x 128 28.9, of 2048 x
+//   1024 x 2048, 256 tiles, 21.5 and 19.0: the small tile below one large one for each compute unit (two for floats, whose
+//   products hide a small tile's reads: 1999 rows of 720 x 1000 with their gradient 85 and 119).  Up to 256 rows of a large
+//   matrix, which each row of tiles reads again, stay with the large one: 160 x 8192 x 4096 49 and 56.
+//   Few rows: tiles of 64 or 32 rows.
+//   Parts: 500 x 4096 x 1000 (128 tiles) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024 (48) 25.8, 13.5 with
+//   four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their adapters (32 tiles) 17.7
+//   with eight, 20.1 with four, 23.4 with sixteen.
 Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
 {
     groups = std::max<int64_t>(1, std::min(groups, rows));
     const int64_t avg = ceil_div(rows, groups);
     auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
+    const bool floats = type == NMF_F32;
     Plan p;
-    if (avg >= (groups > 1 ? 400 : 256) && tiles(0) >= 200) p.shape = 0;
-    else if (avg > 64) p.shape = 1;
-    else if (avg > 32) p.shape = 2;
-    else p.shape = 3;
-    p.splits = p.shape == 0 || rows > 4096 ? 1 : splits_for(tiles(p.shape), m, stage_of(type));
+    if (avg >= (groups > 1 ? 400 : 256) && tiles(k256x256) >= 200) p.shape = k256x256;
+    else if (avg <= 32) p.shape = k32x128;
+    else if (avg <= 64) p.shape = k64x128;
+    else if (tiles(k128x128) >= (floats ? 2 : 1) * kComputeUnits || (avg <= 256 && groups * m * n * bytes_of(type) > (32 << 20))) p.shape = k128x128;
+    else p.shape = k64x64;
+    const int64_t workgroups = p.shape != k64x64 ? kComputeUnits : (floats ? 800 : 400);
+    p.splits = p.shape == k256x256 || rows > 4096 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage_of(type));
     return p;
 }
 
+// The same for a gradient, m x n for each group.  Parts of it cost their size again, written and read: only where there are few.
 Plan gradient_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
 {
     auto tiles = [&](int shape) { return groups * ceil_div(m, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
     Plan p;
-    p.shape = tiles(0) >= 200 ? 0 : 1;
-    p.splits = p.shape == 0 ? 1 : splits_for(tiles(1), ceil_div(rows, groups), stage_of(type));
+    if (tiles(k256x256) >= 200) p.shape = k256x256;
+    else p.shape = tiles(k128x128) >= (type == NMF_F32 ? 2 : 1) * kComputeUnits ? k128x128 : k64x64;
+    p.splits = p.shape == k64x64 ? splits_for(tiles(p.shape), kComputeUnits, ceil_div(rows, groups) / 2, stage_of(type)) : 1;
     return p;
 }
 
 int shrink_plan(int32_t type, int64_t rows, int64_t segments, int64_t m, int kmax)
 {
     const int64_t tiles = (ceil_div(rows, kShrinkRows) + std::min(segments, rows)) * ceil_div(kmax, kShrinkCols);
-    return splits_for(tiles, m, stage_of(type));
+    return splits_for(tiles, rows > 4096 ? 2 * kComputeUnits : kComputeUnits, m, stage_of(type));
 }
 
 // A tile runs its segments' adapters one after the other, 2.5 us each; where segments are short, the launch that joins parts
@@ -69,7 +82,7 @@ bool joined_plan(int64_t rows, int64_t segments, int splits) { return splits > 1
 int factor_plan(int32_t type, int64_t rows, int64_t runs, int64_t m, int64_t n, int kmax)
 {
     const int64_t tiles = runs * ceil_div(kmax, kmax <= 32 ? 32 : 64) * (ceil_div(m, 128) + ceil_div(n, 128));
-    return splits_for(tiles, ceil_div(rows, runs), stage_of(type));
+    return splits_for(tiles, 2 * kComputeUnits, ceil_div(rows, runs), stage_of(type));
 }
 
 size_t product_part(int64_t rows, int64_t n, int splits) { return (size_t)splits * rows * up4(n) * 4; }

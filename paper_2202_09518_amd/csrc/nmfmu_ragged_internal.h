@@ -9,9 +9,9 @@
 namespace nmfmu {
 namespace ragged {
 
-// Tile shapes of the product kernels, largest first.
-constexpr int kShapes = 4;
-constexpr int kTileRows[kShapes] = {256, 128, 64, 32}, kTileCols[kShapes] = {256, 128, 128, 128};
+// Tile shapes of the product kernels (gradients: those of as many rows as columns).
+enum Shape { k256x256, k128x128, k64x64, k64x128, k32x128 };
+constexpr int kTileRows[] = {256, 128, 64, 64, 32}, kTileCols[] = {256, 128, 64, 128, 128};
 constexpr int kShrinkRows = 64, kShrinkCols = 64;
 constexpr int kMaxSplits = 16, kMaxRank = 256;
 
