@@ -79,17 +79,26 @@ int shrink_plan(int32_t type, int64_t rows, int64_t segments, int64_t m, int kma
 // adds the adapters row by row, for the price of the product's floats written and read once (26 us for a tile of 256 x 256).
 bool joined_plan(int64_t rows, int64_t segments, int splits) { return splits > 1 || rows < 24 * segments; }
 
-int factor_plan(int32_t type, int64_t rows, int64_t runs, int64_t m, int64_t n, int kmax)
+// Blocks of rows to a workgroup, and chunks of so many: about four workgroups for each compute unit, at least four blocks each.
+struct FactorPlan {
+    int chunk, chunks;
+};
+FactorPlan factor_plan(int32_t type, int64_t rows, int64_t segments, int64_t runs, int64_t m, int64_t n, int kmax)
 {
-    const int64_t tiles = runs * ceil_div(kmax, kmax <= 32 ? 32 : 64) * (ceil_div(m, 128) + ceil_div(n, 128));
-    return splits_for(tiles, 2 * kComputeUnits, ceil_div(rows, runs), stage_of(type));
+    const int64_t tiles = ceil_div(kmax, factor_tile(kmax)) * (ceil_div(m, 128) + ceil_div(n, 128));
+    const int64_t blocks = ceil_div(rows, factor_rows(bytes_of(type))) + std::min(segments, rows);
+    const int64_t chunk = std::max<int64_t>(4, ceil_div(blocks, std::max<int64_t>(1, 4 * kComputeUnits / tiles)));
+    return FactorPlan{(int)chunk, (int)(ceil_div(blocks, chunk) + runs)};
 }
 
 size_t product_part(int64_t rows, int64_t n, int splits) { return (size_t)splits * rows * up4(n) * 4; }
 size_t shrink_part(int64_t rows, int kmax, int splits) { return splits > 1 ? (size_t)splits * up4(rows * kmax) * 4 : 0; }
 size_t pack_part(int64_t rows, int kmax) { return (size_t)rows * (4 * ceil_div(kmax, 32) * 32) + (size_t)up4(rows) * 4; }
 size_t gradient_part(int64_t groups, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * groups * m * up4(n) * 4 : 0; }
-size_t factor_part(int64_t ktotal, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * ktotal * (up4(m) + up4(n)) * 4 : 0; }
+size_t factor_part(int kmax, int64_t m, int64_t n, int chunks)
+{
+    return (size_t)chunks * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * (up4(m) + up4(n)) * 4;
+}
 
 // Splits that a scratch of `have` bytes can hold.
 template <class F> int fit(int splits, size_t have, F bytes)
@@ -257,9 +266,15 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     p.x = X; p.dy = dY; p.ldx = ldx; p.ldy = ldy; p.rows = rows; p.m = m; p.n = n;
     p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, nullptr, nullptr, nullptr, nullptr};
     p.u = U; p.v = V; p.ddown = dWt; p.dup = dH;
-    p.splits = fit(factor_plan(type, rows, runs, m, n, kmax), work_bytes, [&](int s) { return factor_part(ktotal, m, n, s); });
+    const FactorPlan plan = factor_plan(type, rows, segments, runs, m, n, kmax);
+    p.chunk = plan.chunk;
+    p.chunks = plan.chunks;
     p.part = static_cast<float *>(work);
-    if ((int64_t)runs * ceil_div(kmax, 32) > 65535) return set_error(NMF_EUNSUPPORTED, "more runs than one launch can have");
+    if (factor_part(kmax, m, n, p.chunks) > work_bytes) {      // each run in one chunk
+        p.chunk = 1 << 30;
+        p.chunks = runs;
+    }
+    if (p.chunks > 65535 || (int64_t)runs * kmax > 65535) return set_error(NMF_EUNSUPPORTED, "more runs than one launch can have");
     return launched(type, p, stream, launch_factor_gradient<float>, launch_factor_gradient<bf16_t>, launch_factor_gradient<f16_t>);
 }
 
@@ -282,8 +297,8 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
                shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax));
     }
     case 3:
-        if (runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
-        return factor_part(ktotal, m, n, factor_plan(type, rows, runs, m, n, kmax));
+        if (parts < 1 || runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
+        return factor_part(kmax, m, n, factor_plan(type, rows, parts, runs, m, n, kmax).chunks);
     }
     return 0;
 }

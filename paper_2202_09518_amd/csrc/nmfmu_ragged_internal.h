@@ -72,9 +72,13 @@ struct FactorGradient {
     Adapters ad;                 // its u, down, up and scale are not used
     const float *u, *v;          // rows x kmax
     void *ddown, *dup;           // ktotal x m, ktotal x n
-    int splits;
-    float *part;                 // splits x ktotal x (m rounded up to 4 + n rounded up to 4)
+    int chunk, chunks;           // blocks of rows (factor_rows) to a workgroup, and how many such chunks there can be
+    float *part;                 // chunks x (kmax in whole tiles) x (m rounded up to 4 + n rounded up to 4)
 };
+
+// Rows of a block, and factors of a tile.
+inline int factor_rows(int bytes) { return bytes == 4 ? 32 : 64; }
+inline int factor_tile(int kmax) { return kmax <= 32 ? 32 : 64; }
 
 // Types by their bits (float as it is).
 struct bf16_t { unsigned short bits; };

@@ -48,11 +48,17 @@ template <> struct Cut<float> {
 template <class T> constexpr bool two_piece_matrix() { return false; }
 template <> constexpr bool two_piece_matrix<f16_t>() { return true; }      // its 11 bits are two bf16
 
-// Entries [k, k + N) of a row of floats that ends at kend; zero behind it.
-template <int N> __device__ __forceinline__ void floats_at(const float *row, int k, int kend, float (&x)[N])
+// Entries [k, k + N) of a row of `width` floats, zero from kend on.
+template <int N> __device__ __forceinline__ void floats_at(const float *row, int k, int kend, int width, float (&x)[N])
 {
+    if (k + N <= width) {
+        __builtin_memcpy(x, row + k, sizeof(x));
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = k + i < kend ? row[k + i] : 0.f;
+        for (int i = 0; i < N; ++i) x[i] = k + i < kend ? x[i] : 0.f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = k + i < kend ? row[k + i] : 0.f;
+    }
 }
 
 // The product of the first pieces d with that of the others, which is left out where d is not finite: a second piece of an
@@ -197,6 +203,32 @@ __device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_
                     for (int i = 0; i < C::TM; ++i) acc[i][j][v] = in[i] ? __builtin_fmaf(u[i], x, acc[i][j][v]) : acc[i][j][v];
                 }
         }
+    }
+}
+
+// For floats a call with registers of its own (the training step of 4096 rows 1222 -> 1176 us); in 16 bits the same costs the
+// tile more than it gives (prompts 434 -> 478 us).
+template <class C>
+__device__ __noinline__ void add_plainly_called(const Product &a, int64_t r0, int64_t r1, int64_t c0, bool packed, int group, typename C::Acc &acc)
+{
+    add_plainly<C>(a, r0, r1, c0, packed, group, acc);
+}
+template <class C>
+__device__ __forceinline__ void add_rest(const Product &a, int64_t r0, int64_t r1, int64_t c0, bool packed, int group, typename C::Acc &acc)
+{
+    if constexpr (sizeof(typename C::T) == 2) {
+        add_plainly<C>(a, r0, r1, c0, packed, group, acc);
+    } else {
+        typename C::Acc copy;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) copy[i][j] = acc[i][j];
+        add_plainly_called<C>(a, r0, r1, c0, packed, group, copy);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) acc[i][j] = copy[i][j];
     }
 }
 
@@ -345,7 +377,7 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
         using X = Tile<T, C::BM, C::BN, C::WM, C::WN, 2, false, true, C::DMA, C::SB, (sizeof(T) == 2 ? 2 : 1)>;
         if (!a.joined) {
             const bool packed = a.pack != nullptr;
-            if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_plainly<C>(a, f.r0, f.r1, c0, packed, 2 * X::SK, acc);
+            if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_rest<C>(a, f.r0, f.r1, c0, packed, 2 * X::SK, acc);
             if constexpr (std::is_same<T, f16_t>::value)
                 if (packed) unscale<C>(a, f.r0, f.r1, acc);
         }
@@ -489,8 +521,53 @@ __global__ __launch_bounds__(256) void join_kernel(const float *part, int splits
     }
 }
 
-// Gradients of the factors of one run: BM of its factors x 128 columns of m or of n, summed over the rows of its segments,
-// 64 (halves) or 32 (floats) rows at a time.
+// ---- gradients of the factors --------------------------------------------------------
+// A run's rows, in blocks of `rows` within its segments, are dealt out in chunks of `chunk` blocks, so that a run with many
+// rows takes many workgroups and one without rows a single one, which writes its zeros.
+struct Chunks {
+    int run, first, count;       // a run; its first chunk and how many it has
+};
+// Of chunk `want`, or of run `want`.
+template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const FactorGradient &a, int rows, int want, Chunks &f)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int r0 = 0; r0 < a.ad.runs; r0 += 64) {
+        int blocks = 0;
+        for (int base = 0; base < a.ad.segments; base += 64) {
+            int of = -1, nb = 0;
+            if (base + lane < a.ad.segments) {
+                int64_t lo, hi;
+                range_of(a.ad.offsets, base + lane, a.rows, lo, hi);
+                of = a.ad.run[base + lane];
+                nb = (int)((hi - lo + rows - 1) / rows);
+            }
+            const int here = a.ad.segments - base < 64 ? a.ad.segments - base : 64;
+            for (int i = 0; i < here; ++i)
+                if (__builtin_amdgcn_readlane(of, i) == r0 + lane) blocks += __builtin_amdgcn_readlane(nb, i);
+        }
+        int count = 0;
+        if (r0 + lane < a.ad.runs) count = blocks <= a.chunk ? 1 : (blocks + a.chunk - 1) / a.chunk;
+        int sum = count;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        const unsigned long long past = __ballot(BY_RUN ? r0 + lane == want : before + sum > want);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            f.run = r0 + l;
+            f.count = __builtin_amdgcn_readlane(count, l);
+            f.first = before + __builtin_amdgcn_readlane(sum, l) - f.count;
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (halves) or 32 (floats) at a time.
 template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradient_kernel(FactorGradient a)
 {
     using E = typename Cut<T>::E;
@@ -507,9 +584,10 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     const char *src = (const char *)(down ? a.x : a.dy);
     const int64_t ld = down ? a.ldx : a.ldy;
     const float *fac = down ? a.v : a.u;
-    const int kt = (a.ad.kmax + BM - 1) / BM;
-    const int id = blockIdx.y / kt, f0 = blockIdx.y % kt * BM;
-    const int split = blockIdx.z;
+    const int f0 = blockIdx.y * BM, z = blockIdx.z;
+    Chunks mychunk;
+    if (!find_chunk(a, SK, z, mychunk)) return;
+    const int id = mychunk.run, from = (z - mychunk.first) * a.chunk;
     const int64_t klo = a.ad.koff[id], khi = a.ad.koff[id + 1];
     if (klo < 0 || khi <= klo || klo >= a.ad.ktotal) return;
     int64_t k = (khi < a.ad.ktotal ? khi : a.ad.ktotal) - klo;
@@ -531,7 +609,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     constexpr int EN = chunk_n<E>(), TE = chunk_n<T>();
     constexpr int pc = BM / EN, PJ = SK * pc / 256, qc = BN / TE, QJ = SK * qc / 256;
 
-    // The run's rows in blocks of SK within its segments; every a.splits-th is this workgroup's.
+    // The run's rows in blocks of SK within its segments: a.chunk of them from `from` on.
     int base = -64, turn = -1;
     unsigned long long todo = 0;
     int64_t lo = 0, hi = 0, r = 0, shi = 0;
@@ -555,7 +633,8 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
                 r = Ranges::lane_value(lo, l);
                 shi = Ranges::lane_value(hi, l);
             }
-            if (++turn % a.splits == split) return true;
+            if (++turn >= from + a.chunk) return false;
+            if (turn >= from) return true;
         }
     };
     u32x4 ph[PJ], pl[PJ], qv[QJ];
@@ -574,7 +653,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
             float x[EN];
-            floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, x);
+            floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, a.ad.kmax, x);
             if constexpr (both) cut_chunk(x, ph[j], pl[j]);
             else ph[j] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
         }
@@ -642,9 +721,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         const bool real = f0 + row < k;                     // factors beyond kmax take no part: zero
         const int64_t line = klo + f0 + row;
         float *part = nullptr;
-        if (a.splits > 1)
-            part = down ? a.part + ((int64_t)split * a.ad.ktotal + line) * m4
-                        : a.part + (int64_t)a.splits * a.ad.ktotal * m4 + ((int64_t)split * a.ad.ktotal + line) * n4;
+        if (mychunk.count > 1) part = a.part + ((int64_t)z * gridDim.y * BM + f0 + row) * (m4 + n4) + (down ? 0 : m4);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -656,6 +733,28 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
                 else ((T *)(down ? a.ddown : a.dup))[line * width + col] = Type<T>::round(x);
             }
     }
+}
+
+// The gradients of runs with several chunks: factor y of a run, 1024 columns of m and n side by side.
+template <class T, int BM> __global__ __launch_bounds__(256) void join_factors_kernel(FactorGradient a, int padded)
+{
+    constexpr int SK = stage_k<typename Cut<T>::E>();
+    const int id = blockIdx.y / a.ad.kmax, k = blockIdx.y % a.ad.kmax;
+    const int64_t lo = a.ad.koff[id], hi = a.ad.koff[id + 1];
+    if (lo < 0 || lo + k >= hi || lo + k >= a.ad.ktotal) return;
+    Chunks f;
+    if (!find_chunk<true>(a, SK, id, f)) return;
+    if (f.count < 2) return;
+    const int64_t m4 = up4(a.m), n4 = up4(a.n), at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= m4 + n4) return;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < f.count; ++c) y += *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)(f.first + c) * padded + k) * (m4 + n4) + at);
+    const bool down = at < m4;
+    const int64_t col = down ? at : at - m4, width = down ? a.m : a.n;
+    T *out = (T *)(down ? a.ddown : a.dup) + (lo + k) * width + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (col + e < width) out[e] = Type<T>::round(y[e]);
 }
 
 // ---- launches --------------------------------------------------------------------------
@@ -748,15 +847,16 @@ template <class T> hipError_t launch_gradient(const Gradient &p, hipStream_t st)
 template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hipStream_t st)
 {
     const unsigned cols = (unsigned)((p.m + 127) / 128 + (p.n + 127) / 128);
-    if (p.ad.kmax <= 32)
-        hipLaunchKernelGGL((factor_gradient_kernel<T, 32>), dim3(cols, (unsigned)p.ad.runs, p.splits), dim3(256), 0, st, p);
-    else
-        hipLaunchKernelGGL((factor_gradient_kernel<T, 64>), dim3(cols, (unsigned)(p.ad.runs * ((p.ad.kmax + 63) / 64)), p.splits), dim3(256), 0,
-                           st, p);
-    if (p.splits > 1) {
-        launch_join<T>(p.part, p.splits, p.ad.ktotal, p.m, (T *)p.ddown, p.ad.ktotal, 0, p.m, st);
-        launch_join<T>(p.part + (int64_t)p.splits * p.ad.ktotal * up4(p.m), p.splits, p.ad.ktotal, p.n, (T *)p.dup, p.ad.ktotal, 0, p.n, st);
-    }
+    auto go = [&](auto bm) {
+        constexpr int BM = bm.value;
+        const unsigned kt = (unsigned)((p.ad.kmax + BM - 1) / BM);
+        hipLaunchKernelGGL((factor_gradient_kernel<T, BM>), dim3(cols, kt, (unsigned)p.chunks), dim3(256), 0, st, p);
+        if (p.chunks > p.ad.runs)
+            hipLaunchKernelGGL((join_factors_kernel<T, BM>), dim3((unsigned)((up4(p.m) + up4(p.n) + 1023) / 1024), (unsigned)(p.ad.runs * p.ad.kmax)),
+                               dim3(256), 0, st, p, (int)kt * BM);
+    };
+    if (p.ad.kmax <= 32) go(std::integral_constant<int, 32>{});
+    else go(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 
