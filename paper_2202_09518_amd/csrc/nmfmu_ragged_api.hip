@@ -31,16 +31,31 @@ int splits_for(int64_t tiles, int64_t workgroups, int64_t k, int stage)
     return s < 2 ? 1 : (int)s;
 }
 
-// Tile shape and parts of a product of `rows` rows in `groups` ranges.  us, bf16 unless said otherwise:
-//   256 x 256 where that gives most compute units a tile: 8192 x 4096 x 4096 takes 207; 128 x 128 of 2000 x 4096 x 2048
-//   takes 56, 64 x 64 63.  Of 1000 x 2048 x 1024, 64 tiles of 128 x 128, 64 x 64 takes 14.6 and 128 x 128 28.9, of 2048 x
-//   1024 x 2048, 256 tiles, 21.5 and 19.0: the small tile below one large one for each compute unit (two for floats, whose
-//   products hide a small tile's reads: 1999 rows of 720 x 1000 with their gradient 85 and 119).  Up to 256 rows of a large
-//   matrix, which each row of tiles reads again, stay with the large one: 160 x 8192 x 4096 49 and 56.
-//   Few rows: tiles of 64 or 32 rows.
-//   Parts: 500 x 4096 x 1000 (128 tiles) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024 (48) 25.8, 13.5 with
-//   four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their adapters (32 tiles) 17.7
-//   with eight, 20.1 with four, 23.4 with sixteen.
+// Time of `tiles` tiles of a shape: those of the busiest compute unit, by their size and by what share of the large tile's
+// rate they reach.  us, bf16 unless said otherwise: 8192 x 4096 x 4096 takes 207 in tiles of 256 x 256; 2000 x 4096 x 2048
+// 56 in 128 x 128 and 63 in 64 x 64; 2048 x 1024 x 2048 19.0 and 21.5; 1000 x 2048 x 1024, only 64 tiles of 128 x 128, 28.9
+// and 14.6.  Float products hide a small tile's reads: 4096 x 4096 x 2048 with its gradients 1252 and 1439, 1999 rows of
+// 720 x 1000 with theirs 119 and 85; 2048 x 4095 x 4097, 272 tiles of 256 x 256 and so twice the time of 256, 1002.
+// Several groups of unequal lengths: the longest one's tiles take twice the others' at least.
+double tile_time(int shape, bool floats, int64_t tiles, bool unequal)
+{
+    static const double rate[2][3] = {{1.0, 0.72, 0.5}, {0.93, 0.85, 0.74}};      // 256 x 256, 128 x 128, 64 x 64
+    return (double)std::max<int64_t>(ceil_div(tiles, kComputeUnits), unequal ? 2 : 1) * kTileRows[shape] * kTileCols[shape] / rate[floats][shape];
+}
+template <class F> int fastest(bool floats, bool unequal, F tiles)
+{
+    int best = k256x256;
+    for (int shape : {k128x128, k64x64})
+        if (tile_time(shape, floats, tiles(shape), unequal) < tile_time(best, floats, tiles(best), unequal)) best = shape;
+    return best;
+}
+
+// Tile shape and parts of a product of `rows` rows in `groups` ranges.  Few rows take tiles of 64 or 32 rows, others the
+// fastest; but up to 256 rows of a large matrix, which each row of tiles reads again, take the 128 x 128 rather than the
+// 64 x 64 (160 x 8192 x 4096: 49 and 56 us).
+// Parts (us): 500 x 4096 x 1000 (128 tiles of 64 x 64) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024
+// (48) 25.8, 13.5 with four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their
+// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.
 Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
 {
     groups = std::max<int64_t>(1, std::min(groups, rows));
@@ -48,11 +63,10 @@ Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t
     auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
     const bool floats = type == NMF_F32;
     Plan p;
-    if (avg >= (groups > 1 ? 400 : 256) && tiles(k256x256) >= 200) p.shape = k256x256;
-    else if (avg <= 32) p.shape = k32x128;
+    if (avg <= 32) p.shape = k32x128;
     else if (avg <= 64) p.shape = k64x128;
-    else if (tiles(k128x128) >= (floats ? 2 : 1) * kComputeUnits || (avg <= 256 && groups * m * n * bytes_of(type) > (32 << 20))) p.shape = k128x128;
-    else p.shape = k64x64;
+    else p.shape = fastest(floats, false, tiles);
+    if (p.shape == k64x64 && avg <= 256 && groups * m * n * bytes_of(type) > (32 << 20)) p.shape = k128x128;
     const int64_t workgroups = p.shape != k64x64 ? kComputeUnits : (floats ? 800 : 400);
     p.splits = p.shape == k256x256 || rows > 4096 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage_of(type));
     return p;
@@ -63,8 +77,7 @@ Plan gradient_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_
 {
     auto tiles = [&](int shape) { return groups * ceil_div(m, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
     Plan p;
-    if (tiles(k256x256) >= 200) p.shape = k256x256;
-    else p.shape = tiles(k128x128) >= (type == NMF_F32 ? 2 : 1) * kComputeUnits ? k128x128 : k64x64;
+    p.shape = fastest(type == NMF_F32, groups > 1, tiles);
     p.splits = p.shape == k64x64 ? splits_for(tiles(p.shape), kComputeUnits, ceil_div(rows, groups) / 2, stage_of(type)) : 1;
     return p;
 }
@@ -105,6 +118,82 @@ template <class F> int fit(int splits, size_t have, F bytes)
 {
     while (splits > 1 && bytes(splits) > have) --splits;
     return splits;
+}
+
+// ---- operands whose rows do not begin and end on 16 bytes ----------------------------------
+// The tiles bring 16 bytes at a time straight to LDS; other operands pass registers, which takes 1.5 to 6 times as long
+// (8192 x 4095 x 4097 bf16: 517 us, 641 with B by columns, its gradient 1430; aligned 243, 223, 211).  Where the product is
+// long enough they are copied once per call into rows that do.
+struct Scratch {
+    char *at;
+    size_t left;
+    void *take(size_t bytes)
+    {
+        bytes = (bytes + 15) / 16 * 16;
+        if (bytes > left) return nullptr;
+        void *p = at;
+        at += bytes;
+        left -= bytes;
+        return p;
+    }
+};
+
+int64_t whole(int64_t cols, int e) { return (cols * e + 15) / 16 * 16 / e; }
+size_t copy_bytes(int64_t lines, int64_t cols, int e) { return (size_t)lines * whole(cols, e) * e; }
+
+// Copies of `bytes` are worth their time: launches and their bytes twice, against what the product loses without them, about as
+// long as it takes at a middling rate.  2048 x 1023 x 2049 bf16: 31 us, without 42; 1237 rows of 515 x 389 in 9 groups f32,
+// where they are not: 33 with, 25 without.
+bool worth_copies(int e, size_t bytes, double flops)
+{
+    return 5e-6 + 2.0 * bytes / 4.5e12 < 1.2 * flops / (e == 4 ? 0.8e14 : 0.5e15);
+}
+
+struct Matrix {
+    const void *p;
+    int64_t ld, stride, rows, cols, count;
+    bool bad(int e) const { return ((uintptr_t)p | (uint64_t)(ld * e) | (uint64_t)(count > 1 ? stride * e : 0) | (uint64_t)(cols * e)) & 15; }
+    size_t bytes(int e) const { return copy_bytes(count * rows, cols, e); }
+};
+
+// Copies those of `n` matrices that need it, if that is worth it and fits; returns whether all are whole now.
+int align_all(int32_t type, Matrix *const *all, int n, double flops, Scratch *s, hipStream_t st, bool *done)
+{
+    const int e = bytes_of(type);
+    size_t bytes = 0;
+    for (int i = 0; i < n; ++i)
+        if (all[i]->bad(e)) bytes += all[i]->bytes(e);
+    *done = false;
+    if (!bytes || bytes > s->left || !worth_copies(e, bytes, flops)) return NMF_OK;
+    for (int i = 0; i < n; ++i) {
+        Matrix &m = *all[i];
+        if (!m.bad(e)) continue;
+        Align a = {m.p, m.ld, m.count > 1 ? m.stride : 0, m.rows, m.cols, m.count, s->take(m.bytes(e)), whole(m.cols, e)};
+        const hipError_t rc = type == NMF_F32 ? launch_align<float>(a, st) : type == NMF_BF16 ? launch_align<bf16_t>(a, st) : launch_align<f16_t>(a, st);
+        if (rc != hipSuccess) return set_error(NMF_EHIP, hipGetErrorString(rc));
+        m.p = a.dst;
+        m.ld = a.ldo;
+        if (m.count > 1) m.stride = a.ldo * m.rows;
+    }
+    *done = true;
+    return NMF_OK;
+}
+// Scratch that they can take, by sizes alone.
+size_t copies_of(int32_t type, size_t bytes, double flops) { return bytes && worth_copies(bytes_of(type), bytes, flops) ? bytes : 0; }
+bool ragged_rows(int64_t cols, int e) { return cols * e % 16 != 0; }
+size_t product_copies(int32_t type, int64_t rows, int64_t count, int64_t m, int64_t n, int64_t ktotal)
+{
+    const int e = bytes_of(type);
+    size_t b = 0;
+    if (ragged_rows(m, e)) b += copy_bytes(rows, m, e) + copy_bytes(ktotal, m, e);
+    if (ragged_rows(n, e)) b += copy_bytes(ktotal, n, e);
+    if (ragged_rows(m, e) || ragged_rows(n, e)) b += std::max(copy_bytes(count * m, n, e), copy_bytes(count * n, m, e));
+    return copies_of(type, b, 2.0 * rows * m * n);
+}
+size_t gradient_copies(int32_t type, int64_t rows, int64_t m, int64_t n)
+{
+    const int e = bytes_of(type);
+    return copies_of(type, (ragged_rows(m, e) ? copy_bytes(rows, m, e) : 0) + (ragged_rows(n, e) ? copy_bytes(rows, n, e) : 0), 2.0 * rows * m * n);
 }
 
 bool sizes_ok(int64_t rows, int64_t m, int64_t n) { return rows >= 0 && m > 0 && n > 0 && rows <= kMost && m <= kMost && n <= kMost; }
@@ -157,13 +246,19 @@ int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t 
     p.x = X; p.ldx = ldx; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
     p.b = B; p.ldb = ldb; p.stride_b = stride_b; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
     p.shape = plan.shape;
-    p.splits = fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); });
-    p.joined = p.splits > 1;
-    p.k_split = ceil_div(ceil_div(m, stage_of(type)), p.splits) * stage_of(type);
-    p.part = static_cast<float *>(work);
     p.shrink_splits = 1;
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
+    Scratch scratch = {static_cast<char *>(work), work_bytes};
+    p.splits = fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); });
+    if (p.splits > 1) p.part = static_cast<float *>(scratch.take(product_part(rows, n, p.splits)));
+    p.joined = p.splits > 1;
+    p.k_split = ceil_div(ceil_div(m, stage_of(type)), p.splits) * stage_of(type);
     if ((rc = check_grid(std::max(product_grid(p), p.joined ? rows * ceil_div(n, 256) : 0)))) return rc;
+    Matrix x = {X, ldx, 0, rows, m, 1}, b = {B, ldb, stride_b, transposed ? n : m, transposed ? m : n, stride_b ? groups : 1};
+    Matrix *const operands[] = {&x, &b};
+    if ((rc = align_all(type, operands, 2, 2.0 * rows * m * n, &scratch, static_cast<hipStream_t>(stream), &p.padded))) return rc;
+    p.x = x.p; p.ldx = x.ld;
+    p.b = b.p; p.ldb = b.ld; p.stride_b = b.count > 1 ? b.stride : 0;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
 }
 
@@ -187,7 +282,16 @@ int nmf_grouped_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     p.splits = fit(plan.splits, work_bytes, [&](int s) { return gradient_part(groups, m, n, s); });
     p.part = static_cast<float *>(work);
     p.vec = aligned(G, 16) && ldg * e % 16 == 0 && stride_g * e % 16 == 0;
-    if ((rc = check_grid(ceil_div(m, kTileRows[p.shape]) * ceil_div(n, kTileCols[p.shape]) * groups * p.splits))) return rc;
+    if ((rc = check_grid((ceil_div(m, kTileRows[p.shape]) * ceil_div(n, kTileCols[p.shape]) * p.splits + 8) * groups))) return rc;
+    if (rows) {
+        Scratch scratch = {static_cast<char *>(work), work_bytes};
+        if (p.splits > 1) scratch.take(gradient_part(groups, m, n, p.splits));
+        Matrix x = {X, ldx, 0, rows, m, 1}, y = {dY, ldy, 0, rows, n, 1};
+        Matrix *const operands[] = {&x, &y};
+        if ((rc = align_all(type, operands, 2, 2.0 * rows * m * n, &scratch, static_cast<hipStream_t>(stream), &p.padded))) return rc;
+        p.x = x.p; p.ldx = x.ld;
+        p.dy = y.p; p.ldy = y.ld;
+    }
     return launched(type, p, stream, launch_gradient<float>, launch_gradient<bf16_t>, launch_gradient<f16_t>);
 }
 
@@ -214,33 +318,39 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
     Product p = {};
     p.x = X; p.ldx = ldx; p.groups = 1; p.rows = rows; p.m = m; p.n = n;
     p.b = A; p.ldb = lda; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
-    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, Wt, H, scale, U};
+    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, Wt, H, m, n, scale, U};
     p.shape = plan.shape;
     p.shrink_splits = 1;
     const int stage = stage_of(type);
-    char *at = static_cast<char *>(work), *end = at + work_bytes;
+    Scratch scratch = {static_cast<char *>(work), work_bytes};
     p.joined = joined_plan(rows, segments, plan.splits) && product_part(rows, n, 1) <= work_bytes;
     p.splits = p.joined ? fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); }) : 1;
     if (p.joined && p.splits == 1 && !segments) p.joined = false;
     if (p.joined) {
-        p.part = reinterpret_cast<float *>(at);
-        at += product_part(rows, n, p.splits);
+        p.part = static_cast<float *>(scratch.take(product_part(rows, n, p.splits)));
     } else if (segments && pack_part(rows, kmax) <= work_bytes) {
-        p.pack = at;
-        at += pack_part(rows, kmax);
-        p.row_scale = reinterpret_cast<float *>(at) - up4(rows);
+        p.pack = scratch.take(pack_part(rows, kmax));
+        p.row_scale = reinterpret_cast<float *>(static_cast<char *>(p.pack) + pack_part(rows, kmax)) - up4(rows);
     }
     p.k_split = ceil_div(ceil_div(m, stage), p.splits) * stage;
     if (segments) {
         // parts of u are added up by the launch that joins y or that packs u
         if (p.joined || p.pack)
-            p.shrink_splits = fit(shrink_plan(type, rows, segments, m, kmax), end - at, [&](int s) { return shrink_part(rows, kmax, s); });
+            p.shrink_splits = fit(shrink_plan(type, rows, segments, m, kmax), scratch.left, [&](int s) { return shrink_part(rows, kmax, s); });
         p.shrink_k = ceil_div(ceil_div(m, stage), p.shrink_splits) * stage;
-        p.upart = reinterpret_cast<float *>(at);
+        if (p.shrink_splits > 1) p.upart = static_cast<float *>(scratch.take(shrink_part(rows, kmax, p.shrink_splits)));
     }
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
     const int64_t shrink = segments ? (ceil_div(rows, kShrinkRows) + segments) * ceil_div(kmax, kShrinkCols) * p.shrink_splits : 0;
     if ((rc = check_grid(std::max(product_grid(p) + shrink, p.joined ? rows * ceil_div(n, 256) : 0)))) return rc;
+    Matrix x = {X, ldx, 0, rows, m, 1}, b = {A, lda, 0, transposed ? n : m, transposed ? m : n, 1};
+    Matrix w = {Wt, m, 0, ktotal, m, 1}, h = {H, n, 0, ktotal, n, 1};
+    Matrix *const operands[] = {&x, &b, &w, &h};
+    if ((rc = align_all(type, operands, segments ? 4 : 2, 2.0 * rows * m * n, &scratch, static_cast<hipStream_t>(stream), &p.padded))) return rc;
+    p.x = x.p; p.ldx = x.ld;
+    p.b = b.p; p.ldb = b.ld;
+    p.ad.down = w.p; p.ad.ld_down = w.ld;
+    p.ad.up = h.p; p.ad.ld_up = h.ld;
     return launched(type, p, stream, launch_product<float>, launch_product<bf16_t>, launch_product<f16_t>);
 }
 
@@ -264,7 +374,7 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     if (rows == 0) segments = 0;
     FactorGradient p = {};
     p.x = X; p.dy = dY; p.ldx = ldx; p.ldy = ldy; p.rows = rows; p.m = m; p.n = n;
-    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, nullptr, nullptr, nullptr, nullptr};
+    p.ad = Adapters{offsets, run, segments, koff, runs, kmax, ktotal, nullptr, nullptr, 0, 0, nullptr, nullptr};
     p.u = U; p.v = V; p.ddown = dWt; p.dup = dH;
     const FactorPlan plan = factor_plan(type, rows, segments, runs, m, n, kmax);
     p.chunk = plan.chunk;
@@ -286,15 +396,17 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
     case 0: {
         if (parts < 1) return 0;
         const int splits = product_plan(type, rows, parts, m, n).splits;
-        return splits > 1 ? product_part(rows, n, splits) : 0;
+        return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0);
     }
-    case 1: return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits);
+    case 1:
+        return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n);
     case 2: {
-        if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K) return 0;
+        if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 0 || ktotal > kMost) return 0;
         const int splits = product_plan(type, rows, 1, m, n).splits;
-        if (parts == 0) return splits > 1 ? product_part(rows, n, splits) : 0;
+        const size_t copies = product_copies(type, rows, 1, m, n, ktotal);
+        if (parts == 0) return (splits > 1 ? product_part(rows, n, splits) : 0) + copies;
         return (joined_plan(rows, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
-               shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax));
+               shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax)) + copies;
     }
     case 3:
         if (parts < 1 || runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;

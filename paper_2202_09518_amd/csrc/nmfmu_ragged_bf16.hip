@@ -3,6 +3,7 @@
 
 namespace nmfmu {
 namespace ragged {
+template hipError_t launch_align<bf16_t>(const Align &, hipStream_t);
 template hipError_t launch_product<bf16_t>(const Product &, hipStream_t);
 template hipError_t launch_gradient<bf16_t>(const Gradient &, hipStream_t);
 template hipError_t launch_factor_gradient<bf16_t>(const FactorGradient &, hipStream_t);

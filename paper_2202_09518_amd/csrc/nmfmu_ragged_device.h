@@ -118,7 +118,8 @@ struct Operand {
     int64_t plane = 0;       // operands in two planes: bytes from the first to the second
 };
 
-// 16 bytes of which only those before `bytes` may be read; the others are zero.
+// 16 bytes of which only those before `bytes` may be read; the others are zero.  (Loads on any border are as fast as they
+// would be from the aligned words around them.)
 template <class T> __device__ __forceinline__ u32x4 chunk_at(const char *at, int64_t bytes)
 {
     u32x4 v = {0, 0, 0, 0};
@@ -522,8 +523,9 @@ template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, 
                 const int in = up + r * kAtOnce, row = first + 16 * WM * (i + in / 16) + in % 16;
                 if (row >= rows) continue;
                 O *at = out + (int64_t)row * ld + col;
-                if (vec && have == N) {
-                    *reinterpret_cast<u32x4 *>(at) = w[r];
+                if (have == N) {
+                    if (vec) *reinterpret_cast<u32x4 *>(at) = w[r];
+                    else __builtin_memcpy(at, &w[r], 16);
                 } else {
 #pragma unroll
                     for (int e = 0; e < N; ++e)

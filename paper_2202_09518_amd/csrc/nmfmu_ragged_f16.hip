@@ -3,6 +3,7 @@
 
 namespace nmfmu {
 namespace ragged {
+template hipError_t launch_align<f16_t>(const Align &, hipStream_t);
 template hipError_t launch_product<f16_t>(const Product &, hipStream_t);
 template hipError_t launch_gradient<f16_t>(const Gradient &, hipStream_t);
 template hipError_t launch_factor_gradient<f16_t>(const FactorGradient &, hipStream_t);

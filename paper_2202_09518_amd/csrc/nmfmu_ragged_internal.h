@@ -24,6 +24,7 @@ struct Adapters {
     int32_t runs, kmax;
     int64_t ktotal;              // rows of down and up
     const void *down, *up;       // ktotal x m and ktotal x n
+    int64_t ld_down, ld_up;
     const float *scale;          // runs, or null
     float *u;                    // rows x kmax
 };
@@ -41,6 +42,7 @@ struct Product {
     int64_t ldy;
     Adapters ad;                 // ad.segments == 0: none
     // plan
+    bool padded;                 // operands whose rows do not fill whole 16 bytes are copies that do, with zeros
     int shape, splits;
     bool joined;                 // y comes from parts (one at least), which a second launch joins; needs part
     int64_t k_split;             // k of a split, whole stages
@@ -61,6 +63,7 @@ struct Gradient {
     int64_t rows, m, n;
     void *g;
     int64_t ldg, stride_g;
+    bool padded;                 // as for Product
     int shape, splits;
     float *part;                 // splits x groups x m x (n rounded up to 4)
     bool vec;
@@ -84,6 +87,14 @@ inline int factor_tile(int kmax) { return kmax <= 32 ? 32 : 64; }
 struct bf16_t { unsigned short bits; };
 struct f16_t { unsigned short bits; };
 
+// A copy with rows of ldo entries, whole 16 bytes.
+struct Align {
+    const void *src;
+    int64_t ld, stride, rows, cols, count;
+    void *dst;
+    int64_t ldo;
+};
+template <class T> hipError_t launch_align(const Align &a, hipStream_t st);
 template <class T> hipError_t launch_product(const Product &p, hipStream_t st);
 template <class T> hipError_t launch_gradient(const Gradient &p, hipStream_t st);
 template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hipStream_t st);

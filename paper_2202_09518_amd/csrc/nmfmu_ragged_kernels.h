@@ -173,12 +173,12 @@ __device__ __forceinline__ void add_plainly(const Product &a, int64_t r0, int64_
         if (hi <= lo || hi <= r0) continue;
         bool use = !packed;
         for (int k = 0; k < run.k; ++k) {
-            const T *h = (const T *)a.ad.up + (int64_t)(run.ko + k) * a.n;
+            const T *h = (const T *)a.ad.up + (int64_t)(run.ko + k) * a.ad.ld_up;
             if (packed && k % group == 0) {
                 bool bad = false;
                 for (int64_t q = threadIdx.x; q < (int64_t)group * C::BN; q += C::THREADS) {
                     const int64_t kk = k + q / C::BN, col = c0 + q % C::BN;
-                    if (kk < run.k && col < a.n) bad |= !__builtin_isfinite(Type<T>::load(h[q / C::BN * a.n + col]));
+                    if (kk < run.k && col < a.n) bad |= !__builtin_isfinite(Type<T>::load(h[q / C::BN * a.ad.ld_up + col]));
                 }
                 use = __syncthreads_or(bad);
             }
@@ -255,7 +255,7 @@ __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t
         Operand P = operand<T>(a.pack, r0 * row_n, row_n, (hi < r1 ? hi : r1) - r0, (a.rows - r0) * row_n);
         P.first = (int)((lo > r0 ? lo : r0) - r0);
         P.plane = kp * (int)sizeof(T);
-        const Operand Q = operand<T>(a.ad.up, (int64_t)run.ko * a.n + c0, a.n, a.n - c0, (a.ad.ktotal - run.ko) * a.n - c0);
+        const Operand Q = operand<T>(a.ad.up, run.ko * a.ad.ld_up + c0, a.ad.ld_up, a.n - c0, (a.ad.ktotal - 1 - run.ko) * a.ad.ld_up + a.n - c0);
         typename X::LoadP lp;
         typename X::LoadQ lq;
         lp.open(P);
@@ -320,7 +320,7 @@ template <class C> __device__ __forceinline__ void shrink_tile(const Product &a,
     const int c0 = id % ct * C::BN;
     if (c0 >= run.k) return;
     const Operand P = operand<T>(a.x, f.r0 * a.ldx, a.ldx, f.r1 - f.r0, (a.rows - 1 - f.r0) * a.ldx + a.m);
-    const Operand Q = operand<T>(a.ad.down, (run.ko + c0) * a.m, a.m, run.k - c0, (a.ad.ktotal - run.ko - c0) * a.m);
+    const Operand Q = operand<T>(a.ad.down, (run.ko + c0) * a.ad.ld_down, a.ad.ld_down, run.k - c0, (a.ad.ktotal - 1 - run.ko - c0) * a.ad.ld_down + a.m);
     const int64_t k0 = split * a.shrink_k, k1 = k0 + a.shrink_k < a.m ? k0 + a.shrink_k : a.m;
     typename C::Acc acc;
     C::clear(acc);
@@ -436,13 +436,13 @@ template <class T> __global__ __launch_bounds__(256) void join_product_kernel(Pr
             us[k] = u;
         }
         __syncthreads();
-        const T *h = (const T *)a.ad.up + (int64_t)run.ko * a.n;
+        const T *h = (const T *)a.ad.up + run.ko * a.ad.ld_up;
         for (int k0 = w; k0 < run.k; k0 += 16) {
             float x[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = k0 + 4 * i < run.k ? k0 + 4 * i : run.k - 1;
-                const T *line = h + (int64_t)k * a.n;
+                const T *line = h + k * a.ad.ld_up;
                 if (col + 4 <= a.n) {
                     T four[4];
                     __builtin_memcpy(four, line + col, sizeof(four));
@@ -759,6 +759,29 @@ template <class T, int BM> __global__ __launch_bounds__(256) void join_factors_k
 
 // ---- launches --------------------------------------------------------------------------
 
+// `count` matrices of rows x cols to rows of ldo entries (whole 16 bytes), zero behind their ends: operands whose rows do not
+// begin and end on 16 bytes.
+template <class T>
+__global__ __launch_bounds__(256) void align_kernel(const char *src, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t count, char *dst,
+                                                    int64_t ldo)
+{
+    constexpr int E = chunk_n<T>();
+    const int64_t per = ldo / E, all = count * rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t line = i / per, c = (i - line * per) * E, g = line / rows, r = line - g * rows;
+        const int64_t e = g * stride + r * ld + c;
+        const int64_t end = (count - 1) * stride + (rows - 1) * ld + cols;
+        *reinterpret_cast<u32x4 *>(dst + i * 16) = keep_first<T>(chunk_at<T>(src + e * (int64_t)sizeof(T), (end - e) * (int64_t)sizeof(T)), cols - c);
+    }
+}
+template <class T> hipError_t launch_align(const Align &a, hipStream_t st)
+{
+    const int64_t chunks = a.count * a.rows * (a.ldo / chunk_n<T>()), blocks = (chunks + 255) / 256;
+    hipLaunchKernelGGL((align_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, (const char *)a.src, a.ld, a.stride,
+                       a.rows, a.cols, a.count, (char *)a.dst, a.ldo);
+    return hipGetLastError();
+}
+
 template <class T, bool QRC, bool DMA> void launch_shape(const Product &p, int shrink, hipStream_t st)
 {
     using S = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, DMA>;
@@ -784,9 +807,10 @@ template <class T> hipError_t launch_product(const Product &p, hipStream_t st)
 {
     constexpr int E = sizeof(T);
     const int64_t far = (int64_t)1 << 30;
-    bool dma = by16(p.x, p.ldx * E, p.m * E) && by16(p.b, p.ldb * E, p.stride_b * E) && p.ldx * E * 256 < far && p.ldb * E * 256 < far;
-    if (p.transposed == 0) dma = dma && p.n * E % 16 == 0;
-    if (p.ad.segments) dma = dma && by16(p.ad.down) && by16(p.ad.up, p.n * E);
+    const bool whole_m = p.padded || p.m * E % 16 == 0, whole_n = p.padded || p.n * E % 16 == 0;       // rows fill their 16 bytes
+    bool dma = whole_m && by16(p.x, p.ldx * E) && by16(p.b, p.ldb * E, p.stride_b * E) && p.ldx * E * 256 < far && p.ldb * E * 256 < far;
+    if (p.transposed == 0) dma = dma && whole_n;
+    if (p.ad.segments) dma = dma && whole_n && by16(p.ad.down, p.ad.ld_down * E) && by16(p.ad.up, p.ad.ld_up * E);
     using ShrinkDma = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, true>;
     using Shrink = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, false>;
     int shrink = 0;
@@ -823,7 +847,8 @@ template <class T> hipError_t launch_gradient(const Gradient &p, hipStream_t st)
 {
     constexpr int E = sizeof(T);
     const int64_t far = (int64_t)1 << 30;
-    const bool dma = by16(p.x, p.ldx * E, p.m * E) && by16(p.dy, p.ldy * E, p.n * E) && p.ldx * E * 64 < far && p.ldy * E * 64 < far;
+    const bool dma = by16(p.x, p.ldx * E) && by16(p.dy, p.ldy * E) && (p.padded || ((p.m | p.n) * E % 16 == 0)) && p.ldx * E * 64 < far &&
+                     p.ldy * E * 64 < far;
     auto go = [&](auto tile) {
         using C = decltype(tile);
         const int64_t tiles = ((p.m + C::BM - 1) / C::BM * ((p.n + C::BN - 1) / C::BN) * p.splits + 7) / 8 * 8 * p.groups;
