@@ -16,10 +16,12 @@
  * Conventions, where they differ from nmfmu.h or add to it
  *   - `type` says what X, Y, A, B, W, H and their gradients hold: NMF_F32, NMF_BF16 or NMF_F16.  Products
  *     are summed in fp32 and rounded once when they are written; U and V are floats.  Floats meet the fp32
- *     matrix instruction; halves and bf16 are exact operands of theirs; where U or V meets factors in 16
- *     bits it goes as two bf16 pieces (16 bits of it).
+ *     matrix instruction; halves and bf16 are exact operands of theirs; where U or V meets them it goes as two
+ *     pieces (16 bits of it and more; to f16 factors under a scale of its row).
  *   - Matrices are row-major; `ld...` is the distance of two rows in entries, at least the row's length.
- *     Base pointers are aligned to an entry.  Rows on 16-byte borders take the faster kernels.
+ *     Base pointers are aligned to an entry.  Operands whose rows do not begin and end on 16-byte borders are
+ *     copied into rows that do, once per call and in its scratch, where the product is long enough, or take
+ *     slower kernels.
  *   - offsets: device, int64[groups + 1] (segments + 1), non-decreasing; range g is rows offsets[g] to
  *     offsets[g + 1] - 1, which may be none.  It is read by the kernels, not by the host.  Values are held
  *     inside [0, rows] where they are used: malformed offsets, runs or koff give a meaningless result but no
@@ -28,8 +30,9 @@
  *   - Results may not overlap operands.  All calls are asynchronous on `stream`, allocate nothing, and
  *     share nothing: they may be made on several streams at once and captured into graphs.
  *   - work: device scratch of the call alone, 16-byte aligned, nmf_ragged_work_bytes(...) bytes for the
- *     plan that is fastest; with less (also NULL, 0) the call uses a plan that fits.  It must stay valid until
- *     the work is done.
+ *     plan that is fastest; with less (also NULL, 0) the call uses a plan that fits (nmf_lowrank_product with
+ *     long segments then adds their adapters by plain sums, much slower).  It must stay valid until the work
+ *     is done.
  *   - Sizes below 2^31.  rows == 0 is a successful no-op (gradients are then zeros).
  */
 #ifndef NMFMU_RAGGED_H
