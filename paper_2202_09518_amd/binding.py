@@ -370,10 +370,11 @@ def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, like, stream):
     need = _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
     if need == 0:
         return None, 0, None
-    buf = torch.empty(need, dtype=torch.uint8, device=like.device)
-    if stream is not None:
-        on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
-        buf.record_stream(on)
+    if stream is None:
+        buf = torch.empty(need, dtype=torch.uint8, device=like.device)
+    else:                                   # memory that is free in the order of the call's stream
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+            buf = torch.empty(need, dtype=torch.uint8, device=like.device)
     return buf.data_ptr(), need, buf
 
 

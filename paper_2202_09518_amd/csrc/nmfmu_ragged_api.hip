@@ -12,6 +12,7 @@ using namespace nmfmu::ragged;
 namespace {
 
 constexpr int64_t kMost = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 23) - 1;      // of up to 512: a launch has fewer than 2^32 threads
 constexpr int kComputeUnits = 256;
 
 int bytes_of(int32_t type) { return type == NMF_F32 ? 4 : 2; }
@@ -90,7 +91,10 @@ int shrink_plan(int32_t type, int64_t rows, int64_t segments, int64_t m, int kma
 
 // A tile runs its segments' adapters one after the other, 2.5 us each; where segments are short, the launch that joins parts
 // adds the adapters row by row, for the price of the product's floats written and read once (26 us for a tile of 256 x 256).
-bool joined_plan(int64_t rows, int64_t segments, int splits) { return splits > 1 || rows < 24 * segments; }
+bool joined_plan(int64_t rows, int64_t n, int64_t segments, int splits)
+{
+    return splits > 1 || (rows < 24 * segments && rows * ceil_div(n, 256) <= kMostWorkgroups);
+}
 
 // Blocks of rows to a workgroup, and chunks of so many: about four workgroups for each compute unit, at least four blocks each.
 struct FactorPlan {
@@ -216,7 +220,7 @@ int check_work(const void *work, size_t bytes)
 
 int check_grid(int64_t workgroups)
 {
-    return workgroups <= kMost ? NMF_OK : set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
+    return workgroups <= kMostWorkgroups ? NMF_OK : set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
 }
 
 int64_t product_grid(const Product &p)
@@ -323,7 +327,7 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
     p.shrink_splits = 1;
     const int stage = stage_of(type);
     Scratch scratch = {static_cast<char *>(work), work_bytes};
-    p.joined = joined_plan(rows, segments, plan.splits) && product_part(rows, n, 1) <= work_bytes;
+    p.joined = joined_plan(rows, n, segments, plan.splits) && product_part(rows, n, 1) <= work_bytes;
     p.splits = p.joined ? fit(plan.splits, work_bytes, [&](int s) { return product_part(rows, n, s); }) : 1;
     if (p.joined && p.splits == 1 && !segments) p.joined = false;
     if (p.joined) {
@@ -342,7 +346,7 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
     }
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
     const int64_t shrink = segments ? (ceil_div(rows, kShrinkRows) + segments) * ceil_div(kmax, kShrinkCols) * p.shrink_splits : 0;
-    if ((rc = check_grid(std::max(product_grid(p) + shrink, p.joined ? rows * ceil_div(n, 256) : 0)))) return rc;
+    if ((rc = check_grid(std::max(product_grid(p) + shrink, p.joined ? rows * ceil_div(n, 256) : ceil_div(rows, 16))))) return rc;
     Matrix x = {X, ldx, 0, rows, m, 1}, b = {A, lda, 0, transposed ? n : m, transposed ? m : n, 1};
     Matrix w = {Wt, m, 0, ktotal, m, 1}, h = {H, n, 0, ktotal, n, 1};
     Matrix *const operands[] = {&x, &b, &w, &h};
@@ -384,7 +388,8 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
         p.chunk = 1 << 30;
         p.chunks = runs;
     }
-    if (p.chunks > 65535 || (int64_t)runs * kmax > 65535) return set_error(NMF_EUNSUPPORTED, "more runs than one launch can have");
+    if (p.chunks > 65535 || ceil_div(up4(m) + up4(n), 1024) > 65535 || (rc = check_grid((int64_t)runs * kmax)))
+        return set_error(NMF_EUNSUPPORTED, "more runs or columns than one launch can have");
     return launched(type, p, stream, launch_factor_gradient<float>, launch_factor_gradient<bf16_t>, launch_factor_gradient<f16_t>);
 }
 
@@ -405,7 +410,7 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
         const int splits = product_plan(type, rows, 1, m, n).splits;
         const size_t copies = product_copies(type, rows, 1, m, n, ktotal);
         if (parts == 0) return (splits > 1 ? product_part(rows, n, splits) : 0) + copies;
-        return (joined_plan(rows, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
+        return (joined_plan(rows, n, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
                shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax)) + copies;
     }
     case 3:

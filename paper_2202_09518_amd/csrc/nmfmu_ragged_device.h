@@ -601,7 +601,7 @@ struct Ranges {
                 const int64_t l0 = lane_value(lo, l), h0 = lane_value(hi, l);
                 f.r0 = l0 + (int64_t)(want - before) * BM;
                 f.r1 = h0 < f.r0 + BM ? h0 : f.r0 + BM;
-                return true;
+                return f.r0 >= l0 && f.r0 < h0;        // (counts of malformed ranges can overflow)
             }
             want -= __builtin_amdgcn_readlane(sum, 63);
             if (base + 64 >= groups) return false;

@@ -345,7 +345,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void shrink_kernel(P
 template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREADS) void product_kernel(Product a, int shrink)
 {
     using T = typename C::T;
-    constexpr bool both = ADAPTERS && S::THREADS == C::THREADS;
+    constexpr bool both = ADAPTERS && S::THREADS == C::THREADS;      // else shrink is 0
     __shared__ __align__(1024) char lds[both && S::kLds > C::kLds ? S::kLds : C::kLds];
     if constexpr (both) {
         if ((int)blockIdx.x < shrink) {
@@ -742,17 +742,17 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     }
 }
 
-// The gradients of runs with several chunks: factor y of a run, 1024 columns of m and n side by side.
+// The gradients of runs with several chunks: one factor of a run, 1024 columns of m and n side by side.
 template <class T, int BM> __global__ __launch_bounds__(256) void join_factors_kernel(FactorGradient a, int padded)
 {
     constexpr int SK = stage_k<typename Cut<T>::E>();
-    const int id = blockIdx.y / a.ad.kmax, k = blockIdx.y % a.ad.kmax;
+    const int id = blockIdx.x / a.ad.kmax, k = blockIdx.x % a.ad.kmax;
     const int64_t lo = a.ad.koff[id], hi = a.ad.koff[id + 1];
     if (lo < 0 || lo + k >= hi || lo + k >= a.ad.ktotal) return;
     Chunks f;
     if (!find_chunk<true>(a, SK, id, f)) return;
     if (f.count < 2) return;
-    const int64_t m4 = up4(a.m), n4 = up4(a.n), at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t m4 = up4(a.m), n4 = up4(a.n), at = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
     if (at >= m4 + n4) return;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     for (int c = 0; c < f.count; ++c) y += *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)(f.first + c) * padded + k) * (m4 + n4) + at);
@@ -817,14 +817,17 @@ template <class T> hipError_t launch_product(const Product &p, hipStream_t st)
     const bool whole_m = p.padded || p.m * E % 16 == 0, whole_n = p.padded || p.n * E % 16 == 0;       // rows fill their 16 bytes
     bool dma = whole_m && by16(p.x, p.ldx * E) && by16(p.b, p.ldb * E, p.stride_b * E) && p.ldx * E * 256 < far && p.ldb * E * 256 < far;
     if (p.transposed == 0) dma = dma && whole_n;
-    if (p.ad.segments) dma = dma && whole_n && by16(p.ad.down, p.ad.ld_down * E) && by16(p.ad.up, p.ad.ld_up * E);
+    if (p.ad.segments)
+        dma = dma && whole_n && by16(p.ad.down, p.ad.ld_down * E) && by16(p.ad.up, p.ad.ld_up * E) && p.ad.ld_down * E * 256 < far &&
+              p.ad.ld_up * E * 256 < far;
     using ShrinkDma = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, true>;
     using Shrink = Tile<T, kShrinkRows, kShrinkCols, 2, 2, 4, false, false, false>;
     int shrink = 0;
     if (p.ad.segments) {
         const int64_t rt = (p.rows + kShrinkRows - 1) / kShrinkRows + p.ad.segments, ct = (p.ad.kmax + kShrinkCols - 1) / kShrinkCols;
         shrink = (int)(rt * ct * p.shrink_splits);
-        if (!p.joined) {
+        // its tiles run in the product's launch where that has workgroups of their size and nothing waits for u there
+        if (!p.joined || p.shape == k256x256) {
             if (dma) hipLaunchKernelGGL((shrink_kernel<ShrinkDma>), dim3(shrink), dim3(ShrinkDma::THREADS), 0, st, p);
             else hipLaunchKernelGGL((shrink_kernel<Shrink>), dim3(shrink), dim3(Shrink::THREADS), 0, st, p);
             shrink = 0;
@@ -884,7 +887,7 @@ template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hi
         const unsigned kt = (unsigned)((p.ad.kmax + BM - 1) / BM);
         hipLaunchKernelGGL((factor_gradient_kernel<T, BM>), dim3(cols, kt, (unsigned)p.chunks), dim3(256), 0, st, p);
         if (p.chunks > p.ad.runs)
-            hipLaunchKernelGGL((join_factors_kernel<T, BM>), dim3((unsigned)((up4(p.m) + up4(p.n) + 1023) / 1024), (unsigned)(p.ad.runs * p.ad.kmax)),
+            hipLaunchKernelGGL((join_factors_kernel<T, BM>), dim3((unsigned)(p.ad.runs * p.ad.kmax), (unsigned)((up4(p.m) + up4(p.n) + 1023) / 1024)),
                                dim3(256), 0, st, p, (int)kt * BM);
     };
     if (p.ad.kmax <= 32) go(std::integral_constant<int, 32>{});

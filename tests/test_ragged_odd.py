@@ -106,3 +106,26 @@ def test_range_of_u_in_f16():
         # pieces of u under its row's scale: 2^-22 of the row's largest entry for each of at most six factors; size bounds that
         within(got, torch.where(fits, want, 0.0), size, m + 8, "f16", 2.0 ** -17 * size)
         assert bool(torch.isfinite(Y[fits].float()).all())
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,segments,runs,kmin,kmax,m,n", [
+    (1500, 120, 5, 2, 20, 72, 8192),       # short segments beside a product of large tiles
+    (300, 20, 300, 250, 256, 64, 64),      # more factors than a launch dimension holds
+])
+def test_short_segments_in_large_tiles_and_many_factors(rows, segments, runs, kmin, kmax, m, n, typ):
+    p = Problem(rows, segments, runs, kmin, kmax, m, n, True, typ)
+    X, dY, A = p.X.double(), p.dY.double(), p.A.double().t().contiguous()
+    W, H = p.Wt.double(), p.H.double()
+    Y, dX = torch.empty(rows, n, dtype=TYPES[typ], device="cuda"), torch.empty(rows, m, dtype=TYPES[typ], device="cuda")
+    dWt, dH = torch.full_like(p.Wt, 5.0), torch.full_like(p.H, 5.0)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    p.forward(Y, stream=side)              # scratch of a stream that is not the current one
+    side.synchronize()
+    p.backward(dX, dWt, dH)
+    torch.cuda.synchronize()
+    p.check_product(Y, X, A, W, H, p.U)
+    p.check_product(dX, dY, A.t().contiguous(), H, W, p.V)
+    p.check_gradient(dWt, dH)
