@@ -117,6 +117,11 @@ size_t factor_part(int kmax, int64_t m, int64_t n, int chunks)
     return (size_t)chunks * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * (up4(m) + up4(n)) * 4;
 }
 
+size_t pieces_part(int32_t type, int64_t rows, int kmax)
+{
+    return type == NMF_F32 ? 0 : (size_t)rows * 2 * 2 * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * 2;
+}
+
 // Splits that a scratch of `have` bytes can hold.
 template <class F> int fit(int splits, size_t have, F bytes)
 {
@@ -383,12 +388,14 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     const FactorPlan plan = factor_plan(type, rows, segments, runs, m, n, kmax);
     p.chunk = plan.chunk;
     p.chunks = plan.chunks;
-    p.part = static_cast<float *>(work);
-    if (factor_part(kmax, m, n, p.chunks) > work_bytes) {      // each run in one chunk
+    Scratch scratch = {static_cast<char *>(work), work_bytes};
+    p.part = static_cast<float *>(scratch.take(factor_part(kmax, m, n, p.chunks)));
+    if (!p.part) {                                             // each run in one chunk
         p.chunk = 1 << 30;
         p.chunks = runs;
     }
-    if (p.chunks > 65535 || ceil_div(up4(m) + up4(n), 1024) > 65535 || (rc = check_grid((int64_t)runs * kmax)))
+    if (type != NMF_F32 && segments) p.pieces = scratch.take(pieces_part(type, rows, kmax));
+    if (p.chunks > 65535 || ceil_div(up4(m) + up4(n), 1024) > 65535 || (rc = check_grid(std::max((int64_t)runs * kmax, ceil_div(rows, 16)))))
         return set_error(NMF_EUNSUPPORTED, "more runs or columns than one launch can have");
     return launched(type, p, stream, launch_factor_gradient<float>, launch_factor_gradient<bf16_t>, launch_factor_gradient<f16_t>);
 }
@@ -415,7 +422,7 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
     }
     case 3:
         if (parts < 1 || runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
-        return factor_part(kmax, m, n, factor_plan(type, rows, parts, runs, m, n, kmax).chunks);
+        return factor_part(kmax, m, n, factor_plan(type, rows, parts, runs, m, n, kmax).chunks) + pieces_part(type, rows, kmax);
     }
     return 0;
 }

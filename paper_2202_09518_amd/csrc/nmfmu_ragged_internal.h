@@ -75,6 +75,7 @@ struct FactorGradient {
     Adapters ad;                 // its u, down, up and scale are not used
     const float *u, *v;          // rows x kmax
     void *ddown, *dup;           // ktotal x m, ktotal x n
+    void *pieces;                // 16-bit types: u and v in two pieces, 2 x rows x 2 x (kmax in whole tiles) bf16; null: cut where they are used
     int chunk, chunks;           // blocks of rows (factor_rows) to a workgroup, and how many such chunks there can be
     float *part;                 // chunks x (kmax in whole tiles) x (m rounded up to 4 + n rounded up to 4)
 };

@@ -572,9 +572,28 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
     return false;
 }
 
+// U and V (blockIdx.y) as the two bf16 pieces that the gradients' products take, once for all column tiles: rows x 2 planes x kp
+// entries, kp = kmax in whole tiles, zero behind a run's rank and in rows without a run.  One row per 16 lanes.
+__global__ __launch_bounds__(256) inline void pack_factors_kernel(FactorGradient a, int kp)
+{
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (row >= a.rows) return;
+    Run run = {0, 0};
+    const int s = range_at(a.ad.offsets, a.ad.segments, row);
+    if (s < a.ad.segments && a.ad.offsets[s] <= row) run = run_of(a.ad, s);
+    const float *in = (blockIdx.y ? a.v : a.u) + row * a.ad.kmax;
+    bf16_t *out = (bf16_t *)a.pieces + (blockIdx.y * a.rows + row) * (2 * (int64_t)kp);
+    for (int k = threadIdx.x & 15; k < kp; k += 16) {
+        const float x = k < run.k ? in[k] : 0.f;
+        out[k] = Type<bf16_t>::round(x);
+        out[kp + k] = Type<bf16_t>::round(piece<true>(x));
+    }
+}
+
 // BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (halves) or 32 (floats) at a time.
-// Reads X and dY once; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 65 us (2.1 TB/s), bound by cutting u and v into
-// pieces in each of the 64 column tiles; 4096 rows of 4096 + 2048 floats, ranks to 16: 36 us (2.8 TB/s).
+// Reads X and dY once; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 50 us (2.7 TB/s) on pieces (65 where each column
+// tile cuts them itself), bound by the latency of its loads at two workgroups a compute unit; 4096 rows of 4096 + 2048 floats,
+// ranks to 16: 36 us (2.8 TB/s).
 template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradient_kernel(FactorGradient a)
 {
     using E = typename Cut<T>::E;
@@ -591,6 +610,8 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     const char *src = (const char *)(down ? a.x : a.dy);
     const int64_t ld = down ? a.ldx : a.ldy;
     const float *fac = down ? a.v : a.u;
+    const int kp = gridDim.y * BM;
+    [[maybe_unused]] const bf16_t *pieces = a.pieces ? (const bf16_t *)a.pieces + (down ? a.rows * 2 * (int64_t)kp : 0) : nullptr;
     const int f0 = blockIdx.y * BM, z = blockIdx.z;
     Chunks mychunk;
     if (!find_chunk(a, SK, z, mychunk)) return;
@@ -659,6 +680,14 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 #pragma unroll
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
+            if constexpr (both) {
+                if (pieces) {
+                    const bf16_t *line = pieces + (r + (kr < left ? kr : 0)) * (2 * (int64_t)kp) + f0 + c * EN;
+                    ph[j] = kr < left ? *reinterpret_cast<const u32x4 *>(line) : u32x4{0, 0, 0, 0};
+                    pl[j] = kr < left ? *reinterpret_cast<const u32x4 *>(line + kp) : u32x4{0, 0, 0, 0};
+                    continue;
+                }
+            }
             float x[EN];
             floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, a.ad.kmax, x);
             if constexpr (both) cut_chunk(x, ph[j], pl[j]);
@@ -885,6 +914,7 @@ template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hi
     auto go = [&](auto bm) {
         constexpr int BM = bm.value;
         const unsigned kt = (unsigned)((p.ad.kmax + BM - 1) / BM);
+        if (p.pieces) hipLaunchKernelGGL(pack_factors_kernel, dim3((unsigned)((p.rows + 15) / 16), 2), dim3(256), 0, st, p, (int)kt * BM);
         hipLaunchKernelGGL((factor_gradient_kernel<T, BM>), dim3(cols, kt, (unsigned)p.chunks), dim3(256), 0, st, p);
         if (p.chunks > p.ad.runs)
             hipLaunchKernelGGL((join_factors_kernel<T, BM>), dim3((unsigned)(p.ad.runs * p.ad.kmax), (unsigned)((up4(p.m) + up4(p.n) + 1023) / 1024)),
