@@ -232,9 +232,10 @@ __device__ __forceinline__ void add_rest(const Product &a, int64_t r0, int64_t r
     }
 }
 
-// acc (cleared) += s_r x W_r H_r from the packed u, segment by segment, 64 factors at a time in two stages: the tile's
-// product with H_r, in which the rows of other segments are zeros.  H is looked at first; what has entries that are not
-// finite is left out.  (A row of u that is not finite is a row of the result.)  Returns whether something was.
+// acc (cleared) += s_r x W_r H_r from the packed u, segment by segment, a stage of factors at a time, while the next one is
+// on its way: the tile's product with H_r, in which the rows of other segments are zeros.  H is looked at first; what has
+// entries that are not finite is left out.  (A row of u that is not finite is a row of the result.)  Returns whether
+// something was.
 template <class C, class X>
 __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t r1, int64_t c0, char *lds, typename C::Acc &acc)
 {
@@ -246,49 +247,62 @@ __device__ __forceinline__ bool add_packed(const Product &a, int64_t r0, int64_t
     typename X::ReadQ rq;
     rp.open(X::wave_row());
     rq.open(X::wave_col());
-    for (int s = first_range(a.ad.offsets, a.ad.segments, r0); s < a.ad.segments; ++s) {
-        int64_t lo, hi;
-        range_of(a.ad.offsets, s, a.rows, lo, hi);
-        if (lo >= r1) break;
-        const Run run = run_of(a.ad, s);
-        if (run.k == 0 || hi <= lo || hi <= r0) continue;
-        Operand P = operand<T>(a.pack, r0 * row_n, row_n, (hi < r1 ? hi : r1) - r0, (a.rows - r0) * row_n);
-        P.first = (int)((lo > r0 ? lo : r0) - r0);
-        P.plane = kp * (int)sizeof(T);
-        const Operand Q = operand<T>(a.ad.up, run.ko * a.ad.ld_up + c0, a.ad.ld_up, a.n - c0, (a.ad.ktotal - 1 - run.ko) * a.ad.ld_up + a.n - c0);
-        typename X::LoadP lp;
-        typename X::LoadQ lq;
-        lp.open(P);
-        lq.open(Q);
-        for (int k = 0; k < run.k; k += 2 * X::SK) {
-            bool bad = false;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                char *stage = lds + h * X::kLdsStage;
-                lp.fetch(k + h * X::SK, run.k, stage);
-                lq.fetch(k + h * X::SK, run.k, stage + X::kLdsP);
-                if constexpr (!X::DMA) {
-                    lp.put(stage);
-                    lq.put(stage + X::kLdsP);
-                }
-            }
-            wait_loads<0>();
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < X::LoadQ::kJobs; ++j)      // a thread looks at the chunks that it brought
-                    bad |= !all_finite<T>(*reinterpret_cast<const u32x4 *>(lds + h * X::kLdsStage + X::kLdsP + (threadIdx.x + j * X::THREADS) * 16));
-            bad = __syncthreads_or(bad);
-            left_out |= bad;
-            const int stages = bad ? 0 : (k + X::SK < run.k ? 2 : 1);
-            for (int h = 0; h < stages; ++h) {
-                const char *stage = lds + h * X::kLdsStage;
-                // floats: a matrix step without factors is left out, it takes long
-                if (sizeof(T) == 4 && run.k - k - h * X::SK <= X::SK / 2) X::first_step(stage, rp, rq, acc);
-                else X::step(stage, rp, rq, acc, [](int) {});
-            }
-            meet();
+    typename X::LoadP lp;
+    typename X::LoadQ lq;
+    int s = first_range(a.ad.offsets, a.ad.segments, r0) - 1, k = 0;
+    Run run = {0, 0};
+    // the next stage: of the run at hand, or of the next segment that has one
+    auto advance = [&]() {
+        k += X::SK;
+        while (k >= run.k) {
+            if (++s >= a.ad.segments) return false;
+            int64_t lo, hi;
+            range_of(a.ad.offsets, s, a.rows, lo, hi);
+            if (lo >= r1) return false;
+            run = run_of(a.ad, s);
+            k = 0;
+            if (hi <= lo || hi <= r0) run.k = 0;
+            if (run.k == 0) continue;
+            Operand P = operand<T>(a.pack, r0 * row_n, row_n, (hi < r1 ? hi : r1) - r0, (a.rows - r0) * row_n);
+            P.first = (int)((lo > r0 ? lo : r0) - r0);
+            P.plane = kp * (int)sizeof(T);
+            lp.open(P);
+            lq.open(operand<T>(a.ad.up, run.ko * a.ad.ld_up + c0, a.ad.ld_up, a.n - c0, (a.ad.ktotal - 1 - run.ko) * a.ad.ld_up + a.n - c0));
         }
+        return true;
+    };
+    auto bring = [&](char *stage) {
+        lp.fetch(k, run.k, stage);
+        lq.fetch(k, run.k, stage + X::kLdsP);
+        if constexpr (!X::DMA) {
+            lp.put(stage);
+            lq.put(stage + X::kLdsP);
+        }
+    };
+    bool more = advance();
+    if (more) bring(lds);
+    for (int n = 0; more; ++n) {
+        const char *stage = lds + (n & 1) * X::kLdsStage;
+        [[maybe_unused]] const int left = run.k - k;
+        more = advance();
+        if (more) {
+            bring(lds + (~n & 1) * X::kLdsStage);
+            wait_loads<X::DMA ? X::LoadP::kJobs + X::LoadQ::kJobs : 0>();
+        } else {
+            wait_loads<0>();
+        }
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < X::LoadQ::kJobs; ++j)      // a thread looks at the chunks that it brought
+            bad |= !all_finite<T>(*reinterpret_cast<const u32x4 *>(stage + X::kLdsP + (threadIdx.x + j * X::THREADS) * 16));
+        bad = __syncthreads_or(bad);
+        left_out |= bad;
+        if (!bad) {
+            // floats: a matrix step without factors is left out, it takes long
+            if (sizeof(T) == 4 && left <= X::SK / 2) X::first_step(stage, rp, rq, acc);
+            else X::step(stage, rp, rq, acc, [](int) {});
+        }
+        meet();
     }
     return left_out;
 }
@@ -381,7 +395,7 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
         using X = Tile<T, C::BM, C::BN, C::WM, C::WN, 2, false, true, C::DMA, C::SB, (sizeof(T) == 2 ? 2 : 1)>;
         if (!a.joined) {
             const bool packed = a.pack != nullptr;
-            if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_rest<C>(a, f.r0, f.r1, c0, packed, 2 * X::SK, acc);
+            if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_rest<C>(a, f.r0, f.r1, c0, packed, X::SK, acc);
             if constexpr (std::is_same<T, f16_t>::value)
                 if (packed) unscale<C>(a, f.r0, f.r1, acc);
         }
