@@ -16,8 +16,9 @@
  * Conventions, where they differ from nmfmu.h or add to it
  *   - `type` says what X, Y, A, B, W, H and their gradients hold: NMF_F32, NMF_BF16 or NMF_F16.  Products
  *     are summed in fp32 and rounded once when they are written; U and V are floats.  Floats meet the fp32
- *     matrix instruction; halves and bf16 are exact operands of theirs; where U or V meets them it goes as two
- *     pieces (16 bits of it and more; to f16 factors under a scale of its row).
+ *     matrix instruction; halves and bf16 are exact operands of theirs; where U meets them in the product it goes as two
+ *     pieces (16 bits of it and more; to f16 factors under a scale of its row), in the gradients U and V go as three
+ *     (all 24 bits).
  *   - Matrices are row-major; `ld...` is the distance of two rows in entries, at least the row's length.
  *     Base pointers are aligned to an entry.  Operands whose rows do not begin and end on 16-byte borders are
  *     copied into rows that do, once per call and in its scratch, where the product is long enough, or take

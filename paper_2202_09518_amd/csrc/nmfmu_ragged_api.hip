@@ -119,7 +119,7 @@ size_t factor_part(int kmax, int64_t m, int64_t n, int chunks)
 
 size_t pieces_part(int32_t type, int64_t rows, int kmax)
 {
-    return type == NMF_F32 ? 0 : (size_t)rows * 2 * 2 * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * 2;
+    return type == NMF_F32 ? 0 : (size_t)rows * 2 * kFactorPieces * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * 2;
 }
 
 // Splits that a scratch of `have` bytes can hold.

@@ -14,6 +14,7 @@ enum Shape { k256x256, k128x128, k64x64, k64x128, k32x128 };
 constexpr int kTileRows[] = {256, 128, 64, 64, 32}, kTileCols[] = {256, 128, 64, 128, 128};
 constexpr int kShrinkRows = 64, kShrinkCols = 64;
 constexpr int kMaxSplits = 16, kMaxRank = 256;
+constexpr int kFactorPieces = 3;      // bf16 that hold a float
 
 // Factor pairs of segments of rows.
 struct Adapters {
@@ -75,7 +76,7 @@ struct FactorGradient {
     Adapters ad;                 // its u, down, up and scale are not used
     const float *u, *v;          // rows x kmax
     void *ddown, *dup;           // ktotal x m, ktotal x n
-    void *pieces;                // 16-bit types: u and v in two pieces, 2 x rows x 2 x (kmax in whole tiles) bf16; null: cut where they are used
+    void *pieces;                // 16-bit types: u and v in pieces, 2 x rows x kFactorPieces x (kmax in whole tiles) bf16; null: cut where they are used
     int chunk, chunks;           // blocks of rows (factor_rows) to a workgroup, and how many such chunks there can be
     float *part;                 // chunks x (kmax in whole tiles) x (m rounded up to 4 + n rounded up to 4)
 };

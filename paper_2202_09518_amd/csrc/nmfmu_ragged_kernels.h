@@ -10,40 +10,36 @@ namespace nmfmu {
 namespace ragged {
 
 // ---- float factors on the halves' matrix cores -------------------------------------
-// u = hi + lo, two bf16: 16 to 17 bits of a float, which is 2^-8 of what an output in 16 bits can show.
-template <bool LOW> __device__ __forceinline__ float piece(float x)
+// x = hi + lo + last, N = 3 bf16, is all 24 bits of a float (each piece takes 8 of them; below 2^-110 the last ones are lost),
+// N = 2 all 11 bits of a half.  What is left of x once its piece is taken; nothing of what is not finite.
+__device__ __forceinline__ float after_piece(float x)
 {
-    const float hi = Type<bf16_t>::load(Type<bf16_t>::round(x));
-    if (!LOW) return hi;
-    const float lo = x - hi;
-    return __builtin_isfinite(hi) ? lo : 0.f;
+    const float piece = Type<bf16_t>::load(Type<bf16_t>::round(x));
+    return __builtin_isfinite(piece) ? x - piece : 0.f;
 }
-__device__ __forceinline__ void cut_chunk(const float (&x)[8], u32x4 &hi, u32x4 &lo)
+template <int N> __device__ __forceinline__ void cut_chunk(float (&x)[8], u32x4 (&pieces)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        hi[i] = cvt_pk_bf16(x[2 * i], x[2 * i + 1]);
-        lo[i] = cvt_pk_bf16(piece<true>(x[2 * i]), piece<true>(x[2 * i + 1]));
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pieces[n][i] = cvt_pk_bf16(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = after_piece(x[i]);
     }
 }
-__device__ __forceinline__ void floats_of(u32x4 v, float (&x)[8], f16_t)
+__device__ __forceinline__ void floats_of(u32x4 v, float (&x)[8])      // of halves
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = Type<f16_t>::load(f16_t{(unsigned short)(v[i >> 1] >> (16 * (i & 1)))});
 }
-__device__ __forceinline__ void floats_of(u32x4 v, float (&x)[8], bf16_t)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = Type<bf16_t>::load(bf16_t{(unsigned short)(v[i >> 1] >> (16 * (i & 1)))});
-}
 
 template <class T> struct Cut {                      // the type that float factors are multiplied in
     using E = bf16_t;
-    static constexpr bool kBoth = sizeof(T) == 2;    // float operand in two pieces
+    static constexpr int kPieces = kFactorPieces;           // of a float operand
 };
 template <> struct Cut<float> {
     using E = float;
-    static constexpr bool kBoth = false;
+    static constexpr int kPieces = 1;
 };
 template <class T> constexpr bool two_piece_matrix() { return false; }
 template <> constexpr bool two_piece_matrix<f16_t>() { return true; }      // its 11 bits are two bf16
@@ -586,7 +582,7 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
     return false;
 }
 
-// U and V (blockIdx.y) as the two bf16 pieces that the gradients' products take, once for all column tiles: rows x 2 planes x kp
+// U and V (blockIdx.y) as the three bf16 pieces that the gradients' products take, once for all column tiles: rows x 3 planes x kp
 // entries, kp = kmax in whole tiles, zero behind a run's rank and in rows without a run.  One row per 16 lanes.
 __global__ __launch_bounds__(256) inline void pack_factors_kernel(FactorGradient a, int kp)
 {
@@ -596,26 +592,27 @@ __global__ __launch_bounds__(256) inline void pack_factors_kernel(FactorGradient
     const int s = range_at(a.ad.offsets, a.ad.segments, row);
     if (s < a.ad.segments && a.ad.offsets[s] <= row) run = run_of(a.ad, s);
     const float *in = (blockIdx.y ? a.v : a.u) + row * a.ad.kmax;
-    bf16_t *out = (bf16_t *)a.pieces + (blockIdx.y * a.rows + row) * (2 * (int64_t)kp);
+    bf16_t *out = (bf16_t *)a.pieces + (blockIdx.y * a.rows + row) * (kFactorPieces * (int64_t)kp);
     for (int k = threadIdx.x & 15; k < kp; k += 16) {
-        const float x = k < run.k ? in[k] : 0.f;
-        out[k] = Type<bf16_t>::round(x);
-        out[kp + k] = Type<bf16_t>::round(piece<true>(x));
+        float x = k < run.k ? in[k] : 0.f;
+#pragma unroll
+        for (int n = 0; n < kFactorPieces; ++n, x = after_piece(x)) out[n * kp + k] = Type<bf16_t>::round(x);
     }
 }
 
 // BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (halves) or 32 (floats) at a time.
-// Reads X and dY once; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 50 us (2.7 TB/s) on pieces (65 where each column
+// Reads X and dY once for every BM factors; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 50 us (2.7 TB/s) on pieces (65 where each column
 // tile cuts them itself), bound by the latency of its loads at two workgroups a compute unit; 4096 rows of 4096 + 2048 floats,
 // ranks to 16: 36 us (2.8 TB/s).
 template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradient_kernel(FactorGradient a)
 {
     using E = typename Cut<T>::E;
     constexpr int BN = 128, SK = stage_k<E>();
-    constexpr bool two = two_piece_matrix<T>(), both = Cut<T>::kBoth;
+    constexpr int N = Cut<T>::kPieces;
+    constexpr bool two = two_piece_matrix<T>();
     constexpr int kP = SK * BM * (int)sizeof(E), kQ = SK * BN * (int)sizeof(E);
     constexpr int TM = BM / 16, TN = 2;
-    constexpr int kAllP = kP * (both ? 2 : 1), kStage = kAllP + kQ * (two ? 2 : 1);
+    constexpr int kAllP = kP * N, kStage = kAllP + kQ * (two ? 2 : 1);
     __shared__ __align__(1024) char lds[2 * kStage];
 
     const int mt = (int)((a.m + BN - 1) / BN);
@@ -625,7 +622,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
     const int64_t ld = down ? a.ldx : a.ldy;
     const float *fac = down ? a.v : a.u;
     const int kp = gridDim.y * BM;
-    [[maybe_unused]] const bf16_t *pieces = a.pieces ? (const bf16_t *)a.pieces + (down ? a.rows * 2 * (int64_t)kp : 0) : nullptr;
+    [[maybe_unused]] const bf16_t *pieces = a.pieces ? (const bf16_t *)a.pieces + (down ? a.rows * N * (int64_t)kp : 0) : nullptr;
     const int f0 = blockIdx.y * BM, z = blockIdx.z;
     Chunks mychunk;
     if (!find_chunk(a, SK, z, mychunk)) return;
@@ -679,7 +676,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
             if (turn >= from) return true;
         }
     };
-    u32x4 ph[PJ], pl[PJ], qv[QJ];
+    u32x4 pv[PJ][N], qv[QJ];
     auto get = [&]() {
         const int64_t left = shi - r;
 #pragma unroll
@@ -694,18 +691,18 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 #pragma unroll
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
-            if constexpr (both) {
+            if constexpr (N > 1) {
                 if (pieces) {
-                    const bf16_t *line = pieces + (r + (kr < left ? kr : 0)) * (2 * (int64_t)kp) + f0 + c * EN;
-                    ph[j] = kr < left ? *reinterpret_cast<const u32x4 *>(line) : u32x4{0, 0, 0, 0};
-                    pl[j] = kr < left ? *reinterpret_cast<const u32x4 *>(line + kp) : u32x4{0, 0, 0, 0};
+                    const bf16_t *line = pieces + (r + (kr < left ? kr : 0)) * (N * (int64_t)kp) + f0 + c * EN;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) pv[j][i] = kr < left ? *reinterpret_cast<const u32x4 *>(line + i * kp) : u32x4{0, 0, 0, 0};
                     continue;
                 }
             }
             float x[EN];
             floats_at<EN>(fac + (r + (kr < left ? kr : 0)) * a.ad.kmax, f0 + c * EN, kr < left ? (int)k : 0, a.ad.kmax, x);
-            if constexpr (both) cut_chunk(x, ph[j], pl[j]);
-            else ph[j] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
+            if constexpr (N > 1) cut_chunk(x, pv[j]);
+            else pv[j][0] = __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]});
         }
     };
     auto put = [&](char *to) {
@@ -713,8 +710,8 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
             char *at = to + kr * (BM * (int)sizeof(E)) + ((c ^ rc_shift<E, BM>(kr)) << 4);
-            *reinterpret_cast<u32x4 *>(at) = ph[j];
-            if constexpr (both) *reinterpret_cast<u32x4 *>(at + kP) = pl[j];
+#pragma unroll
+            for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(at + i * kP) = pv[j][i];
         }
 #pragma unroll
         for (int j = 0; j < QJ; ++j) {
@@ -722,11 +719,11 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
             char *at = to + kAllP + kr * (BN * (int)sizeof(E)) + ((c ^ rc_shift<E, BN>(kr)) << 4);
             if constexpr (two) {
                 float x[8];
-                u32x4 h, w;
-                floats_of(qv[j], x, T{});
-                cut_chunk(x, h, w);
-                *reinterpret_cast<u32x4 *>(at) = h;
-                *reinterpret_cast<u32x4 *>(at + kQ) = w;
+                u32x4 two_of[2];
+                floats_of(qv[j], x);
+                cut_chunk(x, two_of);
+                *reinterpret_cast<u32x4 *>(at) = two_of[0];
+                *reinterpret_cast<u32x4 *>(at + kQ) = two_of[1];
             } else {
                 *reinterpret_cast<u32x4 *>(at) = qv[j];
             }
@@ -753,12 +750,17 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
             }
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const u32x4 p = rp.read(lp, i, kk);
-                u32x4 pl2;
-                if constexpr (both) pl2 = rp.read(lp + kP, i, kk);
-                if constexpr (two) mac_row<E>(ql, p, low[i]);
-                if constexpr (both) mac_row<E>(q, pl2, low[i]);
-                mac_row<E>(q, p, acc[i]);
+                // all products of pieces but a half's second with a float's last, below 2^-26 of the whole
+                u32x4 p[N];
+#pragma unroll
+                for (int n = 0; n < N; ++n) p[n] = rp.read(lp + n * kP, i, kk);
+                if constexpr (two) {
+                    mac_row<E>(ql, p[1], low[i]);
+                    mac_row<E>(ql, p[0], low[i]);
+                }
+#pragma unroll
+                for (int n = N - 1; n > 0; --n) mac_row<E>(q, p[n], low[i]);
+                mac_row<E>(q, p[0], acc[i]);
             }
         }
         if (more) put(lds + ((n + 1) & 1) * kStage);
@@ -778,7 +780,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
             for (int v = 0; v < 4; ++v) {
                 const int64_t col = c0 + 32 * wave + 16 * j + 4 * (lane >> 4) + v;
                 if (col >= width) continue;
-                const float x = real ? both_pieces<both>(acc[i][j][v], low[i][j][v]) : 0.f;
+                const float x = real ? both_pieces<(N > 1)>(acc[i][j][v], low[i][j][v]) : 0.f;
                 if (part) part[col] = x;
                 else ((T *)(down ? a.ddown : a.dup))[line * width + col] = Type<T>::round(x);
             }
