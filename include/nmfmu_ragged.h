@@ -17,8 +17,8 @@
  *   - `type` says what X, Y, A, B, W, H and their gradients hold: NMF_F32, NMF_BF16 or NMF_F16.  Products
  *     are summed in fp32 and rounded once when they are written; U and V are floats.  Floats meet the fp32
  *     matrix instruction; halves and bf16 are exact operands of theirs; where U meets them in the product it goes as two
- *     pieces (16 bits of it and more; to f16 factors under a scale of its row), in the gradients U and V go as three
- *     (all 24 bits).
+ *     pieces (bf16: 16 bits of it and more; f16: 22 bits of what is above 2^-17 of the row's largest entry, and no entry is
+ *     off by more than 2^-39 of the largest), in the gradients U and V go as three (all 24 bits).
  *   - Matrices are row-major; `ld...` is the distance of two rows in entries, at least the row's length.
  *     Base pointers are aligned to an entry.  Operands whose rows do not begin and end on 16-byte borders are
  *     copied into rows that do, once per call and in its scratch, where the product is long enough, or take

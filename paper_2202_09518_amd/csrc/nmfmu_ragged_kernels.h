@@ -90,8 +90,11 @@ template <class T> __device__ __forceinline__ Operand operand(const void *base, 
 // ---- adapters in a tile's accumulators --------------------------------------------
 // u as an operand of the matrix instructions: rows of `planes` x kp entries, kp = kmax in whole 32s, zero behind a run's
 // rank and in rows without a run.  Floats: as they are.  Halves and bf16: u = hi + lo in two planes; the products with hi and
-// with lo both run over H's rows.  A half has too small a range for u, so f16 rows are scaled by a power of two that brings
-// their largest entry to [1/2, 1), held to 2^24 at most so that sums stay in range; row_scale undoes it.
+// with lo both run over H's rows.  bf16: 16 bits of u and more, 2^-8 of what an output's last place shows.  A half has too
+// small a range for u, so f16 rows are scaled by a power of two that brings their largest entry to [2^14, 2^15), the top of the
+// range: halves end at 2^-24, so lo is off by up to 2^-25 there, and an entry keeps 22 bits down to 2^-17 of the largest and 16
+// down to 2^-23, as where W's columns and H's rows are scaled against each other; sums of 256 products stay below 2^39.
+// row_scale undoes it.
 // One row per 16 lanes; adds up the parts of u on the way.
 template <class T> __global__ __launch_bounds__(256) void pack_kernel(Product a)
 {
@@ -122,8 +125,7 @@ template <class T> __global__ __launch_bounds__(256) void pack_kernel(Product a)
     if constexpr (sizeof(T) == 2 && !std::is_same<T, bf16_t>::value) {
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
-        int e = half_exponent(__float_as_uint(most)) + 1;
-        e = e < -24 ? -24 : (e > 126 ? 126 : e);
+        const int e = half_exponent(__float_as_uint(most)) - 14;      // -126 to 114
         up = power_of_two(-e);
         if (l == 0) a.row_scale[row] = power_of_two(e);
     }
