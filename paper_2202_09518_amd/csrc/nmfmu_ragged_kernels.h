@@ -544,7 +544,9 @@ __global__ __launch_bounds__(256) void join_kernel(const float *part, int splits
 struct Chunks {
     int run, first, count;       // a run; its first chunk and how many it has
 };
-// Of chunk `want`, or of run `want`.
+// Of chunk `want`, or of run `want`.  Ranges that do not overlap give a.chunks chunks at most; those that do can give any
+// number, so blocks, counts and their sums are held to what the launch has, and chunks beyond a.chunks do not exist.
+constexpr int kMostBlocks = 1 << 28;      // rows / 32 and as many segments as rows, for the rows that a launch takes
 template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const FactorGradient &a, int rows, int want, Chunks &f)
 {
     const int lane = threadIdx.x & 63;
@@ -562,9 +564,11 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
             const int here = a.ad.segments - base < 64 ? a.ad.segments - base : 64;
             for (int i = 0; i < here; ++i)
                 if (__builtin_amdgcn_readlane(of, i) == r0 + lane) blocks += __builtin_amdgcn_readlane(nb, i);
+            if (blocks > kMostBlocks) blocks = kMostBlocks;      // (64 times what one segment can have fits)
         }
         int count = 0;
-        if (r0 + lane < a.ad.runs) count = blocks <= a.chunk ? 1 : (blocks + a.chunk - 1) / a.chunk;
+        if (r0 + lane < a.ad.runs) count = blocks <= a.chunk ? 1 : (blocks - 1) / a.chunk + 1;
+        if (count > a.chunks) count = a.chunks;
         int sum = count;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -577,9 +581,11 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
             f.run = r0 + l;
             f.count = __builtin_amdgcn_readlane(count, l);
             f.first = before + __builtin_amdgcn_readlane(sum, l) - f.count;
-            return true;
+            if (f.count > a.chunks - f.first) f.count = a.chunks - f.first;
+            return f.count > 0;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
+        if (before > a.chunks) before = a.chunks;
     }
     return false;
 }
@@ -775,7 +781,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         const bool real = f0 + row < k;                     // factors beyond kmax take no part: zero
         const int64_t line = klo + f0 + row;
         float *part = nullptr;
-        if (mychunk.count > 1) part = a.part + ((int64_t)z * gridDim.y * BM + f0 + row) * (m4 + n4) + (down ? 0 : m4);
+        if (mychunk.count > 1 && a.part) part = a.part + ((int64_t)z * gridDim.y * BM + f0 + row) * (m4 + n4) + (down ? 0 : m4);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll

@@ -1,0 +1,57 @@
+"""What the products over ragged ranges keep to: their scratch on malformed offsets."""
+import pytest
+import torch
+
+import paper_2202_09518_amd as nmf
+
+gpu = pytest.mark.gpu
+
+
+def overlapping(rows, segments):
+    """Offsets that go back and forth: every second segment has all rows."""
+    return [rows * (i % 2) for i in range(segments + 1)]
+
+
+OVERLAP = dict(rows=4096, segments=64, m=128, n=136, kmax=16)
+
+
+def chunks_planned(typ, block):
+    """Chunks that the scratch has room for, and those that the rows of overlapping segments would fill at the planned length of
+    four blocks each (the least)."""
+    c = OVERLAP
+    line = 32 * (c["m"] + c["n"]) * 4                               # one factor tile of 32, columns of both gradients
+    pieces = 0 if typ == nmf.NMF_F32 else c["rows"] * 2 * 3 * 32 * 2
+    room = (nmf.nmf_ragged_work_bytes(3, typ, c["rows"], c["m"], c["n"], c["segments"], 1, c["kmax"], c["kmax"]) - pieces) // line
+    return room, c["segments"] // 2 * (c["rows"] // block) // 4
+
+
+@pytest.mark.parametrize("typ,block", [(nmf.NMF_F32, 32), (nmf.NMF_BF16, 64), (nmf.NMF_F16, 64)])
+def test_overlapping_segments_would_fill_more_chunks_than_there_are(typ, block):
+    room, filled = chunks_planned(typ, block)
+    assert 1 <= room < filled // 2
+
+
+@gpu
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("runs", [1, 3])
+def test_factor_gradients_of_overlapping_segments_stay_in_their_scratch(runs, dt):
+    """The results mean nothing, but come from the scratch alone (what lies behind it is NaN) and are written to their place."""
+    rows, segments, m, n, kmax = (OVERLAP[k] for k in ("rows", "segments", "m", "n", "kmax"))
+    need = nmf.nmf_ragged_work_bytes(3, nmf.binding._TYPES[dt], rows, m, n, segments, runs, kmax, runs * kmax)
+    mem = torch.full((64 * need // 4,), float("nan"), device="cuda")
+    work = mem.view(torch.uint8)[:need]
+    X, dY = torch.randn(rows, m, device="cuda").to(dt), torch.randn(rows, n, device="cuda").to(dt)
+    U, V = torch.randn(rows, kmax, device="cuda"), torch.randn(rows, kmax, device="cuda")
+    offsets = torch.tensor(overlapping(rows, segments), device="cuda")
+    run = (torch.arange(segments, device="cuda") // 2 % runs).int()
+    koff = (torch.arange(runs + 1, device="cuda") * kmax).int()
+    outs = [torch.full((3 * runs * kmax, cols), 7.0, dtype=dt, device="cuda") for cols in (m, n)]
+    dWt, dH = (o[runs * kmax:2 * runs * kmax] for o in outs)
+    for scratch in (work, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        dWt.zero_(), dH.zero_()
+        nmf.nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work=scratch)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(dWt.float()).all()) and bool(torch.isfinite(dH.float()).all())
+        for o in outs:
+            assert bool((o[:runs * kmax] == 7).all()) and bool((o[2 * runs * kmax:] == 7).all())
+    assert bool(mem[need // 4:].isnan().all())
