@@ -97,24 +97,28 @@ bool joined_plan(int64_t rows, int64_t n, int64_t segments, int splits)
 }
 
 // Blocks of rows to a workgroup, and chunks of so many: about four workgroups for each compute unit, at least four blocks each.
+// A run of one chunk writes its gradients itself; runs with b > chunk blocks have b / chunk chunks, rounded up, which is at most
+// b * 2 / (chunk + 1): so many parts there can be, however many runs there are.
 struct FactorPlan {
-    int chunk, chunks;
+    int chunk, chunks, slots;
 };
 FactorPlan factor_plan(int32_t type, int64_t rows, int64_t segments, int64_t runs, int64_t m, int64_t n, int kmax)
 {
     const int64_t tiles = ceil_div(kmax, factor_tile(kmax)) * (ceil_div(m, 128) + ceil_div(n, 128));
     const int64_t blocks = ceil_div(rows, factor_rows(bytes_of(type))) + std::min(segments, rows);
     const int64_t chunk = std::max<int64_t>(4, ceil_div(blocks, std::max<int64_t>(1, 4 * kComputeUnits / tiles)));
-    return FactorPlan{(int)chunk, (int)(ceil_div(blocks, chunk) + runs)};
+    if (blocks <= chunk) return FactorPlan{(int)chunk, (int)runs, 0};
+    const int64_t chunks = ceil_div(blocks, chunk) + runs;
+    return FactorPlan{(int)chunk, (int)chunks, (int)std::min(chunks, 2 * blocks / (chunk + 1))};
 }
 
 size_t product_part(int64_t rows, int64_t n, int splits) { return (size_t)splits * rows * up4(n) * 4; }
 size_t shrink_part(int64_t rows, int kmax, int splits) { return splits > 1 ? (size_t)splits * up4(rows * kmax) * 4 : 0; }
 size_t pack_part(int64_t rows, int kmax) { return (size_t)rows * (4 * ceil_div(kmax, 32) * 32) + (size_t)up4(rows) * 4; }
 size_t gradient_part(int64_t groups, int64_t m, int64_t n, int splits) { return splits > 1 ? (size_t)splits * groups * m * up4(n) * 4 : 0; }
-size_t factor_part(int kmax, int64_t m, int64_t n, int chunks)
+size_t factor_part(int kmax, int64_t m, int64_t n, int slots)
 {
-    return (size_t)chunks * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * (up4(m) + up4(n)) * 4;
+    return (size_t)slots * ceil_div(kmax, factor_tile(kmax)) * factor_tile(kmax) * (up4(m) + up4(n)) * 4;
 }
 
 size_t pieces_part(int32_t type, int64_t rows, int kmax)
@@ -388,11 +392,12 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
     const FactorPlan plan = factor_plan(type, rows, segments, runs, m, n, kmax);
     p.chunk = plan.chunk;
     p.chunks = plan.chunks;
+    p.slots = plan.slots;
     Scratch scratch = {static_cast<char *>(work), work_bytes};
-    p.part = static_cast<float *>(scratch.take(factor_part(kmax, m, n, p.chunks)));
-    if (!p.part) {                                             // each run in one chunk
+    if (p.slots && !(p.part = static_cast<float *>(scratch.take(factor_part(kmax, m, n, p.slots))))) {      // each run in one chunk
         p.chunk = 1 << 30;
         p.chunks = runs;
+        p.slots = 0;
     }
     if (type != NMF_F32 && segments) p.pieces = scratch.take(pieces_part(type, rows, kmax));
     if (p.chunks > 65535 || ceil_div(up4(m) + up4(n), 1024) > 65535 || (rc = check_grid(std::max((int64_t)runs * kmax, ceil_div(rows, 16)))))
@@ -422,7 +427,7 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
     }
     case 3:
         if (parts < 1 || runs < 1 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 1 || ktotal > kMost) return 0;
-        return factor_part(kmax, m, n, factor_plan(type, rows, parts, runs, m, n, kmax).chunks) + pieces_part(type, rows, kmax);
+        return factor_part(kmax, m, n, factor_plan(type, rows, parts, runs, m, n, kmax).slots) + pieces_part(type, rows, kmax);
     }
     return 0;
 }

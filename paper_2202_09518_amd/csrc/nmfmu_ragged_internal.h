@@ -78,7 +78,8 @@ struct FactorGradient {
     void *ddown, *dup;           // ktotal x m, ktotal x n
     void *pieces;                // 16-bit types: u and v in pieces, 2 x rows x kFactorPieces x (kmax in whole tiles) bf16; null: cut where they are used
     int chunk, chunks;           // blocks of rows (factor_rows) to a workgroup, and how many such chunks there can be
-    float *part;                 // chunks x (kmax in whole tiles) x (m rounded up to 4 + n rounded up to 4)
+    int slots;                   // chunks of runs with several: parts that a second launch joins
+    float *part;                 // slots x (kmax in whole tiles) x (m rounded up to 4 + n rounded up to 4)
 };
 
 // Rows of a block, and factors of a tile.

@@ -543,14 +543,15 @@ __global__ __launch_bounds__(256) void join_kernel(const float *part, int splits
 // rows takes many workgroups and one without rows a single one, which writes its zeros.
 struct Chunks {
     int run, first, count;       // a run; its first chunk and how many it has
+    int slot;                    // of the first one among the parts, which runs with several chunks have
 };
-// Of chunk `want`, or of run `want`.  Ranges that do not overlap give a.chunks chunks at most; those that do can give any
-// number, so blocks, counts and their sums are held to what the launch has, and chunks beyond a.chunks do not exist.
+// Of chunk `want`, or of run `want`.  Ranges that do not overlap give a.chunks chunks and a.slots parts at most; those that do
+// can give any number, so blocks, counts and their sums are held to what the launch has, and chunks beyond do not exist.
 constexpr int kMostBlocks = 1 << 28;      // rows / 32 and as many segments as rows, for the rows that a launch takes
 template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const FactorGradient &a, int rows, int want, Chunks &f)
 {
     const int lane = threadIdx.x & 63;
-    int before = 0;
+    int before = 0, slots = 0;
     for (int r0 = 0; r0 < a.ad.runs; r0 += 64) {
         int blocks = 0;
         for (int base = 0; base < a.ad.segments; base += 64) {
@@ -569,11 +570,11 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
         int count = 0;
         if (r0 + lane < a.ad.runs) count = blocks <= a.chunk ? 1 : (blocks - 1) / a.chunk + 1;
         if (count > a.chunks) count = a.chunks;
-        int sum = count;
+        int sum = count, parts = count > 1 ? count : 0;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
+            const int o = __shfl_up(sum, d), q = __shfl_up(parts, d);
+            if (lane >= d) sum += o, parts += q;
         }
         const unsigned long long past = __ballot(BY_RUN ? r0 + lane == want : before + sum > want);
         if (past) {
@@ -581,11 +582,15 @@ template <bool BY_RUN = false> __device__ __forceinline__ bool find_chunk(const 
             f.run = r0 + l;
             f.count = __builtin_amdgcn_readlane(count, l);
             f.first = before + __builtin_amdgcn_readlane(sum, l) - f.count;
+            f.slot = slots + __builtin_amdgcn_readlane(parts, l) - f.count;
             if (f.count > a.chunks - f.first) f.count = a.chunks - f.first;
-            return f.count > 0;
+            if (f.count > 1 && f.count > a.slots - f.slot) f.count = a.slots - f.slot;
+            return BY_RUN || want - f.first < f.count;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
         if (before > a.chunks) before = a.chunks;
+        slots += __builtin_amdgcn_readlane(parts, 63);
+        if (slots > a.slots) slots = a.slots;
     }
     return false;
 }
@@ -781,7 +786,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         const bool real = f0 + row < k;                     // factors beyond kmax take no part: zero
         const int64_t line = klo + f0 + row;
         float *part = nullptr;
-        if (mychunk.count > 1 && a.part) part = a.part + ((int64_t)z * gridDim.y * BM + f0 + row) * (m4 + n4) + (down ? 0 : m4);
+        if (mychunk.count > 1) part = a.part + ((int64_t)(mychunk.slot + z - mychunk.first) * gridDim.y * BM + f0 + row) * (m4 + n4) + (down ? 0 : m4);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -808,7 +813,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void join_factors_k
     const int64_t m4 = up4(a.m), n4 = up4(a.n), at = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
     if (at >= m4 + n4) return;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < f.count; ++c) y += *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)(f.first + c) * padded + k) * (m4 + n4) + at);
+    for (int c = 0; c < f.count; ++c) y += *reinterpret_cast<const f32x4 *>(a.part + ((int64_t)(f.slot + c) * padded + k) * (m4 + n4) + at);
     const bool down = at < m4;
     const int64_t col = down ? at : at - m4, width = down ? a.m : a.n;
     T *out = (T *)(down ? a.ddown : a.dup) + (lo + k) * width + col;
@@ -940,7 +945,7 @@ template <class T> hipError_t launch_factor_gradient(const FactorGradient &p, hi
         const unsigned kt = (unsigned)((p.ad.kmax + BM - 1) / BM);
         if (p.pieces) hipLaunchKernelGGL(pack_factors_kernel, dim3((unsigned)((p.rows + 15) / 16), 2), dim3(256), 0, st, p, (int)kt * BM);
         hipLaunchKernelGGL((factor_gradient_kernel<T, BM>), dim3(cols, kt, (unsigned)p.chunks), dim3(256), 0, st, p);
-        if (p.chunks > p.ad.runs)
+        if (p.slots)
             hipLaunchKernelGGL((join_factors_kernel<T, BM>), dim3((unsigned)(p.ad.runs * p.ad.kmax), (unsigned)((up4(p.m) + up4(p.n) + 1023) / 1024)),
                                dim3(256), 0, st, p, (int)kt * BM);
     };

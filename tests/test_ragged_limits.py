@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2202_09518_amd as nmf
+from test_ragged_products import Problem
 
 gpu = pytest.mark.gpu
 
@@ -55,3 +56,25 @@ def test_factor_gradients_of_overlapping_segments_stay_in_their_scratch(runs, dt
         for o in outs:
             assert bool((o[:runs * kmax] == 7).all()) and bool((o[2 * runs * kmax:] == 7).all())
     assert bool(mem[need // 4:].isnan().all())
+
+
+@pytest.mark.parametrize("rows,segments,kmax", [(512, 512, 64), (256, 256, 16), (4096, 40, 256)])
+def test_scratch_of_factor_gradients_does_not_grow_with_idle_runs(rows, segments, kmax):
+    """Only runs with several chunks have parts, and the rows bound their number."""
+    need = [nmf.nmf_ragged_work_bytes(3, nmf.NMF_F32, rows, 8192, 8192, segments, runs, kmax, runs * kmax) for runs in (200, 2000, 8000)]
+    assert need[0] == need[1] == need[2]
+    assert nmf.nmf_ragged_work_bytes(3, nmf.NMF_F32, 60, 8192, 8192, 2, 2000, kmax, 2000 * kmax) == 0       # one chunk for each run
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_few_runs_with_many_rows_among_many_with_few(typ):
+    """Three of 150 runs have several chunks, two of them behind the first 64; others one or none."""
+    p = Problem(3000, 160, 150, 2, 40, 200, 136, False, typ)
+    p.which[:50], p.which[60:75], p.which[100:140:2] = 70, 9, 149
+    p.run = torch.tensor(p.which, dtype=torch.int32, device="cuda")
+    Y, dX = torch.empty_like(p.dY), torch.empty_like(p.X)
+    dWt, dH = torch.full_like(p.Wt, 5.0), torch.full_like(p.H, 5.0)
+    p.forward(Y)
+    p.backward(dX, dWt, dH)
+    p.check_gradient(dWt, dH)
