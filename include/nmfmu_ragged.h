@@ -100,7 +100,11 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
  * Scratch of the fastest plan, in bytes (0: none needed, or invalid sizes).  kind: 0 grouped product,
  * 1 grouped gradient, 2 low-rank product, 3 low-rank gradient; parts: groups or segments; runs, kmax,
  * ktotal: kinds 2 and 3 only.
+ * To kinds 0 to 2 is added which operands lie off 16-byte borders, by their base pointer, leading dimension
+ * or stride (their widths are seen from the sizes), so that there is room for copies of them:
+ * NMF_ODD_X, NMF_ODD_B (B or A; dY for kind 1) and NMF_ODD_FACTORS (Wt or H).
  */
+enum { NMF_ODD_X = 16, NMF_ODD_B = 32, NMF_ODD_FACTORS = 64 };
 size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, int64_t n, int32_t parts,
                              int32_t runs, int32_t kmax, int64_t ktotal);
 

@@ -29,6 +29,7 @@ NMF_MU_MAX_K = 64
 NMF_MU_MAX_K_SLICED = 1024
 NMF_LOWRANK_MAX_K = 256
 NMF_F32, NMF_BF16, NMF_F16 = range(3)
+NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS = 16, 32, 64
 
 _lib = None
 
@@ -346,6 +347,14 @@ def _list(t, dtype, count, what):
     raise ValueError(f"{what}: need a contiguous {dtype} device tensor of {count} entries")
 
 
+def _odd(flag, typ, ptr, *steps) -> int:
+    """flag if a matrix at ptr does not lie on 16-byte borders; steps: its leading dimension and stride in entries."""
+    at = ptr
+    for s in steps:
+        at |= s * (4 if typ == NMF_F32 else 2)
+    return flag if at & 15 else 0
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less a call than the stream object
 
 
@@ -388,7 +397,8 @@ def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=N
     x, ldx = _rows_of(X, X.dtype, rows, m, "X")
     b, ldb, stride_b = _stack_of(B, X.dtype, groups, *((n, m) if transposed else (m, n)), "B")
     y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
-    w, nbytes, _keep = _work(0, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
+    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, b, ldb, stride_b if groups > 1 else 0)
+    w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
     _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
                                      int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(X, stream)))
 
@@ -399,7 +409,8 @@ def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, strea
     x, ldx = _rows_of(X, X.dtype, rows, m, "X")
     dy, ldy = _rows_of(dY, X.dtype, rows, n, "dY")
     g, ldg, stride_g = _stack_of(G, X.dtype, groups, m, n, "G")
-    w, nbytes, _keep = _work(1, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
+    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, dy, ldy)
+    w, nbytes, _keep = _work(1 | odd, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
     _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, m, n,
                                       g, ldg, stride_g, w, nbytes, _stream_at(X, stream)))
 
@@ -412,10 +423,12 @@ def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt
     x, ldx = _rows_of(X, X.dtype, rows, m, "X")
     a, lda = _rows_of(A, X.dtype, *((n, m) if transposed else (m, n)), "A")
     y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
-    w, nbytes, _keep = _work(2, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
+    down, up = _list(Wt, X.dtype, ktotal * m, "Wt"), _list(H, X.dtype, ktotal * n, "H")
+    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, a, lda) | (_odd(NMF_ODD_FACTORS, typ, down | up) if segments else 0)
+    w, nbytes, _keep = _work(2 | odd, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
     _check(lib().nmf_lowrank_product(
         typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, segments + 1, "offsets"),
-        _list(run, torch.int32, segments, "run"), segments, _list(Wt, X.dtype, ktotal * m, "Wt"), _list(H, X.dtype, ktotal * n, "H"),
+        _list(run, torch.int32, segments, "run"), segments, down, up,
         _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal,
         None if scale is None else _list(scale, torch.float32, runs, "scale"), _list(U, torch.float32, rows * kmax, "U"), y, ldy,
         w, nbytes, _stream_at(X, stream)))

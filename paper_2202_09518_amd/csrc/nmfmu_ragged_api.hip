@@ -191,22 +191,27 @@ int align_all(int32_t type, Matrix *const *all, int n, double flops, Scratch *s,
     *done = true;
     return NMF_OK;
 }
-// Scratch that they can take, by sizes alone.
+// Scratch that they can take: of widths that do not fill 16 bytes, and of operands that `odd` says lie off their borders.
 size_t copies_of(int32_t type, size_t bytes, double flops) { return bytes && worth_copies(bytes_of(type), bytes, flops) ? bytes : 0; }
 bool ragged_rows(int64_t cols, int e) { return cols * e % 16 != 0; }
-size_t product_copies(int32_t type, int64_t rows, int64_t count, int64_t m, int64_t n, int64_t ktotal)
+size_t product_copies(int32_t type, int64_t rows, int64_t count, int64_t m, int64_t n, int64_t ktotal, int odd)
+{
+    const int e = bytes_of(type);
+    const bool bad_m = ragged_rows(m, e), bad_n = ragged_rows(n, e);
+    size_t b = 0;
+    if (bad_m || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
+    if (bad_m || bad_n || (odd & NMF_ODD_B)) b += std::max(copy_bytes(count * m, n, e), copy_bytes(count * n, m, e));
+    if (bad_m || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, m, e);
+    if (bad_n || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, n, e);
+    return copies_of(type, b, 2.0 * rows * m * n);
+}
+size_t gradient_copies(int32_t type, int64_t rows, int64_t m, int64_t n, int odd)
 {
     const int e = bytes_of(type);
     size_t b = 0;
-    if (ragged_rows(m, e)) b += copy_bytes(rows, m, e) + copy_bytes(ktotal, m, e);
-    if (ragged_rows(n, e)) b += copy_bytes(ktotal, n, e);
-    if (ragged_rows(m, e) || ragged_rows(n, e)) b += std::max(copy_bytes(count * m, n, e), copy_bytes(count * n, m, e));
+    if (ragged_rows(m, e) || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
+    if (ragged_rows(n, e) || (odd & NMF_ODD_B)) b += copy_bytes(rows, n, e);
     return copies_of(type, b, 2.0 * rows * m * n);
-}
-size_t gradient_copies(int32_t type, int64_t rows, int64_t m, int64_t n)
-{
-    const int e = bytes_of(type);
-    return copies_of(type, (ragged_rows(m, e) ? copy_bytes(rows, m, e) : 0) + (ragged_rows(n, e) ? copy_bytes(rows, n, e) : 0), 2.0 * rows * m * n);
 }
 
 bool sizes_ok(int64_t rows, int64_t m, int64_t n) { return rows >= 0 && m > 0 && n > 0 && rows <= kMost && m <= kMost && n <= kMost; }
@@ -408,19 +413,20 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
 size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, int64_t n, int32_t parts, int32_t runs, int32_t kmax,
                              int64_t ktotal)
 {
+    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ODD_FACTORS);
     if (type < NMF_F32 || type > NMF_F16 || !sizes_ok(rows, m, n) || rows == 0) return 0;
-    switch (kind) {
+    switch (kind - odd) {
     case 0: {
         if (parts < 1) return 0;
         const int splits = product_plan(type, rows, parts, m, n).splits;
-        return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0);
+        return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0, odd);
     }
     case 1:
-        return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n);
+        return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n, odd);
     case 2: {
         if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 0 || ktotal > kMost) return 0;
         const int splits = product_plan(type, rows, 1, m, n).splits;
-        const size_t copies = product_copies(type, rows, 1, m, n, ktotal);
+        const size_t copies = product_copies(type, rows, 1, m, n, ktotal, odd);
         if (parts == 0) return (splits > 1 ? product_part(rows, n, splits) : 0) + copies;
         return (joined_plan(rows, n, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
                shrink_part(rows, kmax, shrink_plan(type, rows, parts, m, kmax)) + copies;
