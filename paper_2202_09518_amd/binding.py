@@ -305,7 +305,8 @@ def nmf_aht_w_update_dense(A, m, n, k, H, GH, W, eps, stream=None) -> None:
 
 
 # ---- products over ragged ranges of rows (include/nmfmu_ragged.h) ------------------
-# Types and leading dimensions are the tensors'; the scratch is torch's unless `work` (a uint8 device tensor) is given.
+# Types and leading dimensions are the tensors'; the scratch is torch's unless `work` (a uint8 device tensor) is given.  All
+# tensors lie on X's device, and the call runs there, whichever device is current.
 
 _TYPES = {torch.float32: NMF_F32, torch.bfloat16: NMF_BF16, torch.float16: NMF_F16}
 
@@ -317,34 +318,34 @@ def _type(t: torch.Tensor, what: str) -> int:
     return typ
 
 
-def _rows_of(t, dtype, rows, cols, what):
+def _rows_of(t, dtype, device, rows, cols, what):
     """(pointer, leading dimension) of a rows x cols matrix whose rows are contiguous."""
-    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+    if t.dtype is dtype and t.get_device() == device and t.shape == (rows, cols):
         ld, step = t.stride()
         if step == 1 or cols <= 1:
             if ld >= cols:
                 return t.data_ptr(), ld
             if rows <= 1:
                 return t.data_ptr(), cols
-    raise ValueError(f"{what}: need a {rows} x {cols} {dtype} device tensor with contiguous rows that do not overlap")
+    raise ValueError(f"{what}: need a {rows} x {cols} {dtype} tensor on device {device} with contiguous rows that do not overlap")
 
 
-def _stack_of(t, dtype, count, rows, cols, what):
+def _stack_of(t, dtype, device, count, rows, cols, what):
     """(pointer, leading dimension, stride) of `count` such matrices."""
-    if t.dtype is dtype and t.is_cuda and t.shape == (count, rows, cols):
+    if t.dtype is dtype and t.get_device() == device and t.shape == (count, rows, cols):
         stride, ld, step = t.stride()
         if step == 1 or cols <= 1:
             if rows <= 1 and ld < cols:
                 ld = cols
             if ld >= cols:
                 return t.data_ptr(), ld, stride if count > 1 else max((rows - 1) * ld + cols, stride)
-    raise ValueError(f"{what}: need a {count} x {rows} x {cols} {dtype} device tensor with contiguous rows that do not overlap")
+    raise ValueError(f"{what}: need a {count} x {rows} x {cols} {dtype} tensor on device {device} with contiguous rows that do not overlap")
 
 
-def _list(t, dtype, count, what):
-    if t.dtype is dtype and t.is_cuda and t.numel() == count and t.is_contiguous():
+def _list(t, dtype, device, count, what):
+    if t.dtype is dtype and t.get_device() == device and t.numel() == count and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{what}: need a contiguous {dtype} device tensor of {count} entries")
+    raise ValueError(f"{what}: need a contiguous {dtype} tensor of {count} entries on device {device}")
 
 
 def _odd(flag, typ, ptr, *steps) -> int:
@@ -358,11 +359,22 @@ def _odd(flag, typ, ptr, *steps) -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less a call than the stream object
 
 
-def _stream_at(t, stream) -> int:
-    """The stream of a call: the current one of the tensor's device if none is given."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(t.get_device())
+def _stream_at(device, stream) -> int:
+    """The stream of a call: the current one of its device if none is given."""
+    if stream is None:
+        return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != device:
+        raise ValueError(f"stream: need one of device {device}")
     return _stream(stream)
+
+
+def _run_on(device, entry, *args) -> None:
+    """A C entry with its device current: a launch goes to the current one."""
+    if device == torch.cuda.current_device():
+        _check(entry(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -370,20 +382,21 @@ def _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal) -> int:
     return int(lib().nmf_ragged_work_bytes(kind, typ, rows, m, n, parts, runs, kmax, ktotal))
 
 
-def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, like, stream):
+def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, device, stream):
     """(pointer, bytes, tensor to keep) of the scratch of a call."""
     if work is not None:
-        if not (work.is_cuda and work.dtype == torch.uint8 and work.is_contiguous()):
-            raise ValueError("work: need a contiguous uint8 device tensor")
+        if not (work.get_device() == device and work.dtype == torch.uint8 and work.is_contiguous()):
+            raise ValueError(f"work: need a contiguous uint8 tensor on device {device}")
         return work.data_ptr(), work.numel(), work
     need = _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
     if need == 0:
         return None, 0, None
+    where = torch.device("cuda", device)
     if stream is None:
-        buf = torch.empty(need, dtype=torch.uint8, device=like.device)
+        buf = torch.empty(need, dtype=torch.uint8, device=where)
     else:                                   # memory that is free in the order of the call's stream
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
-            buf = torch.empty(need, dtype=torch.uint8, device=like.device)
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=where)):
+            buf = torch.empty(need, dtype=torch.uint8, device=where)
     return buf.data_ptr(), need, buf
 
 
@@ -393,56 +406,56 @@ def nmf_ragged_work_bytes(kind, type, rows, m, n, parts, runs=0, kmax=0, ktotal=
 
 def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=None, stream=None) -> None:
     """Y_g = X_g B_g; B: groups x m x n, or groups x n x m if transposed."""
-    typ = _type(X, "X")
-    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
-    b, ldb, stride_b = _stack_of(B, X.dtype, groups, *((n, m) if transposed else (m, n)), "B")
-    y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    b, ldb, stride_b = _stack_of(B, dt, d, groups, *((n, m) if transposed else (m, n)), "B")
+    y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
     odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, b, ldb, stride_b if groups > 1 else 0)
-    w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
-    _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
-                                     int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(X, stream)))
+    w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
+    _run_on(d, lib().nmf_grouped_product, typ, x, ldx, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
+            int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream))
 
 
 def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, stream=None) -> None:
     """G_g = X_g^T dY_g (groups x m x n)."""
-    typ = _type(X, "X")
-    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
-    dy, ldy = _rows_of(dY, X.dtype, rows, n, "dY")
-    g, ldg, stride_g = _stack_of(G, X.dtype, groups, m, n, "G")
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    dy, ldy = _rows_of(dY, dt, d, rows, n, "dY")
+    g, ldg, stride_g = _stack_of(G, dt, d, groups, m, n, "G")
     odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, dy, ldy)
-    w, nbytes, _keep = _work(1 | odd, typ, rows, m, n, groups, 0, 0, 0, work, X, stream)
-    _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, groups + 1, "offsets"), groups, rows, m, n,
-                                      g, ldg, stride_g, w, nbytes, _stream_at(X, stream)))
+    w, nbytes, _keep = _work(1 | odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
+    _run_on(d, lib().nmf_grouped_gradient, typ, x, ldx, dy, ldy, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, m, n,
+            g, ldg, stride_g, w, nbytes, _stream_at(d, stream))
 
 
 def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt, H, koff, runs, kmax, scale, U, Y,
                         work=None, stream=None) -> None:
     """Y = X A + scale_r (X W_r) H_r; Wt: ktotal x m, H: ktotal x n, contiguous; U: rows x kmax float32, written."""
-    typ = _type(X, "X")
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
     ktotal = Wt.shape[0]
-    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
-    a, lda = _rows_of(A, X.dtype, *((n, m) if transposed else (m, n)), "A")
-    y, ldy = _rows_of(Y, X.dtype, rows, n, "Y")
-    down, up = _list(Wt, X.dtype, ktotal * m, "Wt"), _list(H, X.dtype, ktotal * n, "H")
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    a, lda = _rows_of(A, dt, d, *((n, m) if transposed else (m, n)), "A")
+    y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
+    down, up = _list(Wt, dt, d, ktotal * m, "Wt"), _list(H, dt, d, ktotal * n, "H")
     odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, a, lda) | (_odd(NMF_ODD_FACTORS, typ, down | up) if segments else 0)
-    w, nbytes, _keep = _work(2 | odd, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
-    _check(lib().nmf_lowrank_product(
-        typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, segments + 1, "offsets"),
-        _list(run, torch.int32, segments, "run"), segments, down, up,
-        _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal,
-        None if scale is None else _list(scale, torch.float32, runs, "scale"), _list(U, torch.float32, rows * kmax, "U"), y, ldy,
-        w, nbytes, _stream_at(X, stream)))
+    w, nbytes, _keep = _work(2 | odd, typ, rows, m, n, segments, runs, kmax, ktotal, work, d, stream)
+    _run_on(
+        d, lib().nmf_lowrank_product, typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"),
+        _list(run, torch.int32, d, segments, "run"), segments, down, up,
+        _list(koff, torch.int32, d, runs + 1, "koff"), runs, kmax, ktotal,
+        None if scale is None else _list(scale, torch.float32, d, runs, "scale"), _list(U, torch.float32, d, rows * kmax, "U"), y, ldy,
+        w, nbytes, _stream_at(d, stream))
 
 
 def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work=None, stream=None) -> None:
     """dW_r = X^T V and dH_r = U^T dY over the rows of each run; dWt: ktotal x m, dH: ktotal x n, contiguous."""
-    typ = _type(X, "X")
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
     ktotal = dWt.shape[0]
-    x, ldx = _rows_of(X, X.dtype, rows, m, "X")
-    dy, ldy = _rows_of(dY, X.dtype, rows, n, "dY")
-    w, nbytes, _keep = _work(3, typ, rows, m, n, segments, runs, kmax, ktotal, work, X, stream)
-    _check(lib().nmf_lowrank_gradient(
-        typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, segments + 1, "offsets"), _list(run, torch.int32, segments, "run"),
-        segments, _list(koff, torch.int32, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, rows * kmax, "U"),
-        _list(V, torch.float32, rows * kmax, "V"), _list(dWt, X.dtype, ktotal * m, "dWt"), _list(dH, X.dtype, ktotal * n, "dH"),
-        w, nbytes, _stream_at(X, stream)))
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    dy, ldy = _rows_of(dY, dt, d, rows, n, "dY")
+    w, nbytes, _keep = _work(3, typ, rows, m, n, segments, runs, kmax, ktotal, work, d, stream)
+    _run_on(
+        d, lib().nmf_lowrank_gradient, typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"), _list(run, torch.int32, d, segments, "run"),
+        segments, _list(koff, torch.int32, d, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, d, rows * kmax, "U"),
+        _list(V, torch.float32, d, rows * kmax, "V"), _list(dWt, dt, d, ktotal * m, "dWt"), _list(dH, dt, d, ktotal * n, "dH"),
+        w, nbytes, _stream_at(d, stream))
