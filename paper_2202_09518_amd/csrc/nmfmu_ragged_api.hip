@@ -41,7 +41,8 @@ int splits_for(int64_t tiles, int64_t workgroups, int64_t k, int stage)
 double tile_time(int shape, bool floats, int64_t tiles, bool unequal)
 {
     static const double rate[2][3] = {{1.0, 0.72, 0.5}, {0.93, 0.85, 0.74}};      // 256 x 256, 128 x 128, 64 x 64
-    return (double)std::max<int64_t>(ceil_div(tiles, kComputeUnits), unequal ? 2 : 1) * kTileRows[shape] * kTileCols[shape] / rate[floats][shape];
+    return (double)std::max<int64_t>(ceil_div(tiles, kComputeUnits), unequal ? 2 : 1) * kTileRows[shape] * kTileCols[shape] /
+           rate[floats][std::min(shape, 2)];
 }
 template <class F> int fastest(bool floats, bool unequal, F tiles)
 {
@@ -51,12 +52,24 @@ template <class F> int fastest(bool floats, bool unequal, F tiles)
     return best;
 }
 
+// Time of a product in s parts, us: its stages, which take what their products do and the latency that a tile does not hide (more where
+// rows pass registers), and the launch that joins the parts, by its workgroups and the parts' bytes written and read.
+// Measured, one part and several: 8192 x 64 columns from 6000 rows f32 181 and 67 (8), from 16384 rows 188 and 169 (3); 64 groups, 8192 rows
+// of 4096 x 64 f32 271 and 85 (4), bf16 22.0 and 27.6 (3); 8192 x 64 from 8192 rows bf16 39.7 and 33.5 (3); 1024 x 128 from 4096 rows bf16 8.6
+// and 14.1 (3); 512 x 256 from 4096 rows f32 15.9 and 25.4 (3); 515 x 389 in 9 groups of 1237 rows f32 29.6 and 24.6 (4), bf16 13.5 and 14.6 (2).
+double parts_time(int shape, bool floats, int64_t tiles, int64_t stages, int s, int64_t rows, int64_t n, bool registers)
+{
+    const double stage = tile_time(shape, floats, tiles * s, false) * (floats ? 1.08e-4 : 1.3e-5) + (floats ? 0.1 : 0.2) + (registers ? 0.8 : 0.0);
+    const double join = s == 1 ? 0.0 : 3.0 + rows * ceil_div(n, 256) / 1100.0 + (double)s * rows * n * 8 / 4.5e6;
+    return ceil_div(stages, s) * stage + join;
+}
+
 // Tile shape and parts of a product of `rows` rows in `groups` ranges.  Few rows take tiles of 64 or 32 rows, others the
 // fastest; but up to 256 rows of a large matrix, which each row of tiles reads again, take the 128 x 128 rather than the
 // 64 x 64 (160 x 8192 x 4096: 49 and 56 us).
 // Parts (us): 500 x 4096 x 1000 (128 tiles of 64 x 64) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024
 // (48) 25.8, 13.5 with four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their
-// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.
+// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.  None where the parts cost more than they save.
 Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
 {
     groups = std::max<int64_t>(1, std::min(groups, rows));
@@ -69,7 +82,11 @@ Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t
     else p.shape = fastest(floats, false, tiles);
     if (p.shape == k64x64 && avg <= 256 && groups * m * n * bytes_of(type) > (32 << 20)) p.shape = k128x128;
     const int64_t workgroups = p.shape != k64x64 ? kComputeUnits : (floats ? 800 : 400);
-    p.splits = p.shape == k256x256 || rows > 4096 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage_of(type));
+    const int stage = stage_of(type);
+    p.splits = p.shape == k256x256 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage);
+    const bool registers = (m | n) * bytes_of(type) % 16 != 0;
+    auto time = [&](int s) { return parts_time(p.shape, floats, tiles(p.shape), ceil_div(m, stage), s, rows, n, registers); };
+    if (p.splits > 1 && time(1) <= time(p.splits)) p.splits = 1;
     return p;
 }
 

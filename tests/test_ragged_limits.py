@@ -1,9 +1,9 @@
-"""What the products over ragged ranges keep to: their scratch on malformed offsets."""
+"""What the products over ragged ranges keep to: their scratch on malformed offsets, its size, and the parts that it holds."""
 import pytest
 import torch
 
 import paper_2202_09518_amd as nmf
-from test_ragged_products import Problem
+from test_ragged_products import TYPES, Problem, within
 
 gpu = pytest.mark.gpu
 
@@ -78,3 +78,33 @@ def test_few_runs_with_many_rows_among_many_with_few(typ):
     p.forward(Y)
     p.backward(dX, dWt, dH)
     p.check_gradient(dWt, dH)
+
+
+def parts(typ, rows, m, n, groups=1):
+    """Parts that the contraction of a grouped product is cut into."""
+    return max(1, nmf.nmf_ragged_work_bytes(0, typ, rows, m, n, groups) // (rows * n * 4))
+
+
+def test_parts_of_products_go_by_what_they_cost_not_by_a_number_of_rows():
+    """Long contractions of few tiles are split beyond 4096 rows as below; short ones of many rows are not, they would pay for the join."""
+    for typ in (nmf.NMF_F32, nmf.NMF_BF16):
+        assert parts(typ, 4096, 8192, 64) > 1 and parts(typ, 4097, 8192, 64) > 1 and parts(typ, 6000, 8192, 64) > 1
+    assert parts(nmf.NMF_F32, 8192, 4096, 64, 64) > 1
+    assert parts(nmf.NMF_BF16, 4096, 1024, 128) == 1 and parts(nmf.NMF_BF16, 4096, 512, 64) == 1
+    assert parts(nmf.NMF_F32, 4096, 512, 256) == 1
+    assert parts(nmf.NMF_BF16, 150, 4096, 1000) > 1 and parts(nmf.NMF_BF16, 24, 4096, 1000) > 1
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_products_of_many_rows_in_parts(typ):
+    rows, m, n = 5003, 4096, 64
+    dt = TYPES[typ]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X, B = torch.randn(rows, m, generator=g, device="cuda").to(dt), torch.randn(2, m, n, generator=g, device="cuda").to(dt)
+    Y = torch.empty(rows, n, dtype=dt, device="cuda")
+    cut = [0, 4100, rows]
+    nmf.nmf_grouped_product(X, torch.tensor(cut, device="cuda"), 2, rows, B, False, m, n, Y)
+    for i in range(2):
+        x, b = X[cut[i]:cut[i + 1]].double(), B[i].double()
+        within(Y[cut[i]:cut[i + 1]], x @ b, x.abs() @ b.abs(), m, typ)
