@@ -122,7 +122,7 @@ struct FactorPlan {
 FactorPlan factor_plan(int32_t type, int64_t rows, int64_t segments, int64_t runs, int64_t m, int64_t n, int kmax)
 {
     const int64_t tiles = ceil_div(kmax, factor_tile(kmax)) * (ceil_div(m, 128) + ceil_div(n, 128));
-    const int64_t blocks = ceil_div(rows, factor_rows(bytes_of(type))) + std::min(segments, rows);
+    const int64_t blocks = ceil_div(rows, factor_rows(bytes_of(type), type == NMF_F16)) + std::min(segments, rows);
     const int64_t chunk = std::max<int64_t>(4, ceil_div(blocks, std::max<int64_t>(1, 4 * kComputeUnits / tiles)));
     if (blocks <= chunk) return FactorPlan{(int)chunk, (int)runs, 0};
     const int64_t chunks = ceil_div(blocks, chunk) + runs;

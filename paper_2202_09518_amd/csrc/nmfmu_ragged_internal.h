@@ -83,7 +83,7 @@ struct FactorGradient {
 };
 
 // Rows of a block, and factors of a tile.
-inline int factor_rows(int bytes) { return bytes == 4 ? 32 : 64; }
+constexpr int factor_rows(int bytes, bool f16) { return bytes == 4 || f16 ? 32 : 64; }
 inline int factor_tile(int kmax) { return kmax <= 32 ? 32 : 64; }
 
 // Types by their bits (float as it is).

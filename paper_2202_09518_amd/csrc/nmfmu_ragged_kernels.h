@@ -43,6 +43,7 @@ template <> struct Cut<float> {
 };
 template <class T> constexpr bool two_piece_matrix() { return false; }
 template <> constexpr bool two_piece_matrix<f16_t>() { return true; }      // its 11 bits are two bf16
+template <class T> constexpr int block_rows() { return factor_rows(sizeof(T), two_piece_matrix<T>()); }
 
 // Entries [k, k + N) of a row of `width` floats, zero from kend on.
 template <int N> __device__ __forceinline__ void floats_at(const float *row, int k, int kend, int width, float (&x)[N])
@@ -613,14 +614,15 @@ __global__ __launch_bounds__(256) inline void pack_factors_kernel(FactorGradient
     }
 }
 
-// BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (halves) or 32 (floats) at a time.
+// BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (bf16) or 32 at a time.  (f16: X and dY are
+// two pieces in LDS; 64 rows of them leave room for one workgroup on a compute unit, 32 for two or three.)
 // Reads X and dY once for every BM factors; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 50 us (2.7 TB/s) on pieces (65 where each column
 // tile cuts them itself), bound by the latency of its loads at two workgroups a compute unit; 4096 rows of 4096 + 2048 floats,
 // ranks to 16: 36 us (2.8 TB/s).
 template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradient_kernel(FactorGradient a)
 {
     using E = typename Cut<T>::E;
-    constexpr int BN = 128, SK = stage_k<E>();
+    constexpr int BN = 128, SK = block_rows<T>();
     constexpr int N = Cut<T>::kPieces;
     constexpr bool two = two_piece_matrix<T>();
     constexpr int kP = SK * BM * (int)sizeof(E), kQ = SK * BN * (int)sizeof(E);
@@ -659,7 +661,8 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         for (int j = 0; j < TN; ++j) acc[i][j] = low[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     constexpr int EN = chunk_n<E>(), TE = chunk_n<T>();
-    constexpr int pc = BM / EN, PJ = SK * pc / 256, qc = BN / TE, QJ = SK * qc / 256;
+    constexpr int pc = BM / EN, PJ = (SK * pc + 255) / 256, qc = BN / TE, QJ = SK * qc / 256;
+    auto one_of = [](int q) { return SK * pc % 256 == 0 || q < SK * pc; };      // a thread's chunk of P exists
 
     // The run's rows in blocks of SK within its segments: a.chunk of them from `from` on.
     int base = -64, turn = -1;
@@ -704,6 +707,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 #pragma unroll
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
+            if (!one_of(q)) continue;
             if constexpr (N > 1) {
                 if (pieces) {
                     const bf16_t *line = pieces + (r + (kr < left ? kr : 0)) * (N * (int64_t)kp) + f0 + c * EN;
@@ -722,6 +726,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 #pragma unroll
         for (int j = 0; j < PJ; ++j) {
             const int q = threadIdx.x + 256 * j, kr = q / pc, c = q % pc;
+            if (!one_of(q)) continue;
             char *at = to + kr * (BM * (int)sizeof(E)) + ((c ^ rc_shift<E, BM>(kr)) << 4);
 #pragma unroll
             for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(at + i * kP) = pv[j][i];
@@ -754,7 +759,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
         if (more) get();
         const char *lp = lds + (n & 1) * kStage, *lq = lp + kAllP;
 #pragma unroll
-        for (int kk = 0; kk < kStageBytes / 64; ++kk) {
+        for (int kk = 0; kk < SK * (int)sizeof(E) / 64; ++kk) {
             u32x4 q[TN], ql[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
@@ -767,13 +772,11 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
                 u32x4 p[N];
 #pragma unroll
                 for (int n = 0; n < N; ++n) p[n] = rp.read(lp + n * kP, i, kk);
-                if constexpr (two) {
-                    mac_row<E>(ql, p[1], low[i]);
-                    mac_row<E>(ql, p[0], low[i]);
-                }
-#pragma unroll
-                for (int n = N - 1; n > 0; --n) mac_row<E>(q, p[n], low[i]);
+                if constexpr (two) mac_row<E>(ql, p[1], low[i]);
+                if constexpr (N > 1) mac_row<E>(q, p[N - 1], low[i]);
                 mac_row<E>(q, p[0], acc[i]);
+                if constexpr (two) mac_row<E>(ql, p[0], low[i]);
+                if constexpr (N > 1) mac_row<E>(q, p[1], low[i]);
             }
         }
         if (more) put(lds + ((n + 1) & 1) * kStage);
@@ -803,7 +806,7 @@ template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradien
 // The gradients of runs with several chunks: one factor of a run, 1024 columns of m and n side by side.
 template <class T, int BM> __global__ __launch_bounds__(256) void join_factors_kernel(FactorGradient a, int padded)
 {
-    constexpr int SK = stage_k<typename Cut<T>::E>();
+    constexpr int SK = block_rows<T>();
     const int id = blockIdx.x / a.ad.kmax, k = blockIdx.x % a.ad.kmax;
     const int64_t lo = a.ad.koff[id], hi = a.ad.koff[id + 1];
     if (lo < 0 || lo + k >= hi || lo + k >= a.ad.ktotal) return;

@@ -26,7 +26,7 @@ def chunks_planned(typ, block):
     return room, c["segments"] // 2 * (c["rows"] // block) // 4
 
 
-@pytest.mark.parametrize("typ,block", [(nmf.NMF_F32, 32), (nmf.NMF_BF16, 64), (nmf.NMF_F16, 64)])
+@pytest.mark.parametrize("typ,block", [(nmf.NMF_F32, 32), (nmf.NMF_BF16, 64), (nmf.NMF_F16, 32)])
 def test_overlapping_segments_would_fill_more_chunks_than_there_are(typ, block):
     room, filled = chunks_planned(typ, block)
     assert 1 <= room < filled // 2
