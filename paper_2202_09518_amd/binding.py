@@ -348,15 +348,13 @@ def _list(t, dtype, device, count, what):
     raise ValueError(f"{what}: need a contiguous {dtype} tensor of {count} entries on device {device}")
 
 
-def _odd(flag, typ, ptr, *steps) -> int:
-    """flag if a matrix at ptr does not lie on 16-byte borders; steps: its leading dimension and stride in entries."""
-    at = ptr
-    for s in steps:
-        at |= s * (4 if typ == NMF_F32 else 2)
-    return flag if at & 15 else 0
+def _odd(flag, bits) -> int:
+    """flag if a matrix does not lie on 16-byte borders; bits: its pointer, and leading dimension and stride in bytes, or-ed."""
+    return flag if bits & 15 else 0
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less a call than the stream object
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # the tensors have opened the device
 
 
 def _stream_at(device, stream) -> int:
@@ -368,13 +366,10 @@ def _stream_at(device, stream) -> int:
     return _stream(stream)
 
 
-def _run_on(device, entry, *args) -> None:
-    """A C entry with its device current: a launch goes to the current one."""
-    if device == torch.cuda.current_device():
-        _check(entry(*args))
-    else:
-        with torch.cuda.device(device):
-            _check(entry(*args))
+def _call_on(device, call, *args) -> None:
+    """A call with its device current: a launch goes to the current one."""
+    with torch.cuda.device(device):
+        call(*args)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -391,12 +386,11 @@ def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, device, stream
     need = _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
     if need == 0:
         return None, 0, None
-    where = torch.device("cuda", device)
     if stream is None:
-        buf = torch.empty(need, dtype=torch.uint8, device=where)
+        buf = torch.empty(need, dtype=torch.uint8, device=device)
     else:                                   # memory that is free in the order of the call's stream
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=where)):
-            buf = torch.empty(need, dtype=torch.uint8, device=where)
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)):
+            buf = torch.empty(need, dtype=torch.uint8, device=device)
     return buf.data_ptr(), need, buf
 
 
@@ -407,55 +401,66 @@ def nmf_ragged_work_bytes(kind, type, rows, m, n, parts, runs=0, kmax=0, ktotal=
 def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=None, stream=None) -> None:
     """Y_g = X_g B_g; B: groups x m x n, or groups x n x m if transposed."""
     typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_grouped_product, X, offsets, groups, rows, B, transposed, m, n, Y, work, stream)
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     b, ldb, stride_b = _stack_of(B, dt, d, groups, *((n, m) if transposed else (m, n)), "B")
     y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
-    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, b, ldb, stride_b if groups > 1 else 0)
+    e = X.element_size()
+    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, b | ldb * e | (stride_b * e if groups > 1 else 0))
     w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
-    _run_on(d, lib().nmf_grouped_product, typ, x, ldx, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
-            int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream))
+    _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
+                                     int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))
 
 
 def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, stream=None) -> None:
     """G_g = X_g^T dY_g (groups x m x n)."""
     typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_grouped_gradient, X, dY, offsets, groups, rows, m, n, G, work, stream)
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     dy, ldy = _rows_of(dY, dt, d, rows, n, "dY")
     g, ldg, stride_g = _stack_of(G, dt, d, groups, m, n, "G")
-    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, dy, ldy)
+    e = X.element_size()
+    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, dy | ldy * e)
     w, nbytes, _keep = _work(1 | odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
-    _run_on(d, lib().nmf_grouped_gradient, typ, x, ldx, dy, ldy, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, m, n,
-            g, ldg, stride_g, w, nbytes, _stream_at(d, stream))
+    _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, m, n,
+                                      g, ldg, stride_g, w, nbytes, _stream_at(d, stream)))
 
 
 def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt, H, koff, runs, kmax, scale, U, Y,
                         work=None, stream=None) -> None:
     """Y = X A + scale_r (X W_r) H_r; Wt: ktotal x m, H: ktotal x n, contiguous; U: rows x kmax float32, written."""
     typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_lowrank_product, X, rows, A, transposed, m, n, offsets, run, segments, Wt, H, koff, runs, kmax, scale, U, Y, work, stream)
     ktotal = Wt.shape[0]
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     a, lda = _rows_of(A, dt, d, *((n, m) if transposed else (m, n)), "A")
     y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
     down, up = _list(Wt, dt, d, ktotal * m, "Wt"), _list(H, dt, d, ktotal * n, "H")
-    odd = _odd(NMF_ODD_X, typ, x, ldx) | _odd(NMF_ODD_B, typ, a, lda) | (_odd(NMF_ODD_FACTORS, typ, down | up) if segments else 0)
+    e = X.element_size()
+    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, a | lda * e) | (_odd(NMF_ODD_FACTORS, down | up) if segments else 0)
     w, nbytes, _keep = _work(2 | odd, typ, rows, m, n, segments, runs, kmax, ktotal, work, d, stream)
-    _run_on(
-        d, lib().nmf_lowrank_product, typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"),
+    _check(lib().nmf_lowrank_product(
+        typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"),
         _list(run, torch.int32, d, segments, "run"), segments, down, up,
         _list(koff, torch.int32, d, runs + 1, "koff"), runs, kmax, ktotal,
         None if scale is None else _list(scale, torch.float32, d, runs, "scale"), _list(U, torch.float32, d, rows * kmax, "U"), y, ldy,
-        w, nbytes, _stream_at(d, stream))
+        w, nbytes, _stream_at(d, stream)))
 
 
 def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work=None, stream=None) -> None:
     """dW_r = X^T V and dH_r = U^T dY over the rows of each run; dWt: ktotal x m, dH: ktotal x n, contiguous."""
     typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_lowrank_gradient, X, dY, rows, m, n, offsets, run, segments, koff, runs, kmax, U, V, dWt, dH, work, stream)
     ktotal = dWt.shape[0]
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     dy, ldy = _rows_of(dY, dt, d, rows, n, "dY")
     w, nbytes, _keep = _work(3, typ, rows, m, n, segments, runs, kmax, ktotal, work, d, stream)
-    _run_on(
-        d, lib().nmf_lowrank_gradient, typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"), _list(run, torch.int32, d, segments, "run"),
+    _check(lib().nmf_lowrank_gradient(
+        typ, x, ldx, dy, ldy, rows, m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"), _list(run, torch.int32, d, segments, "run"),
         segments, _list(koff, torch.int32, d, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, d, rows * kmax, "U"),
         _list(V, torch.float32, d, rows * kmax, "V"), _list(dWt, dt, d, ktotal * m, "dWt"), _list(dH, dt, d, ktotal * n, "dH"),
-        w, nbytes, _stream_at(d, stream))
+        w, nbytes, _stream_at(d, stream)))

@@ -22,6 +22,9 @@ class On:
     def numel(self):
         return self.shape.numel()
 
+    def element_size(self):
+        return self.dtype.itemsize
+
     def stride(self):
         return torch.empty(self.shape, device="meta").stride()
 
@@ -49,7 +52,7 @@ def entries(monkeypatch):
                 return lambda *args: 0
             return lambda *args: calls.append((name, current[0], args[-1])) or 0
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(binding, "_current_device", lambda: current[0])
     monkeypatch.setattr(torch.cuda, "device", device)
     monkeypatch.setattr(binding, "_raw_stream", lambda d: 1000 + d)
     monkeypatch.setattr(binding, "lib", lambda: Lib())
