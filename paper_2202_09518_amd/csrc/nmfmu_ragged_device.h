@@ -69,7 +69,7 @@ template <> struct Type<float> {
     static __device__ __forceinline__ float round(float x) { return x; }
 };
 
-constexpr int kStageBytes = 128;      // bytes of k in a stage, if not said otherwise
+constexpr int kStageBytes = 128;      // bytes of k in a stage
 constexpr unsigned kOutside = 0xfffffff0u;
 constexpr int kBufferFlags = 0x00020000;
 
@@ -92,7 +92,7 @@ template <int N, class F> __device__ __forceinline__ void each(F &&f) { each_of(
 constexpr int jobs_due(int n, int jobs, int slots) { return n * jobs / slots + 1 < jobs ? n * jobs / slots + 1 : jobs; }
 
 // k of a stage.
-template <class T, int SB = kStageBytes> constexpr int stage_k() { return SB / Type<T>::kBytes; }
+template <class T> constexpr int stage_k() { return kStageBytes / Type<T>::kBytes; }
 // Entries of a chunk.
 template <class T> constexpr int chunk_n() { return 16 / Type<T>::kBytes; }
 
@@ -106,7 +106,7 @@ template <class T, int R> __device__ __forceinline__ int rc_shift(int k)
 }
 
 // The same for row `row` of a KC operand.
-template <int SB> __device__ __forceinline__ int kc_shift(int row) { return SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+__device__ __forceinline__ int kc_shift(int row) { return (row >> 1) & 7; }
 
 // One operand of a tile as it lies in memory.
 struct Operand {
@@ -157,11 +157,11 @@ template <class T> __device__ __forceinline__ u32x4 keep_first(u32x4 v, int64_t 
 // PLANES 2: half a stage is k of the first plane, the other half the same k of the second.
 // DMA: base, ld and the extents are multiples of 16 bytes: the chunks go to LDS without passing registers; a chunk that is
 // not there is asked for outside the descriptor's range, which delivers zeros.  Else: any alignment, through registers.
-template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> struct Loader {
-    static constexpr int kJobs = R * (SB / 16) / THREADS;            // chunks of a thread
-    static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : SB / 16;
+template <class T, int R, bool RC, int THREADS, bool DMA, int PLANES> struct Loader {
+    static constexpr int kJobs = R * (kStageBytes / 16) / THREADS;            // chunks of a thread
+    static constexpr int kRowChunks = RC ? R * Type<T>::kBytes / 16 : kStageBytes / 16;
     static constexpr int kRowStep = THREADS / kRowChunks;            // rows from job to job
-    static_assert(R * (SB / 16) % THREADS == 0 && THREADS % kRowChunks == 0, "whole jobs");
+    static_assert(R * (kStageBytes / 16) % THREADS == 0 && THREADS % kRowChunks == 0, "whole jobs");
     static_assert(RC || kRowStep % 16 == 0, "places repeat from job to job");
 
     const char *base;
@@ -174,18 +174,18 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
 
     __device__ __forceinline__ int chunk(int j) const
     {
-        return RC ? place ^ rc_shift<T, R>(line + j * kRowStep) : place ^ kc_shift<SB>(line);
+        return RC ? place ^ rc_shift<T, R>(line + j * kRowStep) : place ^ kc_shift(line);
     }
     // k of job j within its plane's part of a stage, and where its chunk lies from the stage's first k on.
     __device__ __forceinline__ int k_of(int j) const
     {
-        return RC ? (line + j * kRowStep) % (stage_k<T, SB>() / PLANES) : chunk(j) % (SB / 16 / PLANES) * chunk_n<T>();
+        return RC ? (line + j * kRowStep) % (stage_k<T>() / PLANES) : chunk(j) % (kStageBytes / 16 / PLANES) * chunk_n<T>();
     }
     __device__ __forceinline__ int64_t where(int j) const
     {
         const int row = line + j * kRowStep;
-        if (RC) return k_of(j) * ld + chunk(j) * 16 + (PLANES == 2 && row >= stage_k<T, SB>() / 2 ? plane : 0);
-        return (int64_t)row * ld + k_of(j) * Type<T>::kBytes + (PLANES == 2 && chunk(j) >= SB / 32 ? plane : 0);
+        if (RC) return k_of(j) * ld + chunk(j) * 16 + (PLANES == 2 && row >= stage_k<T>() / 2 ? plane : 0);
+        return (int64_t)row * ld + k_of(j) * Type<T>::kBytes + (PLANES == 2 && chunk(j) >= kStageBytes / 32 ? plane : 0);
     }
     __device__ __forceinline__ bool there(int j) const
     {
@@ -221,7 +221,7 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
             const u32x4 r = {(unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)at),
                              (unsigned)__builtin_amdgcn_readfirstlane((int)((uintptr_t)at >> 32)) & 0xffffu, 0x7fffffffu, (unsigned)kBufferFlags};
             unsigned o = off[j];
-            if (left < stage_k<T, SB>() / PLANES && k_of(j) >= left) o = kOutside;
+            if (left < stage_k<T>() / PLANES && k_of(j) >= left) o = kOutside;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(r) : "memory", "m0");
         } else {
             u32x4 v = {0, 0, 0, 0};
@@ -245,8 +245,8 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int SB, int PLANES> st
 };
 
 // Reads operands of the matrix instruction from a stage: block of 16 rows or columns at first + t * STEP, matrix step kk.
-template <class T, int R, bool RC, int STEP, int SB = kStageBytes> struct Reader {
-    int at[SB / 64];        // KC: by kk; RC: unused
+template <class T, int R, bool RC, int STEP> struct Reader {
+    int at[kStageBytes / 64];        // KC: by kk; RC: unused
     int lane, first;
 
     __device__ __forceinline__ void open(int first_)
@@ -255,17 +255,17 @@ template <class T, int R, bool RC, int STEP, int SB = kStageBytes> struct Reader
         first = first_;
         if (!RC) {
 #pragma unroll
-            for (int kk = 0; kk < SB / 64; ++kk) at[kk] = kc_at(kk);
+            for (int kk = 0; kk < kStageBytes / 64; ++kk) at[kk] = kc_at(kk);
         }
     }
     __device__ __forceinline__ int kc_at(int kk) const
     {
         const int row = first + (lane & 15);
-        return row * SB + (((4 * kk + (lane >> 4)) ^ kc_shift<SB>(row)) << 4);
+        return row * kStageBytes + (((4 * kk + (lane >> 4)) ^ kc_shift(row)) << 4);
     }
     __device__ __forceinline__ u32x4 read(const char *lds, int t, int kk) const
     {
-        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * STEP * SB);
+        if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * STEP * kStageBytes);
         constexpr int pitch = R * Type<T>::kBytes;
         u32x4 v;
         if (Type<T>::kBytes == 2) {
@@ -298,20 +298,20 @@ template <int N> __device__ __forceinline__ void wait_loads()      // until at m
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A tile of BM x BN by WM x WN waves.
-template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_, int SB_ = kStageBytes, int PLANES_ = 1> struct Tile {
+template <class T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PRC_, bool QRC_, bool DMA_, int PLANES_ = 1> struct Tile {
     using T = T_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = DMA_ ? STAGES_ : 2, THREADS = 64 * WM * WN;
     static constexpr bool PRC = PRC_, QRC = QRC_, DMA = DMA_;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;      // 16 x 16 blocks of a wave: every WM-th of the rows, neighbouring columns
-    static constexpr int KK = SB_ / 64;                             // matrix steps of a stage
-    static constexpr int SB = SB_, PLANES = PLANES_, SK = stage_k<T, SB>() / PLANES;      // bytes of k in a stage; its k
-    static constexpr int kLdsP = BM * SB, kLdsQ = BN * SB, kLdsStage = kLdsP + kLdsQ;
+    static constexpr int KK = kStageBytes / 64;                             // matrix steps of a stage
+    static constexpr int PLANES = PLANES_, SK = stage_k<T>() / PLANES;      // k of a stage
+    static constexpr int kLdsP = BM * kStageBytes, kLdsQ = BN * kStageBytes, kLdsStage = kLdsP + kLdsQ;
     static constexpr int kLds = STAGES * kLdsStage;
     using Acc = f32x4[TM][TN];
-    using LoadP = Loader<T, BM, PRC, THREADS, DMA, SB, PLANES>;
-    using LoadQ = Loader<T, BN, QRC, THREADS, DMA, SB, PLANES>;
-    using ReadP = Reader<T, BM, PRC, 16 * WM, SB>;
-    using ReadQ = Reader<T, BN, QRC, 16, SB>;
+    using LoadP = Loader<T, BM, PRC, THREADS, DMA, PLANES>;
+    using LoadQ = Loader<T, BN, QRC, THREADS, DMA, PLANES>;
+    using ReadP = Reader<T, BM, PRC, 16 * WM>;
+    using ReadQ = Reader<T, BN, QRC, 16>;
 
     static __device__ __forceinline__ void clear(Acc &acc)
     {

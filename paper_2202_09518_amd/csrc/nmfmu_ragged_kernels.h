@@ -391,7 +391,7 @@ template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREA
     typename C::Acc acc;
     C::clear(acc);
     if constexpr (ADAPTERS) {
-        using X = Tile<T, C::BM, C::BN, C::WM, C::WN, 2, false, true, C::DMA, C::SB, (sizeof(T) == 2 ? 2 : 1)>;
+        using X = Tile<T, C::BM, C::BN, C::WM, C::WN, 2, false, true, C::DMA, (sizeof(T) == 2 ? 2 : 1)>;
         if (!a.joined) {
             const bool packed = a.pack != nullptr;
             if (!packed || add_packed<C, X>(a, f.r0, f.r1, c0, lds, acc)) add_rest<C>(a, f.r0, f.r1, c0, packed, X::SK, acc);
