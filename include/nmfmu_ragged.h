@@ -33,8 +33,11 @@
  *   - work: device scratch of the call alone, 16-byte aligned, nmf_ragged_work_bytes(...) bytes for the
  *     plan that is fastest; with less (also NULL, 0) the call uses a plan that fits (nmf_lowrank_product with
  *     long segments then adds their adapters by plain sums, much slower).  It must stay valid until the work
- *     is done.
- *   - Sizes below 2^31.  rows == 0 is a successful no-op (gradients are then zeros).
+ *     is done.  nmf_lowrank_product asks for the result in floats, 4 rows n bytes, for each part that its
+ *     contraction is cut into, and one of them where segments have fewer than 24 rows on average, whose
+ *     adapters are added to it; else for 4 rows kmax bytes, kmax in whole 32s.
+ *   - Sizes below 2^31; more tiles, rows or runs than one launch has room for (2^23 workgroups, 65535 runs in
+ *     nmf_lowrank_gradient) give NMF_EUNSUPPORTED.  rows == 0 is a successful no-op (gradients are then zeros).
  */
 #ifndef NMFMU_RAGGED_H
 #define NMFMU_RAGGED_H

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2202_09518_amd as nmf
-from test_ragged_products import TYPES, Problem, within
+from test_ragged_products import TYPES, Problem, lengths_of, within
 
 gpu = pytest.mark.gpu
 
@@ -108,3 +108,18 @@ def test_products_of_many_rows_in_parts(typ):
     for i in range(2):
         x, b = X[cut[i]:cut[i + 1]].double(), B[i].double()
         within(Y[cut[i]:cut[i + 1]], x @ b, x.abs() @ b.abs(), m, typ)
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_gradients_of_more_groups_than_a_wave_has_lanes(typ):
+    rows, groups, m, n = 900, 150, 136, 264
+    dt = TYPES[typ]
+    g = torch.Generator(device="cuda").manual_seed(4)
+    X, dY = torch.randn(rows, m, generator=g, device="cuda").to(dt), torch.randn(rows, n, generator=g, device="cuda").to(dt)
+    cut = lengths_of("ragged", rows, groups, 11)
+    G = torch.full((groups, m, n), 5.0, dtype=dt, device="cuda")
+    nmf.nmf_grouped_gradient(X, dY, torch.from_numpy(cut).cuda(), groups, rows, m, n, G)
+    for i in range(groups):
+        x, dy = X[cut[i]:cut[i + 1]].double(), dY[cut[i]:cut[i + 1]].double()
+        within(G[i], x.t() @ dy, x.abs().t() @ dy.abs(), max(1, len(x)), typ)
