@@ -11,7 +11,7 @@
 //
 // Matrix instructions: v_mfma_f32_16x16x32 on halves, v_mfma_f32_16x16x4_f32 on floats (its k are taken in the order that
 // a 16-byte read of a KC operand delivers them, on both operands alike).  On normal random bf16 the 16 x 16 form holds
-// 2040 TFLOP/s in registers where the 32 x 32 form holds 1830: it moves half as much of the accumulators.  Q is the
+// 2020 TFLOP/s in registers where the 32 x 32 form holds 1790: it moves half as much of the accumulators.  Q is the
 // first operand, so a lane ends with four neighbouring columns of one row in its accumulators, which it stores together.
 #pragma once
 

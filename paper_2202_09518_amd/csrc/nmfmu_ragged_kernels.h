@@ -318,8 +318,8 @@ template <class C> __device__ __forceinline__ void unscale(const Product &a, int
     }
 }
 
-// u (or a part of it) for one tile of a segment's rows: s_r x W_r.  Bound by reading x: 16384 rows of 4096 bf16 take 29 us
-// (4.6 TB/s), 8192 rows 16.4; 64 x 64 tiles because ranks are small, four stages of them because memory is far.
+// u (or a part of it) for one tile of a segment's rows: s_r x W_r.  Bound by reading x: 16384 rows of 4096 bf16 take 25 to 29 us
+// (5.4 to 4.6 TB/s), 8192 rows 16.7; 64 x 64 tiles because ranks are small, four stages of them because memory is far.
 template <class C> __device__ __forceinline__ void shrink_tile(const Product &a, int id, char *lds)
 {
     using T = typename C::T;
@@ -352,9 +352,9 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void shrink_kernel(P
 }
 
 // Y, or parts of it over the contraction.  The first `shrink` workgroups form parts of u instead.  Long products are bound by
-// their loads and by power: 8192 x 4096 x 4096 bf16 207 us (1330 TFLOP/s), 16384 rows with adapters up to rank 64 406 us
-// (1375), float32 in tiles of 256 x 256 144 TFLOP/s.  Few rows are bound by reading b: 512 rows over 64 groups of
-// 4096 x 2048 f16 171 us (5.7 TB/s).
+// their loads and by power: 8192 x 4096 x 4096 bf16 208 us (1325 TFLOP/s), 16384 rows with adapters up to rank 64 406 to 419 us
+// (1310 to 1355), float32 in tiles of 256 x 256 144 TFLOP/s.  Few rows are bound by reading b: 512 rows over 64 groups of
+// 4096 x 2048 f16 150 to 171 us (6.5 to 5.7 TB/s).
 template <class C, class S, bool ADAPTERS> __global__ __launch_bounds__(C::THREADS) void product_kernel(Product a, int shrink)
 {
     using T = typename C::T;
@@ -616,9 +616,9 @@ __global__ __launch_bounds__(256) inline void pack_factors_kernel(FactorGradient
 
 // BM factors of one run x 128 columns of m or of n, summed over a chunk of its rows, 64 (bf16) or 32 at a time.  (f16: X and dY are
 // two pieces in LDS; 64 rows of them leave room for one workgroup on a compute unit, 32 for two or three.)
-// Reads X and dY once for every BM factors; 8192 rows, 4096 + 4096 columns, ranks to 64, bf16: 50 us (2.7 TB/s) on pieces (65 where each column
-// tile cuts them itself), bound by the latency of its loads at two workgroups a compute unit; 4096 rows of 4096 + 2048 floats,
-// ranks to 16: 36 us (2.8 TB/s).
+// Reads X and dY once for every BM factors; 8192 rows, 4096 + 4096 columns, ranks to 64: bf16 63 us (2.1 TB/s) on pieces (82 where each
+// column tile cuts them itself), f16 90 (111), bound by the latency of its loads at two workgroups a compute unit; ranks to 16 44 and 63;
+// 4096 rows of 4096 + 2048 floats, ranks to 16: 37 us (2.7 TB/s).
 template <class T, int BM> __global__ __launch_bounds__(256) void factor_gradient_kernel(FactorGradient a)
 {
     using E = typename Cut<T>::E;
