@@ -69,8 +69,11 @@ double parts_time(int shape, bool floats, int64_t tiles, int64_t stages, int s, 
 // 64 x 64 (160 x 8192 x 4096: 49 and 56 us).
 // Parts (us): 500 x 4096 x 1000 (128 tiles of 64 x 64) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024
 // (48) 25.8, 13.5 with four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their
-// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.  None where the parts cost more than they save.
-Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n)
+// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.  None where the parts cost more than they save.  With
+// adapters, which the join takes, parts save the launches that form and pack U; most of it in 16 bits, as U's tiles then share the
+// product's launch.  One part and several: 300 rows of 1024 x 512 bf16 21.2 and 12.9 (4), 2500 of 512 x 128 18.7 and 17.2 (2), 4096 of them
+// 17.4 and 22.6 (2); f32 34.9 and 28.4 (4), 35.3 and 45.7 (4).
+Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n, bool adapters)
 {
     groups = std::max<int64_t>(1, std::min(groups, rows));
     const int64_t avg = ceil_div(rows, groups);
@@ -86,7 +89,8 @@ Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t
     p.splits = p.shape == k256x256 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage);
     const bool registers = (m | n) * bytes_of(type) % 16 != 0;
     auto time = [&](int s) { return parts_time(p.shape, floats, tiles(p.shape), ceil_div(m, stage), s, rows, n, registers); };
-    if (p.splits > 1 && time(1) <= time(p.splits)) p.splits = 1;
+    const double launches = adapters ? (floats ? 2.0 : 6.0) : 0.0;
+    if (p.splits > 1 && time(1) + launches <= time(p.splits)) p.splits = 1;
     return p;
 }
 
@@ -277,7 +281,7 @@ int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t 
     if (!aligned(X, e) || !aligned(B, e) || !aligned(Y, e) || !aligned(offsets, 8)) return set_error(NMF_EINVAL, "misaligned pointer");
     if (ldx < m || ldy < n || ldb < (transposed ? m : n) || stride_b < 0) return set_error(NMF_EINVAL, "leading dimension below the row's length");
     if (rows == 0) return NMF_OK;
-    const Plan plan = product_plan(type, rows, groups, m, n);
+    const Plan plan = product_plan(type, rows, groups, m, n, false);
     Product p = {};
     p.x = X; p.ldx = ldx; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
     p.b = B; p.ldb = ldb; p.stride_b = stride_b; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
@@ -350,7 +354,7 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
         return set_error(NMF_EINVAL, "misaligned pointer");
     if (ldx < m || ldy < n || lda < (transposed ? m : n)) return set_error(NMF_EINVAL, "leading dimension below the row's length");
     if (rows == 0) return NMF_OK;
-    const Plan plan = product_plan(type, rows, 1, m, n);
+    const Plan plan = product_plan(type, rows, 1, m, n, segments > 0);
     Product p = {};
     p.x = X; p.ldx = ldx; p.groups = 1; p.rows = rows; p.m = m; p.n = n;
     p.b = A; p.ldb = lda; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
@@ -436,14 +440,14 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
     switch (kind - odd) {
     case 0: {
         if (parts < 1) return 0;
-        const int splits = product_plan(type, rows, parts, m, n).splits;
+        const int splits = product_plan(type, rows, parts, m, n, false).splits;
         return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0, odd);
     }
     case 1:
         return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n, odd);
     case 2: {
         if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 0 || ktotal > kMost) return 0;
-        const int splits = product_plan(type, rows, 1, m, n).splits;
+        const int splits = product_plan(type, rows, 1, m, n, parts > 0).splits;
         const size_t copies = product_copies(type, rows, 1, m, n, ktotal, odd);
         if (parts == 0) return (splits > 1 ? product_part(rows, n, splits) : 0) + copies;
         return (joined_plan(rows, n, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +

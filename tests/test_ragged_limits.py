@@ -123,3 +123,14 @@ def test_gradients_of_more_groups_than_a_wave_has_lanes(typ):
     for i in range(groups):
         x, dy = X[cut[i]:cut[i + 1]].double(), dY[cut[i]:cut[i + 1]].double()
         within(G[i], x.t() @ dy, x.abs().t() @ dy.abs(), max(1, len(x)), typ)
+
+
+def test_parts_of_lowrank_products_save_launches():
+    """Few rows in long segments: the join of parts takes the adapters, which else are packed by a launch of their own."""
+    def product_parts(typ, rows, m, n):
+        room = nmf.nmf_ragged_work_bytes(2, typ, rows, m, n, 4, 2, 16, 32)
+        return room // (rows * n * 4)                    # U packed is 128 bytes a row: less than one part of 128 columns
+
+    assert product_parts(nmf.NMF_BF16, 300, 1024, 512) >= 4 and product_parts(nmf.NMF_BF16, 1000, 512, 128) >= 2
+    assert product_parts(nmf.NMF_BF16, 4096, 512, 128) == 0 and product_parts(nmf.NMF_F32, 4096, 512, 128) == 0
+    assert parts(nmf.NMF_BF16, 1000, 512, 128) == 1      # without adapters the join costs more than it saves
