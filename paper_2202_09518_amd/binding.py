@@ -306,7 +306,8 @@ def nmf_aht_w_update_dense(A, m, n, k, H, GH, W, eps, stream=None) -> None:
 
 # ---- products over ragged ranges of rows (include/nmfmu_ragged.h) ------------------
 # Types and leading dimensions are the tensors'; the scratch is torch's unless `work` (a uint8 device tensor) is given.  All
-# tensors lie on X's device, and the call runs there, whichever device is current.
+# tensors lie on X's device, and the call runs there, whichever device is current.  `odd` tells the size query which operands lie off
+# 16-byte borders by their pointer, leading dimension or stride.
 
 _TYPES = {torch.float32: NMF_F32, torch.bfloat16: NMF_BF16, torch.float16: NMF_F16}
 
@@ -348,19 +349,14 @@ def _list(t, dtype, device, count, what):
     raise ValueError(f"{what}: need a contiguous {dtype} tensor of {count} entries on device {device}")
 
 
-def _odd(flag, bits) -> int:
-    """flag if a matrix does not lie on 16-byte borders; bits: its pointer, and leading dimension and stride in bytes, or-ed."""
-    return flag if bits & 15 else 0
-
-
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less a call than the stream object
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)      # 3 us less a call
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # the tensors have opened the device
 
 
 def _stream_at(device, stream) -> int:
     """The stream of a call: the current one of its device if none is given."""
     if stream is None:
-        return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+        return _raw_stream(device)
     if isinstance(stream, torch.cuda.Stream) and stream.device_index != device:
         raise ValueError(f"stream: need one of device {device}")
     return _stream(stream)
@@ -406,8 +402,8 @@ def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=N
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     b, ldb, stride_b = _stack_of(B, dt, d, groups, *((n, m) if transposed else (m, n)), "B")
     y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
-    e = X.element_size()
-    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, b | ldb * e | (stride_b * e if groups > 1 else 0))
+    e = 4 if typ == NMF_F32 else 2
+    odd = (NMF_ODD_X if (x | ldx * e) & 15 else 0) | (NMF_ODD_B if (b | (ldb | (stride_b if groups > 1 else 0)) * e) & 15 else 0)
     w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
     _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
                                      int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))
@@ -421,8 +417,8 @@ def nmf_grouped_gradient(X, dY, offsets, groups, rows, m, n, G, work=None, strea
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     dy, ldy = _rows_of(dY, dt, d, rows, n, "dY")
     g, ldg, stride_g = _stack_of(G, dt, d, groups, m, n, "G")
-    e = X.element_size()
-    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, dy | ldy * e)
+    e = 4 if typ == NMF_F32 else 2
+    odd = (NMF_ODD_X if (x | ldx * e) & 15 else 0) | (NMF_ODD_B if (dy | ldy * e) & 15 else 0)
     w, nbytes, _keep = _work(1 | odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
     _check(lib().nmf_grouped_gradient(typ, x, ldx, dy, ldy, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, m, n,
                                       g, ldg, stride_g, w, nbytes, _stream_at(d, stream)))
@@ -439,8 +435,8 @@ def nmf_lowrank_product(X, rows, A, transposed, m, n, offsets, run, segments, Wt
     a, lda = _rows_of(A, dt, d, *((n, m) if transposed else (m, n)), "A")
     y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
     down, up = _list(Wt, dt, d, ktotal * m, "Wt"), _list(H, dt, d, ktotal * n, "H")
-    e = X.element_size()
-    odd = _odd(NMF_ODD_X, x | ldx * e) | _odd(NMF_ODD_B, a | lda * e) | (_odd(NMF_ODD_FACTORS, down | up) if segments else 0)
+    e = 4 if typ == NMF_F32 else 2
+    odd = (NMF_ODD_X if (x | ldx * e) & 15 else 0) | (NMF_ODD_B if (a | lda * e) & 15 else 0) | (NMF_ODD_FACTORS if (down | up) & 15 and segments else 0)
     w, nbytes, _keep = _work(2 | odd, typ, rows, m, n, segments, runs, kmax, ktotal, work, d, stream)
     _check(lib().nmf_lowrank_product(
         typ, x, ldx, rows, a, lda, int(bool(transposed)), m, n, _list(offsets, torch.int64, d, segments + 1, "offsets"),
