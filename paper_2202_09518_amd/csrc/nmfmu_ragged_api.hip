@@ -32,6 +32,44 @@ int splits_for(int64_t tiles, int64_t workgroups, int64_t k, int stage)
     return s < 2 ? 1 : (int)s;
 }
 
+// ---- operands whose rows do not begin and end on 16 bytes ----------------------------------
+// The tiles bring 16 bytes at a time straight to LDS; other operands pass registers, which takes 1.5 to 6 times as long
+// (8192 x 4095 x 4097 bf16: 517 us, 641 with B by columns, its gradient 1430; aligned 243, 223, 211).  Where the product is
+// long enough they are copied once per call into rows that do.
+int64_t whole(int64_t cols, int e) { return (cols * e + 15) / 16 * 16 / e; }
+size_t copy_bytes(int64_t lines, int64_t cols, int e) { return (size_t)lines * whole(cols, e) * e; }
+
+// Copies of `bytes` are worth their time: launches and their bytes twice, against what the product loses without them, about as
+// long as it takes at a middling rate.  2048 x 1023 x 2049 bf16: 31 us, without 42; 1237 rows of 515 x 389 in 9 groups f32,
+// where they are not: 33 with, 25 without.
+bool worth_copies(int e, size_t bytes, double flops)
+{
+    return 5e-6 + 2.0 * bytes / 4.5e12 < 1.2 * flops / (e == 4 ? 0.8e14 : 0.5e15);
+}
+
+// Scratch that they can take: of widths that do not fill 16 bytes, and of operands that `odd` says lie off their borders.
+size_t copies_of(int32_t type, size_t bytes, double flops) { return bytes && worth_copies(bytes_of(type), bytes, flops) ? bytes : 0; }
+bool ragged_rows(int64_t cols, int e) { return cols * e % 16 != 0; }
+size_t product_copies(int32_t type, int64_t rows, int64_t count, int64_t m, int64_t n, int64_t ktotal, int odd)
+{
+    const int e = bytes_of(type);
+    const bool bad_m = ragged_rows(m, e), bad_n = ragged_rows(n, e);
+    size_t b = 0;
+    if (bad_m || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
+    if (bad_m || bad_n || (odd & NMF_ODD_B)) b += std::max(copy_bytes(count * m, n, e), copy_bytes(count * n, m, e));
+    if (bad_m || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, m, e);
+    if (bad_n || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, n, e);
+    return copies_of(type, b, 2.0 * rows * m * n);
+}
+size_t gradient_copies(int32_t type, int64_t rows, int64_t m, int64_t n, int odd)
+{
+    const int e = bytes_of(type);
+    size_t b = 0;
+    if (ragged_rows(m, e) || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
+    if (ragged_rows(n, e) || (odd & NMF_ODD_B)) b += copy_bytes(rows, n, e);
+    return copies_of(type, b, 2.0 * rows * m * n);
+}
+
 // Time of `tiles` tiles of a shape: those of the busiest compute unit, by their size and by what share of the large tile's
 // rate they reach.  us, bf16 unless said otherwise: 8192 x 4096 x 4096 takes 207 in tiles of 256 x 256; 2000 x 4096 x 2048
 // 56 in 128 x 128 and 63 in 64 x 64; 2048 x 1024 x 2048 19.0 and 21.5; 1000 x 2048 x 1024, only 64 tiles of 128 x 128, 28.9
@@ -53,15 +91,24 @@ template <class F> int fastest(bool floats, bool unequal, F tiles)
 }
 
 // Time of a product in s parts, us: its stages, which take what their products do and the latency that a tile does not hide (more where
-// rows pass registers), and the launch that joins the parts, by its workgroups and the parts' bytes written and read.
+// rows pass registers), and the launch that joins the parts, by its workgroups and the parts' bytes written and read.  With adapters the
+// join takes their factors too, and U's tiles run beside the parts, partly hidden; one part has two launches more, which form and pack U.
 // Measured, one part and several: 8192 x 64 columns from 6000 rows f32 181 and 67 (8), from 16384 rows 188 and 169 (3); 64 groups, 8192 rows
 // of 4096 x 64 f32 271 and 85 (4), bf16 22.0 and 27.6 (3); 8192 x 64 from 8192 rows bf16 39.7 and 33.5 (3); 1024 x 128 from 4096 rows bf16 8.6
 // and 14.1 (3); 512 x 256 from 4096 rows f32 15.9 and 25.4 (3); 515 x 389 in 9 groups of 1237 rows f32 29.6 and 24.6 (4), bf16 13.5 and 14.6 (2).
-double parts_time(int shape, bool floats, int64_t tiles, int64_t stages, int s, int64_t rows, int64_t n, bool registers)
+// Adapters, ranks to 16 in long segments: 300 rows of 1024 x 512 bf16 21.2 and 12.9 (4), 2500 of 512 x 128 18.7 and 17.2 (2), 4096 of them 17.4 and
+// 22.6 (2); f32 34.9 and 28.4 (4), 35.3 and 45.7 (4); ranks to 48, 2048 x 192 from 7000 rows f32 129 and 165 (2), from 3000 bf16 33.5 and 32.0 (2).
+double parts_time(int shape, bool floats, int64_t tiles, int64_t stages, int s, int64_t rows, int64_t n, bool registers, int64_t segments, int kmax)
 {
-    const double stage = tile_time(shape, floats, tiles * s, false) * (floats ? 1.08e-4 : 1.3e-5) + (floats ? 0.1 : 0.2) + (registers ? 0.8 : 0.0);
-    const double join = s == 1 ? 0.0 : 3.0 + rows * ceil_div(n, 256) / 1100.0 + (double)s * rows * n * 8 / 4.5e6;
-    return ceil_div(stages, s) * stage + join;
+    const double product = floats ? 1.08e-4 : 1.3e-5;
+    const double stage = tile_time(shape, floats, tiles * s, false) * product + (floats ? 0.1 : 0.2) + (registers ? 0.8 : 0.0);
+    const double all = ceil_div(stages, s) * stage;
+    if (s == 1) return all + (segments ? (floats ? 4.0 : 9.0) : 0.0);
+    const double workgroups = (double)rows * ceil_div(n, 256);
+    const double join = 3.0 + workgroups / 1100.0 + (double)s * rows * n * 8 / 4.5e6;
+    if (!segments) return all + join;
+    const double u_tiles = (double)(ceil_div(rows, kShrinkRows) + std::min(segments, rows)) * ceil_div(kmax, kShrinkCols);
+    return all + join + 3e-5 * workgroups * kmax + 0.6 * u_tiles / kComputeUnits * stages * tile_time(k64x64, floats, 1, false) * product;
 }
 
 // Tile shape and parts of a product of `rows` rows in `groups` ranges.  Few rows take tiles of 64 or 32 rows, others the
@@ -69,12 +116,10 @@ double parts_time(int shape, bool floats, int64_t tiles, int64_t stages, int s, 
 // 64 x 64 (160 x 8192 x 4096: 49 and 56 us).
 // Parts (us): 500 x 4096 x 1000 (128 tiles of 64 x 64) 24.1 with one, 19.9 with two, 19.8 with four; 130 x 4096 x 1024
 // (48) 25.8, 13.5 with four, 12.3 with eight; 1000 x 2048 x 1024 (256) 14.6 and 20.6 with two.  48 rows and their
-// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.  None where the parts cost more than they save.  With
-// adapters, which the join takes, parts save the launches that form and pack U; most of it in 16 bits, as U's tiles then share the
-// product's launch.  One part and several: 300 rows of 1024 x 512 bf16 21.2 and 12.9 (4), 2500 of 512 x 128 18.7 and 17.2 (2), 4096 of them
-// 17.4 and 22.6 (2); f32 34.9 and 28.4 (4), 35.3 and 45.7 (4).
-Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n, bool adapters)
+// adapters (32 tiles) 17.7 with eight, 20.1 with four, 23.4 with sixteen.  None where the parts cost more than they save.
+Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t n, int64_t segments = 0, int kmax = 0)
 {
+    const int64_t count = groups;
     groups = std::max<int64_t>(1, std::min(groups, rows));
     const int64_t avg = ceil_div(rows, groups);
     auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
@@ -87,10 +132,9 @@ Plan product_plan(int32_t type, int64_t rows, int64_t groups, int64_t m, int64_t
     const int64_t workgroups = p.shape != k64x64 ? kComputeUnits : (floats ? 800 : 400);
     const int stage = stage_of(type);
     p.splits = p.shape == k256x256 ? 1 : splits_for(tiles(p.shape), workgroups, m, stage);
-    const bool registers = (m | n) * bytes_of(type) % 16 != 0;
-    auto time = [&](int s) { return parts_time(p.shape, floats, tiles(p.shape), ceil_div(m, stage), s, rows, n, registers); };
-    const double launches = adapters ? (floats ? 2.0 : 6.0) : 0.0;
-    if (p.splits > 1 && time(1) + launches <= time(p.splits)) p.splits = 1;
+    const bool registers = ragged_rows(m | n, bytes_of(type)) && product_copies(type, rows, count, m, n, 0, 0) == 0;
+    auto time = [&](int s) { return parts_time(p.shape, floats, tiles(p.shape), ceil_div(m, stage), s, rows, n, registers, segments, kmax); };
+    if (p.splits > 1 && time(1) <= time(p.splits)) p.splits = 1;
     return p;
 }
 
@@ -155,10 +199,6 @@ template <class F> int fit(int splits, size_t have, F bytes)
     return splits;
 }
 
-// ---- operands whose rows do not begin and end on 16 bytes ----------------------------------
-// The tiles bring 16 bytes at a time straight to LDS; other operands pass registers, which takes 1.5 to 6 times as long
-// (8192 x 4095 x 4097 bf16: 517 us, 641 with B by columns, its gradient 1430; aligned 243, 223, 211).  Where the product is
-// long enough they are copied once per call into rows that do.
 struct Scratch {
     char *at;
     size_t left;
@@ -172,17 +212,6 @@ struct Scratch {
         return p;
     }
 };
-
-int64_t whole(int64_t cols, int e) { return (cols * e + 15) / 16 * 16 / e; }
-size_t copy_bytes(int64_t lines, int64_t cols, int e) { return (size_t)lines * whole(cols, e) * e; }
-
-// Copies of `bytes` are worth their time: launches and their bytes twice, against what the product loses without them, about as
-// long as it takes at a middling rate.  2048 x 1023 x 2049 bf16: 31 us, without 42; 1237 rows of 515 x 389 in 9 groups f32,
-// where they are not: 33 with, 25 without.
-bool worth_copies(int e, size_t bytes, double flops)
-{
-    return 5e-6 + 2.0 * bytes / 4.5e12 < 1.2 * flops / (e == 4 ? 0.8e14 : 0.5e15);
-}
 
 struct Matrix {
     const void *p;
@@ -213,29 +242,6 @@ int align_all(int32_t type, Matrix *const *all, int n, double flops, Scratch *s,
     *done = true;
     return NMF_OK;
 }
-// Scratch that they can take: of widths that do not fill 16 bytes, and of operands that `odd` says lie off their borders.
-size_t copies_of(int32_t type, size_t bytes, double flops) { return bytes && worth_copies(bytes_of(type), bytes, flops) ? bytes : 0; }
-bool ragged_rows(int64_t cols, int e) { return cols * e % 16 != 0; }
-size_t product_copies(int32_t type, int64_t rows, int64_t count, int64_t m, int64_t n, int64_t ktotal, int odd)
-{
-    const int e = bytes_of(type);
-    const bool bad_m = ragged_rows(m, e), bad_n = ragged_rows(n, e);
-    size_t b = 0;
-    if (bad_m || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
-    if (bad_m || bad_n || (odd & NMF_ODD_B)) b += std::max(copy_bytes(count * m, n, e), copy_bytes(count * n, m, e));
-    if (bad_m || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, m, e);
-    if (bad_n || (odd & NMF_ODD_FACTORS)) b += copy_bytes(ktotal, n, e);
-    return copies_of(type, b, 2.0 * rows * m * n);
-}
-size_t gradient_copies(int32_t type, int64_t rows, int64_t m, int64_t n, int odd)
-{
-    const int e = bytes_of(type);
-    size_t b = 0;
-    if (ragged_rows(m, e) || (odd & NMF_ODD_X)) b += copy_bytes(rows, m, e);
-    if (ragged_rows(n, e) || (odd & NMF_ODD_B)) b += copy_bytes(rows, n, e);
-    return copies_of(type, b, 2.0 * rows * m * n);
-}
-
 bool sizes_ok(int64_t rows, int64_t m, int64_t n) { return rows >= 0 && m > 0 && n > 0 && rows <= kMost && m <= kMost && n <= kMost; }
 
 template <class P> int launched(int32_t type, const P &p, void *stream, hipError_t (*f)(const P &, hipStream_t),
@@ -281,7 +287,7 @@ int nmf_grouped_product(int32_t type, const void *X, int64_t ldx, const int64_t 
     if (!aligned(X, e) || !aligned(B, e) || !aligned(Y, e) || !aligned(offsets, 8)) return set_error(NMF_EINVAL, "misaligned pointer");
     if (ldx < m || ldy < n || ldb < (transposed ? m : n) || stride_b < 0) return set_error(NMF_EINVAL, "leading dimension below the row's length");
     if (rows == 0) return NMF_OK;
-    const Plan plan = product_plan(type, rows, groups, m, n, false);
+    const Plan plan = product_plan(type, rows, groups, m, n);
     Product p = {};
     p.x = X; p.ldx = ldx; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
     p.b = B; p.ldb = ldb; p.stride_b = stride_b; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
@@ -354,7 +360,7 @@ int nmf_lowrank_product(int32_t type, const void *X, int64_t ldx, int64_t rows, 
         return set_error(NMF_EINVAL, "misaligned pointer");
     if (ldx < m || ldy < n || lda < (transposed ? m : n)) return set_error(NMF_EINVAL, "leading dimension below the row's length");
     if (rows == 0) return NMF_OK;
-    const Plan plan = product_plan(type, rows, 1, m, n, segments > 0);
+    const Plan plan = product_plan(type, rows, 1, m, n, segments, kmax);
     Product p = {};
     p.x = X; p.ldx = ldx; p.groups = 1; p.rows = rows; p.m = m; p.n = n;
     p.b = A; p.ldb = lda; p.transposed = transposed != 0; p.y = Y; p.ldy = ldy;
@@ -440,14 +446,14 @@ size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, in
     switch (kind - odd) {
     case 0: {
         if (parts < 1) return 0;
-        const int splits = product_plan(type, rows, parts, m, n, false).splits;
+        const int splits = product_plan(type, rows, parts, m, n).splits;
         return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0, odd);
     }
     case 1:
         return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n, odd);
     case 2: {
         if (parts < 0 || kmax < 1 || kmax > NMF_LOWRANK_MAX_K || ktotal < 0 || ktotal > kMost) return 0;
-        const int splits = product_plan(type, rows, 1, m, n, parts > 0).splits;
+        const int splits = product_plan(type, rows, 1, m, n, parts, kmax).splits;
         const size_t copies = product_copies(type, rows, 1, m, n, ktotal, odd);
         if (parts == 0) return (splits > 1 ? product_part(rows, n, splits) : 0) + copies;
         return (joined_plan(rows, n, parts, splits) ? product_part(rows, n, splits) : pack_part(rows, kmax)) +
