@@ -29,7 +29,8 @@
  *     access out of range.
  *   - Rows stand alone: what is not finite in one row, group or run reaches no other one's results.
  *   - Results may not overlap operands.  All calls are asynchronous on `stream`, allocate nothing, and
- *     share nothing: they may be made on several streams at once and captured into graphs.
+ *     share nothing: they may be made on several streams at once and captured into graphs.  All memory lies
+ *     on the current device, which is the stream's.
  *   - work: device scratch of the call alone, 16-byte aligned, nmf_ragged_work_bytes(...) bytes for the
  *     plan that is fastest; with less (also NULL, 0) the call uses a plan that fits (nmf_lowrank_product with
  *     long segments then adds their adapters by plain sums, much slower).  It must stay valid until the work
@@ -105,9 +106,10 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
  * ktotal: kinds 2 and 3 only.
  * To kinds 0 to 2 is added which operands lie off 16-byte borders, by their base pointer, leading dimension
  * or stride (their widths are seen from the sizes), so that there is room for copies of them:
- * NMF_ODD_X, NMF_ODD_B (B or A; dY for kind 1) and NMF_ODD_FACTORS (Wt or H).
+ * NMF_ODD_X, NMF_ODD_B (B or A; dY for kind 1) and NMF_ODD_FACTORS (Wt or H); and to kind 0 NMF_ONE_B where
+ * one matrix serves all groups (stride_b 0), of which there is one copy then.
  */
-enum { NMF_ODD_X = 16, NMF_ODD_B = 32, NMF_ODD_FACTORS = 64 };
+enum { NMF_ODD_X = 16, NMF_ODD_B = 32, NMF_ODD_FACTORS = 64, NMF_ONE_B = 128 };
 size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, int64_t n, int32_t parts,
                              int32_t runs, int32_t kmax, int64_t ktotal);
 

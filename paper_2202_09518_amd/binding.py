@@ -29,7 +29,7 @@ NMF_MU_MAX_K = 64
 NMF_MU_MAX_K_SLICED = 1024
 NMF_LOWRANK_MAX_K = 256
 NMF_F32, NMF_BF16, NMF_F16 = range(3)
-NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS = 16, 32, 64
+NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS, NMF_ONE_B = 16, 32, 64, 128
 
 _lib = None
 
@@ -307,7 +307,7 @@ def nmf_aht_w_update_dense(A, m, n, k, H, GH, W, eps, stream=None) -> None:
 # ---- products over ragged ranges of rows (include/nmfmu_ragged.h) ------------------
 # Types and leading dimensions are the tensors'; the scratch is torch's unless `work` (a uint8 device tensor) is given.  All
 # tensors lie on X's device, and the call runs there, whichever device is current.  `odd` tells the size query which operands lie off
-# 16-byte borders by their pointer, leading dimension or stride.
+# 16-byte borders by their pointer, leading dimension or stride, and whether one matrix serves all groups.
 
 _TYPES = {torch.float32: NMF_F32, torch.bfloat16: NMF_BF16, torch.float16: NMF_F16}
 
@@ -404,6 +404,8 @@ def nmf_grouped_product(X, offsets, groups, rows, B, transposed, m, n, Y, work=N
     y, ldy = _rows_of(Y, dt, d, rows, n, "Y")
     e = 4 if typ == NMF_F32 else 2
     odd = (NMF_ODD_X if (x | ldx * e) & 15 else 0) | (NMF_ODD_B if (b | (ldb | (stride_b if groups > 1 else 0)) * e) & 15 else 0)
+    if stride_b == 0:
+        odd |= NMF_ONE_B
     w, nbytes, _keep = _work(odd, typ, rows, m, n, groups, 0, 0, 0, work, d, stream)
     _check(lib().nmf_grouped_product(typ, x, ldx, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
                                      int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))

@@ -441,13 +441,13 @@ int nmf_lowrank_gradient(int32_t type, const void *X, int64_t ldx, const void *d
 size_t nmf_ragged_work_bytes(int kind, int32_t type, int64_t rows, int64_t m, int64_t n, int32_t parts, int32_t runs, int32_t kmax,
                              int64_t ktotal)
 {
-    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ODD_FACTORS);
+    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ODD_FACTORS | NMF_ONE_B);
     if (type < NMF_F32 || type > NMF_F16 || !sizes_ok(rows, m, n) || rows == 0) return 0;
     switch (kind - odd) {
     case 0: {
         if (parts < 1) return 0;
         const int splits = product_plan(type, rows, parts, m, n).splits;
-        return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, parts, m, n, 0, odd);
+        return (splits > 1 ? product_part(rows, n, splits) : 0) + product_copies(type, rows, odd & NMF_ONE_B ? 1 : parts, m, n, 0, odd);
     }
     case 1:
         return parts < 1 ? 0 : gradient_part(parts, m, n, gradient_plan(type, rows, parts, m, n).splits) + gradient_copies(type, rows, m, n, odd);

@@ -25,7 +25,7 @@ def test_scratch_has_room_for_copies_of_views():
     # widths that do not fill 16 bytes are in already; short products are not worth copies; other kinds are unknown
     assert wb(0 | nmf.NMF_ODD_X, nmf.NMF_BF16, rows, m - 1, n, 3) == wb(0, nmf.NMF_BF16, rows, m - 1, n, 3)
     assert wb(0 | nmf.NMF_ODD_X, nmf.NMF_BF16, 16, 256, 256, 1) == wb(0, nmf.NMF_BF16, 16, 256, 256, 1)
-    assert wb(4 | nmf.NMF_ODD_X, nmf.NMF_BF16, rows, m, n, 3) == 0 and wb(128, nmf.NMF_BF16, rows, m, n, 3) == 0
+    assert wb(4 | nmf.NMF_ODD_X, nmf.NMF_BF16, rows, m, n, 3) == 0 and wb(256, nmf.NMF_BF16, rows, m, n, 3) == 0
 
 
 @pytest.fixture
@@ -89,3 +89,20 @@ def test_lowrank_products_of_column_slices(typ, scratch):
     p.forward(Y)
     assert scratch[-1] >= (rows * m + m * n + p.ktotal * (m + n)) * e
     p.check_product(Y, p.X.double(), p.A.double(), p.Wt.double(), p.H.double(), p.U)
+
+
+@gpu
+@pytest.mark.parametrize("transposed", [False, True])
+def test_one_odd_matrix_for_many_groups_is_copied_once(transposed, scratch):
+    rows, groups, m, n = 2300, 40, 1023, 1537
+    g = torch.Generator(device="cuda").manual_seed(9)
+    cut = [rows * i // groups for i in range(groups + 1)]
+    X = torch.randn(rows, m, generator=g, device="cuda").bfloat16()
+    B = torch.randn(*((n, m) if transposed else (m, n)), generator=g, device="cuda").bfloat16()
+    Y = torch.empty(rows, n, dtype=torch.bfloat16, device="cuda")
+    nmf.nmf_grouped_product(X, torch.tensor(cut, device="cuda"), groups, rows, B.expand(groups, *B.shape), transposed, m, n, Y)
+    one = (rows * 1024 + 1024 * 1544) * 2                      # X and B in whole rows
+    assert one - 2 * 1544 * 2 <= scratch[-1] < 2 * one
+    x, w = X.double(), B.double()
+    w = w.t().contiguous() if transposed else w
+    within(Y, x @ w, x.abs() @ w.abs(), m, "bf16")
