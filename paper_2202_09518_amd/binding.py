@@ -22,13 +22,16 @@ EXPORTS = [
     "nmf_mu_workspace_bytes", "nmf_mu_set_workspace", "nmf_mu_release",
     "nmf_csr_partition", "nmf_split_planes", "nmf_csr_to_csc", "nmf_gram_w", "nmf_wta_dense", "nmf_h_update", "nmf_aht_w_update_dense",
     "nmf_grouped_product", "nmf_grouped_gradient", "nmf_lowrank_product", "nmf_lowrank_gradient", "nmf_ragged_work_bytes",
+    "nmf_rms_norm", "nmf_rms_norm_gradient", "nmf_round_blocks", "nmf_grouped_product8", "nmf_route", "nmf_route_gradient",
+    "nmf_spread_rows", "nmf_collect_rows", "nmf_collect_gradient", "nmf_routed_work_bytes",
 ]
 
 NMF_OK, NMF_EINVAL, NMF_ENOMEM, NMF_EHIP, NMF_EUNSUPPORTED = range(5)
 NMF_MU_MAX_K = 64
 NMF_MU_MAX_K_SLICED = 1024
 NMF_LOWRANK_MAX_K = 256
-NMF_F32, NMF_BF16, NMF_F16 = range(3)
+NMF_F32, NMF_BF16, NMF_F16, NMF_E4M3 = range(4)
+NMF_NORM_MAX_M, NMF_ROUTE_MAX_GROUPS, NMF_ROUTE_MAX_K = 32768, 1024, 16
 NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS, NMF_ONE_B = 16, 32, 64, 128
 
 _lib = None
@@ -87,6 +90,18 @@ def lib() -> ctypes.CDLL:
                                        ctypes.c_size_t, vp]
     L.nmf_ragged_work_bytes.restype = ctypes.c_size_t
     L.nmf_ragged_work_bytes.argtypes = [ctypes.c_int, i32, i64, i64, i64, i32, i32, i32, i64]
+    size = ctypes.c_size_t
+    L.nmf_rms_norm.argtypes = [i32, vp, i64, vp, i64, vp, i64, i64, f32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]
+    L.nmf_rms_norm_gradient.argtypes = [i32, vp, i64, vp, vp, vp, i64, vp, i64, i64, i64, vp, i64, vp, vp, size, vp]
+    L.nmf_round_blocks.argtypes = [i32, vp, i64, i64, i32, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp]
+    L.nmf_grouped_product8.argtypes = [i32, vp, i64, vp, i64, vp, i32, i64, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, i64, vp, size, vp]
+    L.nmf_route.argtypes = [i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, size, vp]
+    L.nmf_route_gradient.argtypes = [i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, i64, vp]
+    L.nmf_spread_rows.argtypes = [i32, vp, i64, i64, i32, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
+    L.nmf_collect_rows.argtypes = [i32, vp, i64, i64, i64, i32, vp, vp, i64, vp, i64, vp]
+    L.nmf_collect_gradient.argtypes = [i32, vp, i64, i64, i32, vp, vp, i64, vp, i64, i64, vp, i64, vp, vp]
+    L.nmf_routed_work_bytes.restype = size
+    L.nmf_routed_work_bytes.argtypes = [ctypes.c_int, i64, i64, i64, i32]
     for name in EXPORTS:
         fn = getattr(L, name)
         if fn.restype is ctypes.c_int and name not in ("nmf_status_string", "nmf_last_error"):
@@ -375,11 +390,14 @@ def _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal) -> int:
 
 def _work(kind, typ, rows, m, n, parts, runs, kmax, ktotal, work, device, stream):
     """(pointer, bytes, tensor to keep) of the scratch of a call."""
+    return _scratch(0 if work is not None else _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal), work, device, stream)
+
+
+def _scratch(need, work, device, stream):
     if work is not None:
         if not (work.get_device() == device and work.dtype == torch.uint8 and work.is_contiguous()):
             raise ValueError(f"work: need a contiguous uint8 tensor on device {device}")
         return work.data_ptr(), work.numel(), work
-    need = _need(kind, typ, rows, m, n, parts, runs, kmax, ktotal)
     if need == 0:
         return None, 0, None
     if stream is None:
@@ -462,3 +480,163 @@ def nmf_lowrank_gradient(X, dY, rows, m, n, offsets, run, segments, koff, runs, 
         segments, _list(koff, torch.int32, d, runs + 1, "koff"), runs, kmax, ktotal, _list(U, torch.float32, d, rows * kmax, "U"),
         _list(V, torch.float32, d, rows * kmax, "V"), _list(dWt, dt, d, ktotal * m, "dWt"), _list(dH, dt, d, ktotal * n, "dH"),
         w, nbytes, _stream_at(d, stream)))
+
+
+# ---- the rows' way to the products and back (include/nmfmu_routed.h) ----------------
+# As above: types and leading dimensions are the tensors', all of which lie on the first one's device.  Codes are float8_e4m3fn
+# (or uint8, the same bytes).
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _codes(t, what):
+    if t.dtype not in _CODES or not t.is_cuda:
+        raise ValueError(f"{what}: need a float8_e4m3fn or uint8 device tensor")
+    return t.dtype
+
+
+def _maybe_rows(t, dtype, device, rows, cols, what):
+    return (None, 0) if t is None else _rows_of(t, dtype, device, rows, cols, what)
+
+
+def _maybe_list(t, dtype, device, count, what):
+    return None if t is None else _list(t, dtype, device, count, what)
+
+
+@functools.lru_cache(maxsize=1024)
+def _need_routed(kind, rows, m, n, parts) -> int:
+    return int(lib().nmf_routed_work_bytes(kind, rows, m, n, parts))
+
+
+def nmf_routed_work_bytes(kind, rows, m, n=0, parts=0) -> int:
+    return int(lib().nmf_routed_work_bytes(kind, rows, m, n, parts))
+
+
+def nmf_rms_norm(X, rows, m, eps, weight=None, R=None, H=None, Y=None, Y8=None, scale=None, rstd=None, stream=None) -> None:
+    """H = X + R, Y = H weight / sqrt(mean H^2 + eps), in X's type (Y) and in 8 bits (Y8, scale); rstd: rows float32."""
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_rms_norm, X, rows, m, eps, weight, R, H, Y, Y8, scale, rstd, stream)
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    r, ldr = _maybe_rows(R, dt, d, rows, m, "R")
+    h, ldh = _maybe_rows(H, dt, d, rows, m, "H")
+    y, ldy = _maybe_rows(Y, dt, d, rows, m, "Y")
+    y8, ldy8 = (None, 0) if Y8 is None else _rows_of(Y8, _codes(Y8, "Y8"), d, rows, m, "Y8")
+    s, lds = _maybe_rows(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
+    _check(lib().nmf_rms_norm(typ, x, ldx, r, ldr, _maybe_list(weight, dt, d, m, "weight"), rows, m, eps, h, ldh, y, ldy, y8, ldy8, s, lds,
+                              _maybe_list(rstd, torch.float32, d, rows, "rstd"), _stream_at(d, stream)))
+
+
+def nmf_rms_norm_gradient(H, rstd, dY, rows, m, dX, weight=None, dH=None, dweight=None, work=None, stream=None) -> None:
+    """dX from dY (and dH, what reaches H on other ways), and the weight's gradient."""
+    typ, dt, d = _type(H, "H"), H.dtype, H.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_rms_norm_gradient, H, rstd, dY, rows, m, dX, weight, dH, dweight, work, stream)
+    h, ldh = _rows_of(H, dt, d, rows, m, "H")
+    dy, ldy = _rows_of(dY, dt, d, rows, m, "dY")
+    dh, lddh = _maybe_rows(dH, dt, d, rows, m, "dH")
+    dx, ldx = _rows_of(dX, dt, d, rows, m, "dX")
+    w, nbytes, _keep = _scratch(0 if dweight is None else _need_routed(1, rows, m, 0, 0), work, d, stream)
+    _check(lib().nmf_rms_norm_gradient(typ, h, ldh, _list(rstd, torch.float32, d, rows, "rstd"), _maybe_list(weight, dt, d, m, "weight"), dy, ldy,
+                                       dh, lddh, rows, m, dx, ldx, _maybe_list(dweight, dt, d, m, "dweight"), w, nbytes, _stream_at(d, stream)))
+
+
+def nmf_round_blocks(X, rows, m, block, X8, scale, stream=None) -> None:
+    """Codes and scales of blocks of block x 128 (1 or 128) of a matrix (rows x m) or of a stack of them (count x rows x m)."""
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_round_blocks, X, rows, m, block, X8, scale, stream)
+    lines, M = (rows + block - 1) // max(block, 1), (m + 127) // 128
+    codes = _codes(X8, "X8")
+    if X.dim() == 3:
+        count = X.shape[0]
+        x, ldx, stride = _stack_of(X, dt, d, count, rows, m, "X")
+        x8, ldx8, stride8 = _stack_of(X8, codes, d, count, rows, m, "X8")
+        s, lds, stride_s = _stack_of(scale, torch.float32, d, count, lines, M, "scale")
+    else:
+        count, stride, stride8, stride_s = 1, 0, 0, 0
+        x, ldx = _rows_of(X, dt, d, rows, m, "X")
+        x8, ldx8 = _rows_of(X8, codes, d, rows, m, "X8")
+        s, lds = _rows_of(scale, torch.float32, d, lines, M, "scale")
+    _check(lib().nmf_round_blocks(typ, x, ldx, stride, count, rows, m, block, x8, ldx8, stride8, s, lds, stride_s, _stream_at(d, stream)))
+
+
+def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transposed, m, n, Y, work=None, stream=None) -> None:
+    """Y_g = X_g B_g from codes and scales; B8: groups x m x n, or groups x n x m if transposed; the result has Y's type."""
+    typ, d = _type(Y, "Y"), X8.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_grouped_product8, X8, xscale, offsets, groups, rows, B8, bscale, transposed, m, n, Y, work, stream)
+    M, N = (m + 127) // 128, (n + 127) // 128
+    x, ldx = _rows_of(X8, _codes(X8, "X8"), d, rows, m, "X8")
+    xs, ldxs = _rows_of(xscale, torch.float32, d, rows, M, "xscale")
+    b, ldb, stride_b = _stack_of(B8, _codes(B8, "B8"), d, groups, *((n, m) if transposed else (m, n)), "B8")
+    bs, ldbs, stride_bs = _stack_of(bscale, torch.float32, d, groups, *((N, M) if transposed else (M, N)), "bscale")
+    y, ldy = _rows_of(Y, Y.dtype, d, rows, n, "Y")
+    w, nbytes, _keep = _scratch(_need_routed(2, rows, m, n, groups), work, d, stream)
+    _check(lib().nmf_grouped_product8(typ, x, ldx, xs, ldxs, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
+                                      bs, ldbs, stride_bs, int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))
+
+
+def nmf_route(logits, rows, groups, k, normalise, choice, gate, offsets, place, balance, work=None, stream=None) -> None:
+    """k groups of each row, gates, the groups' offsets, places of the sorted rows, and how unequal the groups are."""
+    typ, d = _type(logits, "logits"), logits.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_route, logits, rows, groups, k, normalise, choice, gate, offsets, place, balance, work, stream)
+    l, ldl = _rows_of(logits, logits.dtype, d, rows, groups, "logits")
+    w, nbytes, _keep = _scratch(_need_routed(0, rows, groups, 0, 0), work, d, stream)
+    _check(lib().nmf_route(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
+                           _list(gate, torch.float32, d, rows * k, "gate"), _list(offsets, torch.int64, d, groups + 1, "offsets"),
+                           _list(place, torch.int32, d, rows * k, "place"), _list(balance, torch.float32, d, 1, "balance"), w, nbytes,
+                           _stream_at(d, stream)))
+
+
+def nmf_route_gradient(logits, rows, groups, k, normalise, choice, offsets, dgate, dbalance, dlogits, stream=None) -> None:
+    """Gradient of the logits from those of the gates and of balance, either of which may be None."""
+    typ, d = _type(logits, "logits"), logits.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_route_gradient, logits, rows, groups, k, normalise, choice, offsets, dgate, dbalance, dlogits, stream)
+    l, ldl = _rows_of(logits, logits.dtype, d, rows, groups, "logits")
+    dl, lddl = _rows_of(dlogits, logits.dtype, d, rows, groups, "dlogits")
+    _check(lib().nmf_route_gradient(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
+                                    _list(offsets, torch.int64, d, groups + 1, "offsets"), _maybe_list(dgate, torch.float32, d, rows * k, "dgate"),
+                                    _maybe_list(dbalance, torch.float32, d, 1, "dbalance"), dl, lddl, _stream_at(d, stream)))
+
+
+def nmf_spread_rows(X, rows, k, place, m, Y, scale=None, Yscale=None, stream=None) -> None:
+    """Each row of X to its k places among Y's rows; codes take their scales along (scale to Yscale)."""
+    dt, d = X.dtype, X.get_device()
+    typ = NMF_E4M3 if dt in _CODES else _type(X, "X")
+    if d != _current_device():
+        return _call_on(d, nmf_spread_rows, X, rows, k, place, m, Y, scale, Yscale, stream)
+    x, ldx = _rows_of(X, dt, d, rows, m, "X")
+    count = Y.shape[0]
+    y, ldy = _rows_of(Y, dt, d, count, m, "Y")
+    xs, ldxs = _maybe_rows(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
+    ys, ldys = _maybe_rows(Yscale, torch.float32, d, count, (m + 127) // 128, "Yscale")
+    _check(lib().nmf_spread_rows(typ, x, ldx, rows, k, _list(place, torch.int32, d, rows * k, "place"), m, y, ldy, count, xs, ldxs, ys, ldys,
+                                 _stream_at(d, stream)))
+
+
+def nmf_collect_rows(X, rows, k, place, gate, m, Y, stream=None) -> None:
+    """Y[r] = sum over a row's choices of gate X[place]; gate None: 1."""
+    typ, dt, d = _type(X, "X"), X.dtype, X.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_collect_rows, X, rows, k, place, gate, m, Y, stream)
+    x, ldx = _rows_of(X, dt, d, X.shape[0], m, "X")
+    y, ldy = _rows_of(Y, dt, d, rows, m, "Y")
+    _check(lib().nmf_collect_rows(typ, x, ldx, X.shape[0], rows, k, _list(place, torch.int32, d, rows * k, "place"),
+                                  _maybe_list(gate, torch.float32, d, rows * k, "gate"), m, y, ldy, _stream_at(d, stream)))
+
+
+def nmf_collect_gradient(dY, rows, k, place, gate, m, dX, X=None, dgate=None, stream=None) -> None:
+    """dX[place] = gate dY[r], and with X and dgate the gates' gradients <dY[r], X[place]>."""
+    typ, dt, d = _type(dY, "dY"), dY.dtype, dY.get_device()
+    if d != _current_device():
+        return _call_on(d, nmf_collect_gradient, dY, rows, k, place, gate, m, dX, X, dgate, stream)
+    dy, ldy = _rows_of(dY, dt, d, rows, m, "dY")
+    count = dX.shape[0]
+    dx, lddx = _rows_of(dX, dt, d, count, m, "dX")
+    x, ldx = _maybe_rows(X, dt, d, count, m, "X")
+    _check(lib().nmf_collect_gradient(typ, dy, ldy, rows, k, _list(place, torch.int32, d, rows * k, "place"),
+                                      _maybe_list(gate, torch.float32, d, rows * k, "gate"), m, dx, lddx, count, x, ldx,
+                                      _maybe_list(dgate, torch.float32, d, rows * k, "dgate"), _stream_at(d, stream)))

@@ -9,10 +9,11 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnmfmu.so")
 SOURCES = ["nmfmu_dense.hip", "nmfmu_pairs.hip", "nmfmu_csr.hip", "nmfmu_api.hip",
-           "nmfmu_ragged_bf16.hip", "nmfmu_ragged_f16.hip", "nmfmu_ragged_f32.hip", "nmfmu_ragged_api.hip"]
+           "nmfmu_ragged_bf16.hip", "nmfmu_ragged_f16.hip", "nmfmu_ragged_f32.hip", "nmfmu_ragged_api.hip",
+           "nmfmu_rows.hip", "nmfmu_route.hip", "nmfmu_product8.hip", "nmfmu_routed_api.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("nmfmu_internal.h", "nmfmu_device.h", "nmfmu_ragged_internal.h", "nmfmu_ragged_device.h",
-                                           "nmfmu_ragged_kernels.h")] + \
-          [os.path.join(ROOT, "include", h) for h in ("nmfmu.h", "nmfmu_test.h", "nmfmu_ragged.h")]
+                                           "nmfmu_ragged_kernels.h", "nmfmu_routed_internal.h", "nmfmu_routed_device.h")] + \
+          [os.path.join(ROOT, "include", h) for h in ("nmfmu.h", "nmfmu_test.h", "nmfmu_ragged.h", "nmfmu_routed.h")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

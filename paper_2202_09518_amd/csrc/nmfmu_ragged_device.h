@@ -101,6 +101,10 @@ template <class T, int R> __device__ __forceinline__ int rc_shift(int k)
 {
     constexpr int pitch = R * Type<T>::kBytes;                // bytes of a row
     if (Type<T>::kBytes == 4) return pitch >= 256 ? ((k >> 2) & 1) * 4 : 0;
+    if (Type<T>::kBytes == 1) {                               // 32 lanes read 8 values of k twice, 16 apart, 16 bytes of each
+        constexpr int a = pitch >= 256 ? 0 : (pitch == 128 ? 1 : 2);
+        return (k & 7) >> a | ((k >> 4) & 1) << (3 - a);
+    }
     constexpr int b = pitch >= 256 ? 0 : (pitch == 128 ? 1 : 2);      // bits of k that choose a part of the 256 bytes
     return 2 * (((k & 3) >> b) | ((k >> 3) & 1) << (2 - b));
 }
@@ -128,6 +132,10 @@ template <class T> __device__ __forceinline__ u32x4 chunk_at(const char *at, int
     } else if (Type<T>::kBytes == 4) {
         for (int i = 0; i < 3; ++i)
             if (4 * i + 4 <= bytes) __builtin_memcpy((char *)&v + 4 * i, at + 4 * i, 4);
+    } else if (Type<T>::kBytes == 1) {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+            if (i < bytes) v[i >> 2] |= (unsigned)(unsigned char)at[i] << (8 * (i & 3));
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -148,6 +156,7 @@ template <class T> __device__ __forceinline__ u32x4 keep_first(u32x4 v, int64_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (Type<T>::kBytes == 4) v[i] = i < keep ? v[i] : 0u;
+        else if (Type<T>::kBytes == 1) v[i] &= keep >= 4 * i + 4 ? 0xffffffffu : (keep > 4 * i ? (1u << (8 * (int)(keep - 4 * i))) - 1u : 0u);
         else v[i] &= (2 * i < keep ? 0xffffu : 0u) | (2 * i + 1 < keep ? 0xffff0000u : 0u);
     }
     return v;
@@ -268,7 +277,7 @@ template <class T, int R, bool RC, int STEP> struct Reader {
         if (!RC) return *reinterpret_cast<const u32x4 *>(lds + at[kk] + t * STEP * kStageBytes);
         constexpr int pitch = R * Type<T>::kBytes;
         u32x4 v;
-        if (Type<T>::kBytes == 2) {
+        if constexpr (Type<T>::kBytes == 2) {
             // 16 lanes read 4 values of k x 16 columns, and each leaves with the 4 k of one column
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -277,6 +286,15 @@ template <class T, int R, bool RC, int STEP> struct Reader {
             const char *p = lds + (32 * kk + k) * pitch + (((col >> 3) ^ rc_shift<T, R>(k)) << 4) + (col & 7) * 2;
             const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
             const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * pitch)));
+            v = u32x4{a[0], a[1], b[0], b[1]};
+        } else if constexpr (Type<T>::kBytes == 1) {
+            // 16 lanes read 8 values of k x 16 columns, and each leaves with the 8 k of one column
+            typedef int i32x2 __attribute__((ext_vector_type(2)));
+            typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+            const int i = lane & 15, k = 64 * kk + 16 * (lane >> 4) + (i >> 1), c = (first + t * STEP) >> 4;
+            const char *p = lds + k * pitch + ((c ^ rc_shift<T, R>(k)) << 4) + (i & 1) * 8;      // (the shift of k + 8 is that of k)
+            const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)p));
+            const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p + 8 * pitch)));
             v = u32x4{a[0], a[1], b[0], b[1]};
         } else {
             const int col = first + t * STEP + (lane & 15);

@@ -1,0 +1,326 @@
+// C ABI of the norm, routing, the rows' way to their groups and products in 8 bits: argument checks and plans.
+// Public contract: include/nmfmu_routed.h.
+#include "nmfmu_routed.h"
+#include "nmfmu_internal.h"
+#include "nmfmu_routed_internal.h"
+
+#include <algorithm>
+
+using namespace nmfmu;
+using namespace nmfmu::routed;
+using namespace nmfmu::ragged;
+
+namespace {
+
+constexpr int64_t kMost = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 23) - 1;
+constexpr int kComputeUnits = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int bytes_of(int32_t type) { return type == NMF_F32 ? 4 : 2; }
+bool aligned(const void *p, int to) { return ((uintptr_t)p & (to - 1)) == 0; }
+bool size_ok(int64_t n) { return n > 0 && n <= kMost; }
+bool rows_ok(int64_t n) { return n >= 0 && n <= kMost; }
+
+int check_type(int32_t type) { return type >= NMF_F32 && type <= NMF_F16 ? NMF_OK : set_error(NMF_EINVAL, "unknown type"); }
+int check_work(const void *work, size_t bytes)
+{
+    if (bytes && !work) return set_error(NMF_EINVAL, "work is null but work_bytes is not 0");
+    if (!aligned(work, 16)) return set_error(NMF_EINVAL, "work must be 16-byte aligned");
+    return NMF_OK;
+}
+int bad(const char *what) { return set_error(NMF_EINVAL, what); }
+
+const char *const kSizes = "sizes must be positive and below 2^31", *const kNull = "null pointer", *const kMisaligned = "misaligned pointer",
+                  *const kShort = "leading dimension below the row's length";
+
+int launched(hipError_t e) { return e == hipSuccess ? NMF_OK : set_error(NMF_EHIP, hipGetErrorString(e)); }
+template <class P>
+int launched(int32_t type, const P &p, void *stream, hipError_t (*f)(const P &, hipStream_t), hipError_t (*b)(const P &, hipStream_t),
+             hipError_t (*h)(const P &, hipStream_t))
+{
+    return launched((type == NMF_F32 ? f : type == NMF_BF16 ? b : h)(p, static_cast<hipStream_t>(stream)));
+}
+
+// ---- plans ---------------------------------------------------------------------------------
+
+// Rows that one workgroup takes rather than three launches.
+constexpr int64_t kRouteAlone = 64;
+
+size_t route_bytes(int64_t blocks, int64_t groups)
+{
+    const int64_t each = ceil_div(blocks * groups, 4) * 4;
+    return (size_t)(each * 8 + groups * 16);
+}
+
+size_t norm_bytes(int64_t parts, int64_t m) { return parts > 1 ? (size_t)(parts * m * 4) : 0; }
+
+struct Plan {
+    int shape, splits;
+};
+
+// Time of `tiles` tiles of a shape: those of the busiest compute unit, by their size and by what share of the large tile's rate
+// they reach.
+double tile_time(int shape, int64_t tiles)
+{
+    static const double rate[] = {1.0, 0.72, 0.5};
+    return (double)ceil_div(tiles, kComputeUnits) * kTileRows[shape] * kTileCols[shape] / rate[std::min(shape, 2)];
+}
+
+// large: the 256 x 256 tile can be had.
+Plan product_plan(int64_t rows, int64_t groups, int64_t m, int64_t n, bool large)
+{
+    groups = std::max<int64_t>(1, std::min(groups, rows));
+    const int64_t avg = ceil_div(rows, groups);
+    auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
+    Plan p;
+    if (avg <= 32) p.shape = k32x128;
+    else if (avg <= 64) p.shape = k64x128;
+    else {
+        p.shape = large ? k256x256 : k128x128;
+        for (int shape : {k128x128, k64x64})
+            if (tile_time(shape, tiles(shape)) < tile_time(p.shape, tiles(p.shape))) p.shape = shape;
+    }
+    const int64_t want = kComputeUnits / std::max<int64_t>(tiles(p.shape), 1), have = m / (4 * 128);
+    const int64_t s = p.shape == k256x256 ? 1 : std::min<int64_t>(std::min(want, have), kMaxSplits);
+    p.splits = s < 2 ? 1 : (int)s;
+    return p;
+}
+size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (size_t)splits * rows * up4(n) * 4 : 0; }
+
+// A matrix of entries of e bytes: rows x cols, ld from row to row.
+int check_matrix(const void *p, int64_t ld, int64_t rows, int64_t cols, int e)
+{
+    if (rows && !p) return bad(kNull);
+    if (!aligned(p, e)) return bad(kMisaligned);
+    if (ld < cols) return bad(kShort);
+    return NMF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nmf_rms_norm(int32_t type, const void *X, int64_t ldx, const void *R, int64_t ldr, const void *weight, int64_t rows, int64_t m,
+                 float eps, void *H, int64_t ldh, void *Y, int64_t ldy, void *Y8, int64_t ldy8, float *scale, int64_t lds,
+                 float *rstd, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !size_ok(m)) return bad(kSizes);
+    if (m > NMF_NORM_MAX_M) return set_error(NMF_EUNSUPPORTED, "more columns than NMF_NORM_MAX_M");
+    if (!(eps >= 0.f)) return bad("eps must not be negative");
+    const int e = bytes_of(type);
+    if ((rc = check_matrix(X, ldx, rows, m, e))) return rc;
+    if (R && (rc = check_matrix(R, ldr, rows, m, e))) return rc;
+    if (H && (rc = check_matrix(H, ldh, rows, m, e))) return rc;
+    if (Y && (rc = check_matrix(Y, ldy, rows, m, e))) return rc;
+    if ((Y8 == nullptr) != (scale == nullptr)) return bad("Y8 and scale: both or neither");
+    if (Y8 && ((rc = check_matrix(Y8, ldy8, rows, m, 1)) || (rc = check_matrix(scale, lds, rows, blocks_of(m), 4)))) return rc;
+    if (rows && !Y && !Y8) return bad("neither Y nor Y8");
+    if (!aligned(weight, e) || !aligned(rstd, 4)) return bad(kMisaligned);
+    if ((H && H == X && ldh != ldx) || (H && H == R && ldh != ldr)) return bad("H in the place of an operand must have its leading dimension");
+    if (rows == 0) return NMF_OK;
+    Norm a = {};
+    a.x = X; a.r = R; a.w = weight; a.ldx = ldx; a.ldr = ldr; a.rows = rows; a.m = m; a.eps = eps;
+    a.h = H; a.y = Y; a.y8 = Y8; a.ldh = ldh; a.ldy = ldy; a.ldy8 = ldy8; a.lds = lds; a.scale = scale; a.rstd = rstd;
+    return launched(type, a, stream, launch_norm<float>, launch_norm<bf16_t>, launch_norm<f16_t>);
+}
+
+int nmf_rms_norm_gradient(int32_t type, const void *H, int64_t ldh, const float *rstd, const void *weight, const void *dY,
+                          int64_t ldy, const void *dH, int64_t lddh, int64_t rows, int64_t m, void *dX, int64_t ldx, void *dweight,
+                          void *work, size_t work_bytes, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !size_ok(m)) return bad(kSizes);
+    if (m > NMF_NORM_MAX_M) return set_error(NMF_EUNSUPPORTED, "more columns than NMF_NORM_MAX_M");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    const int e = bytes_of(type);
+    if ((rc = check_matrix(H, ldh, rows, m, e)) || (rc = check_matrix(dY, ldy, rows, m, e)) || (rc = check_matrix(dX, ldx, rows, m, e))) return rc;
+    if (dH && (rc = check_matrix(dH, lddh, rows, m, e))) return rc;
+    if (rows && !rstd) return bad(kNull);
+    if (!aligned(weight, e) || !aligned(dweight, e) || !aligned(rstd, 4)) return bad(kMisaligned);
+    if ((dX && dX == dH && ldx != lddh) || (dX && dX == dY && ldx != ldy)) return bad("dX in the place of an operand must have its leading dimension");
+    if (rows == 0 && !dweight) return NMF_OK;
+    NormGradient a = {};
+    a.h = H; a.w = weight; a.dy = dY; a.dh = dH; a.rstd = rstd; a.ldh = ldh; a.ldy = ldy; a.lddh = lddh; a.ldx = ldx; a.rows = rows; a.m = m;
+    a.dx = dX; a.dw = dweight;
+    a.parts = norm_parts(rows, m);
+    if (norm_bytes(a.parts, m) > work_bytes) a.parts = (int)std::max<int64_t>(1, (int64_t)(work_bytes / ((size_t)m * 4)));
+    a.part = a.parts > 1 ? static_cast<float *>(work) : nullptr;
+    return launched(type, a, stream, launch_norm_gradient<float>, launch_norm_gradient<bf16_t>, launch_norm_gradient<f16_t>);
+}
+
+int nmf_round_blocks(int32_t type, const void *X, int64_t ldx, int64_t stride, int32_t count, int64_t rows, int64_t m, int32_t block,
+                     void *X8, int64_t ldx8, int64_t stride8, float *scale, int64_t lds, int64_t stride_s, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !size_ok(m) || count < 1) return bad(kSizes);
+    if (block != 1 && block != 128) return bad("block must be 1 or 128");
+    const int64_t lines = ceil_div(rows, block), M = blocks_of(m);
+    if ((rc = check_matrix(X, ldx, rows, m, bytes_of(type))) || (rc = check_matrix(X8, ldx8, rows, m, 1)) || (rc = check_matrix(scale, lds, lines, M, 4)))
+        return rc;
+    if (rows == 0) return NMF_OK;
+    if (count > 1 && (stride < 0 || stride8 < (rows - 1) * ldx8 + m || stride_s < (lines - 1) * lds + M)) return bad("results that overlap");
+    if ((__int128)count * rows * M > ((__int128)1 << 62)) return set_error(NMF_EUNSUPPORTED, "too many blocks");
+    Round a = {};
+    a.x = X; a.ldx = ldx; a.stride = stride; a.rows = rows; a.m = m; a.count = count; a.block = block;
+    a.x8 = X8; a.ldx8 = ldx8; a.stride8 = stride8; a.scale = scale; a.lds = lds; a.stride_s = stride_s;
+    return launched(type, a, stream, launch_round<float>, launch_round<bf16_t>, launch_round<f16_t>);
+}
+
+int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float *xscale, int64_t ldxs, const int64_t *offsets,
+                         int32_t groups, int64_t rows, const void *B8, int64_t ldb, int64_t stride_b, const float *bscale, int64_t ldbs,
+                         int64_t stride_bs, int32_t transposed, int64_t m, int64_t n, void *Y, int64_t ldy, void *work, size_t work_bytes,
+                         void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !size_ok(m) || !size_ok(n) || groups < 1) return bad(kSizes);
+    if ((rc = check_work(work, work_bytes))) return rc;
+    const int e = bytes_of(type);
+    const int64_t b_rows = transposed ? n : m, b_cols = transposed ? m : n;
+    if ((rc = check_matrix(X8, ldx, rows, m, 1)) || (rc = check_matrix(xscale, ldxs, rows, blocks_of(m), 4)) ||
+        (rc = check_matrix(B8, ldb, b_rows, b_cols, 1)) || (rc = check_matrix(bscale, ldbs, blocks_of(b_rows), blocks_of(b_cols), 4)) ||
+        (rc = check_matrix(Y, ldy, rows, n, e)))
+        return rc;
+    if (!offsets) return bad(kNull);
+    if (!aligned(offsets, 8)) return bad(kMisaligned);
+    if (stride_b < 0 || stride_bs < 0) return bad("negative stride");
+    if (rows == 0) return NMF_OK;
+    // chunks of 16 bytes go to LDS without passing registers where rows begin and end on 16-byte borders, and distances fit 32 bits
+    const int64_t far = (int64_t)1 << 30;
+    const bool dma = aligned(X8, 16) && aligned(B8, 16) && (ldx | ldb | (groups > 1 ? stride_b : 0) | m | (transposed ? 0 : n)) % 16 == 0 &&
+                     ldx * 256 < far && ldb * 256 < far && ldxs * 4 * 256 < far;
+    const Plan plan = product_plan(rows, groups, m, n, dma && type != NMF_F32);
+    Product8 p = {};
+    p.x = X8; p.ldx = ldx; p.xs = xscale; p.ldxs = ldxs; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
+    p.b = B8; p.ldb = ldb; p.stride_b = stride_b; p.bs = bscale; p.ldbs = ldbs; p.stride_bs = stride_bs; p.transposed = transposed != 0;
+    p.type = type; p.y = Y; p.ldy = ldy;
+    p.dma = dma;
+    p.shape = plan.shape;
+    p.splits = plan.splits;
+    while (p.splits > 1 && product_part(rows, n, p.splits) > work_bytes) --p.splits;
+    p.part = static_cast<float *>(work);
+    p.k_split = ceil_div(blocks_of(m), p.splits);
+    p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
+    const int64_t grid = (ceil_div(rows, kTileRows[p.shape]) + groups) * ceil_div(n, kTileCols[p.shape]) * p.splits;
+    if (std::max(grid, p.splits > 1 ? rows * ceil_div(n, 1024) : 0) > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
+    return launched(launch_product8(p, static_cast<hipStream_t>(stream)));
+}
+
+int nmf_route(int32_t type, const void *logits, int64_t ldl, int64_t rows, int32_t groups, int32_t k, int32_t normalise,
+              int32_t *choice, float *gate, int64_t *offsets, int32_t *place, float *balance, void *work, size_t work_bytes,
+              void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || groups < 1 || k < 1 || k > groups || rows * k > kMost) return bad("sizes must be positive and below 2^31, and k at most groups");
+    if (groups > NMF_ROUTE_MAX_GROUPS || k > NMF_ROUTE_MAX_K) return set_error(NMF_EUNSUPPORTED, "more groups or choices than the limits");
+    if ((rc = check_work(work, work_bytes))) return rc;
+    if ((rc = check_matrix(logits, ldl, rows, groups, bytes_of(type)))) return rc;
+    if (!offsets || !balance || (rows && (!choice || !gate || !place))) return bad(kNull);
+    if (!aligned(choice, 4) || !aligned(gate, 4) || !aligned(place, 4) || !aligned(balance, 4) || !aligned(offsets, 8)) return bad(kMisaligned);
+    Route a = {};
+    a.logits = logits; a.ldl = ldl; a.rows = rows; a.groups = groups; a.k = k; a.normalise = normalise != 0;
+    a.choice = choice; a.gate = gate; a.offsets = offsets; a.place = place; a.balance = balance;
+    a.blocks = ceil_div(rows, kRouteRows);
+    if (a.blocks > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more rows than one launch can have");
+    if (rows > kRouteAlone && route_bytes(a.blocks, groups) <= work_bytes) {
+        const int64_t each = ceil_div(a.blocks * groups, 4) * 4;
+        a.total = static_cast<int64_t *>(work);
+        a.mass = reinterpret_cast<double *>(a.total + groups);
+        a.count = reinterpret_cast<int32_t *>(a.mass + groups);
+        a.share = reinterpret_cast<float *>(a.count + each);
+    }
+    return launched(type, a, stream, launch_route<float>, launch_route<bf16_t>, launch_route<f16_t>);
+}
+
+int nmf_route_gradient(int32_t type, const void *logits, int64_t ldl, int64_t rows, int32_t groups, int32_t k, int32_t normalise,
+                       const int32_t *choice, const int64_t *offsets, const float *dgate, const float *dbalance, void *dlogits,
+                       int64_t lddl, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || groups < 1 || k < 1 || k > groups || rows * k > kMost) return bad("sizes must be positive and below 2^31, and k at most groups");
+    if (groups > NMF_ROUTE_MAX_GROUPS || k > NMF_ROUTE_MAX_K) return set_error(NMF_EUNSUPPORTED, "more groups or choices than the limits");
+    const int e = bytes_of(type);
+    if ((rc = check_matrix(logits, ldl, rows, groups, e)) || (rc = check_matrix(dlogits, lddl, rows, groups, e))) return rc;
+    if (!offsets || (rows && !choice)) return bad(kNull);
+    if (!aligned(choice, 4) || !aligned(dgate, 4) || !aligned(dbalance, 4) || !aligned(offsets, 8)) return bad(kMisaligned);
+    if (rows == 0) return NMF_OK;
+    RouteGradient a = {};
+    a.logits = logits; a.ldl = ldl; a.rows = rows; a.lddl = lddl; a.groups = groups; a.k = k; a.normalise = normalise != 0;
+    a.choice = choice; a.offsets = offsets; a.dgate = dgate; a.dbalance = dbalance; a.dlogits = dlogits;
+    return launched(type, a, stream, launch_route_gradient<float>, launch_route_gradient<bf16_t>, launch_route_gradient<f16_t>);
+}
+
+int nmf_spread_rows(int32_t type, const void *X, int64_t ldx, int64_t rows, int32_t k, const int32_t *place, int64_t m, void *Y, int64_t ldy,
+                    int64_t sorted, const float *xscale, int64_t ldxs, float *yscale, int64_t ldys, void *stream)
+{
+    int rc = type == NMF_E4M3 ? NMF_OK : check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !rows_ok(sorted) || !size_ok(m) || k < 1 || rows * k > kMost) return bad(kSizes);
+    const int e = type == NMF_E4M3 ? 1 : bytes_of(type);
+    if ((rc = check_matrix(X, ldx, rows, m, e)) || (rc = check_matrix(Y, ldy, sorted, m, e))) return rc;
+    if (rows && !place) return bad(kNull);
+    if (!aligned(place, 4)) return bad(kMisaligned);
+    if (type == NMF_E4M3) {
+        if ((rc = check_matrix(xscale, ldxs, rows, blocks_of(m), 4)) || (rc = check_matrix(yscale, ldys, sorted, blocks_of(m), 4))) return rc;
+    } else if (xscale || yscale) {
+        return bad("scales are those of codes");
+    }
+    if (rows == 0 || sorted == 0) return NMF_OK;
+    Spread a = {};
+    a.x = X; a.ldx = ldx * e; a.rows = rows; a.m = m * e; a.ldy = ldy * e; a.sorted = sorted; a.k = k; a.place = place; a.y = Y;
+    if (type == NMF_E4M3) { a.xs = xscale; a.ldxs = ldxs; a.ys = yscale; a.ldys = ldys; a.ms = blocks_of(m); }
+    return launched(launch_spread(a, static_cast<hipStream_t>(stream)));
+}
+
+int nmf_collect_rows(int32_t type, const void *X, int64_t ldx, int64_t sorted, int64_t rows, int32_t k, const int32_t *place,
+                     const float *gate, int64_t m, void *Y, int64_t ldy, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !rows_ok(sorted) || !size_ok(m) || k < 1 || rows * k > kMost) return bad(kSizes);
+    const int e = bytes_of(type);
+    if ((rc = check_matrix(X, ldx, sorted, m, e)) || (rc = check_matrix(Y, ldy, rows, m, e))) return rc;
+    if (rows && !place) return bad(kNull);
+    if (!aligned(place, 4) || !aligned(gate, 4)) return bad(kMisaligned);
+    if (rows == 0) return NMF_OK;
+    Collect a = {};
+    a.x = X; a.ldx = ldx; a.sorted = sorted; a.rows = rows; a.m = m; a.ldy = ldy; a.k = k; a.place = place; a.gate = gate; a.y = Y;
+    return launched(type, a, stream, launch_collect<float>, launch_collect<bf16_t>, launch_collect<f16_t>);
+}
+
+int nmf_collect_gradient(int32_t type, const void *dY, int64_t ldy, int64_t rows, int32_t k, const int32_t *place, const float *gate,
+                         int64_t m, void *dX, int64_t lddx, int64_t sorted, const void *X, int64_t ldx, float *dgate, void *stream)
+{
+    int rc = check_type(type);
+    if (rc) return rc;
+    if (!rows_ok(rows) || !rows_ok(sorted) || !size_ok(m) || k < 1 || rows * k > kMost) return bad(kSizes);
+    const int e = bytes_of(type);
+    if ((rc = check_matrix(dY, ldy, rows, m, e)) || (rc = check_matrix(dX, lddx, sorted, m, e))) return rc;
+    if (dgate && (rc = check_matrix(X, ldx, sorted, m, e))) return rc;
+    if (!dgate && X) return bad("X and dgate: both or neither");
+    if (rows && !place) return bad(kNull);
+    if (!aligned(place, 4) || !aligned(gate, 4) || !aligned(dgate, 4)) return bad(kMisaligned);
+    if (rows == 0) return NMF_OK;
+    CollectGradient a = {};
+    a.dy = dY; a.x = X; a.ldy = ldy; a.rows = rows; a.m = m; a.lddx = lddx; a.sorted = sorted; a.ldx = ldx; a.k = k; a.place = place;
+    a.gate = gate; a.dx = dX; a.dgate = dgate;
+    return launched(type, a, stream, launch_collect_gradient<float>, launch_collect_gradient<bf16_t>, launch_collect_gradient<f16_t>);
+}
+
+size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts)
+{
+    if (!size_ok(rows) || !size_ok(m)) return 0;
+    if (kind == 0) return rows > kRouteAlone && m <= NMF_ROUTE_MAX_GROUPS ? route_bytes(ceil_div(rows, kRouteRows), m) : 0;
+    if (kind == 1) return m <= NMF_NORM_MAX_M ? norm_bytes(norm_parts(rows, m), m) : 0;
+    if (kind != 2 || !size_ok(n) || parts < 1) return 0;
+    return std::max(product_part(rows, n, product_plan(rows, parts, m, n, true).splits), product_part(rows, n, product_plan(rows, parts, m, n, false).splits));
+}
+
+}  // extern "C"

@@ -1,0 +1,322 @@
+"""Calls of the norm, routing, the rows' way to their groups and products in 8 bits: refusals, sizes of scratch, streams, capture,
+and a run of all of them together, forward and backward."""
+import math
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2202_09518_amd as nmf
+
+gpu = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P, Q, O, Z = 4096, 8192, 12288, 16384            # addresses that are never touched
+BIG = 2 ** 31
+E8 = torch.float8_e4m3fn
+
+
+# ---- refusals, by the arguments alone ------------------------------------------------------------
+
+GOOD = {
+    "nmf_rms_norm": dict(type=0, X=P, ldx=8, R=Q, ldr=8, weight=P, rows=4, m=8, eps=1e-6, H=O, ldh=8, Y=Z, ldy=8, Y8=P, ldy8=8, scale=P, lds=1, rstd=P, stream=0),
+    "nmf_rms_norm_gradient": dict(type=0, H=P, ldh=8, rstd=P, weight=P, dY=P, ldy=8, dH=Q, lddh=8, rows=4, m=8, dX=O, ldx=8, dweight=P, work=0, work_bytes=0, stream=0),
+    "nmf_round_blocks": dict(type=0, X=P, ldx=8, stride=32, count=2, rows=4, m=8, block=128, X8=Q, ldx8=8, stride8=32, scale=P, lds=1, stride_s=1, stream=0),
+    "nmf_grouped_product8": dict(type=0, X8=P, ldx=8, xscale=P, ldxs=1, offsets=P, groups=2, rows=4, B8=P, ldb=16, stride_b=128, bscale=P, ldbs=1, stride_bs=1,
+                                 transposed=0, m=8, n=16, Y=Q, ldy=16, work=0, work_bytes=0, stream=0),
+    "nmf_route": dict(type=0, logits=P, ldl=8, rows=4, groups=8, k=2, normalise=1, choice=P, gate=P, offsets=P, place=P, balance=P, work=0, work_bytes=0, stream=0),
+    "nmf_route_gradient": dict(type=0, logits=P, ldl=8, rows=4, groups=8, k=2, normalise=1, choice=P, offsets=P, dgate=P, dbalance=P, dlogits=Q, lddl=8, stream=0),
+    "nmf_spread_rows": dict(type=0, X=P, ldx=8, rows=4, k=2, place=P, m=8, Y=Q, ldy=8, sorted=8, xscale=0, ldxs=0, yscale=0, ldys=0, stream=0),
+    "nmf_collect_rows": dict(type=0, X=P, ldx=8, sorted=8, rows=4, k=2, place=P, gate=P, m=8, Y=Q, ldy=8, stream=0),
+    "nmf_collect_gradient": dict(type=0, dY=P, ldy=8, rows=4, k=2, place=P, gate=P, m=8, dX=Q, lddx=8, sorted=8, X=P, ldx=8, dgate=P, stream=0),
+}
+REFUSED = {
+    "nmf_rms_norm": [dict(type=3), dict(type=-1), dict(rows=-1), dict(rows=BIG), dict(m=0), dict(eps=-1.0), dict(eps=math.nan), dict(X=0), dict(X=P + 2), dict(ldx=7),
+                     dict(R=P + 1), dict(ldr=7), dict(weight=P + 2), dict(ldh=7), dict(H=O + 2), dict(Y=0, Y8=0, scale=0), dict(Y8=0), dict(scale=0),
+                     dict(scale=P + 2), dict(m=129, ldx=129, ldr=129, ldh=129, ldy=129, ldy8=129, lds=1), dict(ldy8=7), dict(rstd=P + 1), dict(H=P, ldh=9), dict(H=Q, ldh=9),
+                     dict(type=1, X=P + 1)],
+    "nmf_rms_norm_gradient": [dict(type=3), dict(rows=-1), dict(m=0), dict(H=0), dict(dY=0), dict(dX=0), dict(rstd=0), dict(ldh=7), dict(ldy=7), dict(lddh=7), dict(ldx=7),
+                              dict(dX=P, ldx=9), dict(dX=Q, ldx=9), dict(work=0, work_bytes=64), dict(work=P + 8, work_bytes=64), dict(weight=P + 1), dict(dweight=P + 1)],
+    "nmf_round_blocks": [dict(type=3), dict(rows=-1), dict(m=0), dict(count=0), dict(block=0), dict(block=64), dict(X=0), dict(X8=0), dict(scale=0), dict(ldx=7), dict(ldx8=7),
+                         dict(lds=0), dict(stride8=31), dict(stride_s=0), dict(stride=-1), dict(X=P + 3)],
+    "nmf_grouped_product8": [dict(type=3), dict(rows=-1), dict(rows=BIG), dict(m=0), dict(n=0), dict(groups=0), dict(X8=0), dict(xscale=0), dict(B8=0), dict(bscale=0), dict(Y=0),
+                             dict(offsets=0), dict(offsets=P + 4), dict(ldx=7), dict(ldxs=0), dict(ldb=15), dict(transposed=1, ldb=7), dict(ldbs=0), dict(ldy=15),
+                             dict(stride_b=-1), dict(stride_bs=-1), dict(xscale=P + 2), dict(Y=Q + 2), dict(work=0, work_bytes=16), dict(work=P + 4, work_bytes=16)],
+    "nmf_route": [dict(type=3), dict(rows=-1), dict(groups=0, k=0), dict(k=0), dict(k=9), dict(rows=BIG - 1), dict(logits=0), dict(ldl=7), dict(choice=0), dict(gate=0),
+                  dict(offsets=0), dict(place=0), dict(balance=0), dict(offsets=P + 4), dict(place=P + 2), dict(work=0, work_bytes=16), dict(work=P + 8, work_bytes=16)],
+    "nmf_route_gradient": [dict(type=3), dict(rows=-1), dict(k=0), dict(k=9), dict(logits=0), dict(dlogits=0), dict(choice=0), dict(offsets=0), dict(ldl=7), dict(lddl=7),
+                           dict(dgate=P + 2), dict(dbalance=P + 1)],
+    "nmf_spread_rows": [dict(type=4), dict(rows=-1), dict(sorted=-1), dict(m=0), dict(k=0), dict(rows=BIG - 1), dict(X=0), dict(Y=0), dict(place=0), dict(ldx=7), dict(ldy=7),
+                        dict(xscale=P, ldxs=1), dict(yscale=P, ldys=1), dict(type=3), dict(type=3, xscale=P, ldxs=1), dict(type=3, xscale=P, ldxs=0, yscale=P, ldys=1)],
+    "nmf_collect_rows": [dict(type=3), dict(rows=-1), dict(sorted=-1), dict(m=0), dict(k=0), dict(X=0), dict(Y=0), dict(place=0), dict(place=P + 1), dict(gate=P + 2), dict(ldx=7), dict(ldy=7)],
+    "nmf_collect_gradient": [dict(type=3), dict(rows=-1), dict(sorted=-1), dict(m=0), dict(k=0), dict(dY=0), dict(dX=0), dict(X=0), dict(dgate=0), dict(place=0), dict(ldy=7),
+                             dict(lddx=7), dict(ldx=7)],
+}
+TOO_MUCH = {
+    "nmf_rms_norm": [{v: 32769 for v in ("m", "ldx", "ldr", "ldh", "ldy", "ldy8")} | dict(lds=257)],
+    "nmf_rms_norm_gradient": [{v: 32769 for v in ("m", "ldx", "ldh", "ldy", "lddh")}],
+    "nmf_grouped_product8": [dict(rows=2 ** 30, n=2 ** 20, ldy=2 ** 20, ldb=2 ** 20, ldbs=2 ** 13)],
+    "nmf_route": [dict(groups=1025, ldl=1025), dict(groups=64, ldl=64, k=17), dict(rows=2 ** 30, k=1)],
+    "nmf_route_gradient": [dict(groups=1025, ldl=1025, lddl=1025), dict(groups=64, ldl=64, lddl=64, k=17)],
+}
+
+
+def status(name, **change):
+    return getattr(nmf.lib(), name)(*{**GOOD[name], **change}.values())
+
+
+@pytest.mark.parametrize("name", sorted(GOOD))
+def test_refusals(name):
+    for change in REFUSED[name]:
+        assert status(name, **change) == nmf.NMF_EINVAL, change
+        assert nmf.nmf_last_error()
+    for change in TOO_MUCH.get(name, []):
+        assert status(name, **change) == nmf.NMF_EUNSUPPORTED, change
+
+
+def test_no_rows_are_no_work():
+    for name in ("nmf_rms_norm", "nmf_round_blocks", "nmf_grouped_product8", "nmf_route_gradient", "nmf_spread_rows", "nmf_collect_rows", "nmf_collect_gradient"):
+        assert status(name, rows=0) == nmf.NMF_OK, name
+    assert status("nmf_rms_norm_gradient", rows=0, dweight=0) == nmf.NMF_OK
+
+
+def test_limits_match_the_header():
+    text = open(os.path.join(ROOT, "include", "nmfmu_routed.h")).read()
+    for name in ("NMF_NORM_MAX_M", "NMF_ROUTE_MAX_GROUPS", "NMF_ROUTE_MAX_K"):
+        assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(nmf, name)
+    assert "NMF_E4M3 = 3" in text and nmf.NMF_E4M3 == 3
+
+
+def test_scratch_sizes():
+    need = nmf.nmf_routed_work_bytes
+    assert need(0, 0, 8) == need(0, 10, 0) == need(0, 10, 8) == need(0, 1000, 1025) == 0
+    assert need(0, 1000, 8) > 0 and need(1, 1000, 32769) == 0 and need(1, 1, 100) == 0
+    assert need(1, 1000, 100) % 400 == 0 and need(3, 10, 10, 10, 1) == need(2, 10, 10, 0, 1) == need(2, 10, 10, 10, 0) == 0
+    assert need(2, 16, 8192, 64, 1) > 0
+
+
+def test_host_tensors_are_refused():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        nmf.nmf_rms_norm(x, 4, 8, 1e-6, Y=x)
+    with pytest.raises(ValueError):
+        nmf.nmf_route(x, 4, 8, 2, True, x, x, x, x, x)
+    with pytest.raises(ValueError):
+        nmf.nmf_collect_rows(x, 4, 1, x, x, 8, x)
+
+
+@gpu
+def test_wrong_tensors_are_refused():
+    X = torch.zeros(4, 256, device="cuda")
+    c, s = torch.zeros(4, 256, dtype=E8, device="cuda"), torch.zeros(4, 2, device="cuda")
+    i = torch.zeros(8, dtype=torch.int32, device="cuda")
+    for call in (lambda: nmf.nmf_rms_norm(X, 4, 255, 1e-6, Y=X.clone()),
+                 lambda: nmf.nmf_rms_norm(X, 4, 256, 1e-6, Y=X.half()),
+                 lambda: nmf.nmf_rms_norm(X, 4, 256, 1e-6, Y8=c.float(), scale=s),
+                 lambda: nmf.nmf_rms_norm(X, 4, 256, 1e-6, Y8=c, scale=s[:, :1]),
+                 lambda: nmf.nmf_rms_norm(X, 4, 256, 1e-6, weight=torch.zeros(255, device="cuda"), Y=X.clone()),
+                 lambda: nmf.nmf_round_blocks(X, 4, 256, 128, c, s),
+                 lambda: nmf.nmf_round_blocks(X[None], 4, 256, 1, c, s),
+                 lambda: nmf.nmf_spread_rows(X, 4, 2, i.long(), 256, torch.zeros(8, 256, device="cuda")),
+                 lambda: nmf.nmf_spread_rows(X.double(), 4, 2, i, 256, torch.zeros(8, 256, device="cuda")),
+                 lambda: nmf.nmf_collect_rows(X, 4, 2, i, torch.zeros(7, device="cuda"), 256, X.clone()),
+                 lambda: nmf.nmf_collect_gradient(X, 4, 2, i, None, 256, torch.zeros(8, 256, device="cuda"), X=torch.zeros(7, 256, device="cuda"), dgate=torch.zeros(4, 2, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(nmf.NmfError):
+        nmf.nmf_spread_rows(c, 4, 2, i, 256, torch.zeros(8, 256, dtype=E8, device="cuda"))       # codes without their scales
+    with pytest.raises(nmf.NmfError):
+        nmf.nmf_rms_norm(X, 4, 256, 1e-6, H=X.clone())
+
+
+# ---- all of them together --------------------------------------------------------------------------
+
+class Layer:
+    """x -> x + sum of gates times (norm(x) B_g) over a row's k groups, in 8 bits, with a router of its own; and its gradients."""
+
+    def __init__(self, rows, m, groups, k, dt, seed=1):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.rows, self.m, self.groups, self.k, self.g = rows, m, groups, k, g
+        new = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+        f, i32, M = torch.float32, torch.int32, -(-m // 128)
+        self.X, self.R = (torch.randn(rows, m, generator=g, device="cuda").to(dt) for _ in range(2))
+        self.w = (1 + 0.2 * torch.randn(m, generator=g, device="cuda")).to(dt)
+        self.B = (torch.randn(groups, m, m, generator=g, device="cuda") / m ** 0.5).to(dt)
+        self.router = (torch.randn(1, groups, m, generator=g, device="cuda") / m ** 0.5).to(dt)
+        self.dout = torch.randn(rows, m, generator=g, device="cuda").to(dt)
+        self.dbalance = torch.full((1,), 3.0, device="cuda")
+        self.one = torch.tensor([0, rows], device="cuda")
+        n = rows * k
+        self.H, self.Y, self.out, self.dH, self.dX, self.dnorm = (new(rows, m) for _ in range(6))
+        self.Y8, self.ys, self.rstd = new(rows, m, dtype=E8), new(rows, M, dtype=f), new(rows, dtype=f)
+        self.B8, self.bs = new(groups, m, m, dtype=E8), new(groups, M, M, dtype=f)
+        self.logits, self.dlogits = new(rows, groups), new(rows, groups)
+        self.choice, self.place = new(rows, k, dtype=i32), new(rows, k, dtype=i32)
+        self.gate, self.dgate, self.balance, self.offsets = new(rows, k, dtype=f), new(rows, k, dtype=f), new(1, dtype=f), new(groups + 1, dtype=torch.int64)
+        self.S8, self.ss = torch.zeros(n, m, dtype=torch.uint8, device="cuda").view(E8), torch.zeros(n, M, device="cuda")
+        self.S, self.Z, self.dZ, self.dS = (torch.zeros(n, m, dtype=dt, device="cuda") for _ in range(4))
+        self.dZ8, self.dzs = new(n, m, dtype=E8), new(n, M, dtype=f)
+        self.dB, self.dw, self.dnorm2 = new(groups, m, m), new(m), new(rows, m)
+        self.drouter = new(1, groups, m)
+        self.back = new(rows, m)
+
+    def forward(self):
+        r, m, G, k = self.rows, self.m, self.groups, self.k
+        nmf.nmf_round_blocks(self.B, m, m, 128, self.B8, self.bs)
+        nmf.nmf_rms_norm(self.X, r, m, 1e-6, weight=self.w, R=self.R, H=self.H, Y=self.Y, Y8=self.Y8, scale=self.ys, rstd=self.rstd)
+        nmf.nmf_grouped_product(self.Y, self.one, 1, r, self.router, True, m, G, self.logits)
+        nmf.nmf_route(self.logits, r, G, k, True, self.choice, self.gate, self.offsets, self.place, self.balance)
+        nmf.nmf_spread_rows(self.Y8, r, k, self.place, m, self.S8, scale=self.ys, Yscale=self.ss)
+        nmf.nmf_grouped_product8(self.S8, self.ss, self.offsets, G, r * k, self.B8, self.bs, False, m, m, self.Z)
+        nmf.nmf_collect_rows(self.Z, r, k, self.place, self.gate, m, self.out)
+
+    def backward(self):
+        r, m, G, k = self.rows, self.m, self.groups, self.k
+        nmf.nmf_collect_gradient(self.dout, r, k, self.place, self.gate, m, self.dZ, X=self.Z, dgate=self.dgate)
+        nmf.nmf_route_gradient(self.logits, r, G, k, True, self.choice, self.offsets, self.dgate, self.dbalance, self.dlogits)
+        nmf.nmf_round_blocks(self.dZ, r * k, m, 1, self.dZ8, self.dzs)
+        nmf.nmf_grouped_product8(self.dZ8, self.dzs, self.offsets, G, r * k, self.B8, self.bs, True, m, m, self.dS)
+        nmf.nmf_spread_rows(self.Y, r, k, self.place, m, self.S)
+        nmf.nmf_grouped_gradient(self.S, self.dZ, self.offsets, G, r * k, m, m, self.dB)
+        nmf.nmf_collect_rows(self.dS, r, k, self.place, None, m, self.dnorm)
+        nmf.nmf_grouped_product(self.dlogits, self.one, 1, r, self.router, False, G, m, self.dnorm2)
+        nmf.nmf_grouped_gradient(self.dlogits, self.Y, self.one, 1, r, G, m, self.drouter)
+        torch.add(self.dnorm, self.dnorm2, out=self.back)
+        nmf.nmf_rms_norm_gradient(self.H, self.rstd, self.back, r, m, self.dX, weight=self.w, dH=self.dout, dweight=self.dw)
+
+    def results(self):
+        return [t.clone() for t in (self.H, self.out, self.balance, self.offsets, self.dX, self.dw, self.dB, self.drouter)]
+
+
+def reference(L):
+    """The same layer in 64 bits, without rounding, with the choices that were made; gradients by autograd."""
+    x = (L.X.double() + L.R.double()).requires_grad_(True)
+    w, B, router = (t.double().requires_grad_(True) for t in (L.w, L.B, L.router[0]))
+    y = x / (x.square().mean(dim=1, keepdim=True) + 1e-6).sqrt() * w
+    p = torch.softmax(y @ router.t(), dim=1)
+    choice = L.choice.long()
+    gate = p.gather(1, choice)
+    gate = gate / gate.sum(1, keepdim=True)
+    z = torch.stack([y @ B[g] for g in range(L.groups)], dim=1)
+    out = (gate[:, :, None] * z.gather(1, choice[:, :, None].expand(-1, -1, L.m))).sum(1)
+    f = torch.bincount(choice.reshape(-1), minlength=L.groups).double() / choice.numel()
+    balance = L.groups * (f * p.mean(0)).sum()
+    ((out * L.dout.double()).sum() + (x * L.dout.double()).sum() + 3.0 * balance).backward()
+    return x.detach(), out.detach(), balance.detach(), x.grad, w.grad, B.grad, router.grad
+
+
+@gpu
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_a_layer_of_groups_forward_and_backward(dt):
+    """Against 64 bits: what 8 bits round is off by 2^-4 at most and by 2^-5.8 of its root mean square (uniform within a step), so a
+    product of two such operands by 2^-5.3 of its own, and sums of them likewise; what is not rounded to 8 bits goes by its type."""
+    L = Layer(200, 256, 8, 2, dt)
+    L.forward()
+    L.backward()
+    x, out, balance, dx, dw, dB, drouter = reference(L)
+    far = lambda a, b: float((a.double() - b).norm() / b.norm())  # noqa: E731
+    small = 2.0 ** -20 if dt == torch.float32 else 2.0 ** -8
+    assert far(L.H, x) <= small and abs(float(L.balance) - float(balance)) <= 4 * small * float(balance)
+    for got, want in ((L.out, out), (L.dX, dx), (L.dw, dw), (L.drouter[0], drouter)):
+        assert far(got, want) <= 2.0 ** -4.5
+    assert far(L.dB, dB) <= 16 * small                       # of the rows as they were before rounding
+
+
+@gpu
+def test_a_captured_layer_gives_the_same_on_every_replay():
+    L = Layer(300, 128, 16, 4, torch.bfloat16)
+    M = Layer(90, 640, 5, 2, torch.bfloat16, seed=2)
+    for a in (L, M):
+        a.forward()
+        a.backward()
+    want = [L.results(), M.results()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for a in (L, M):
+            a.forward()
+            a.backward()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for a in (L, M):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            a.forward()
+            a.backward()
+        graphs.append(graph)
+    for turn in range(4):
+        for a, graph, ref in zip((L, M), graphs, want):
+            for t in (a.H, a.out, a.balance, a.offsets, a.dX, a.dw, a.dB, a.choice, a.place, a.Z):
+                t.zero_()
+            graph.replay()
+            if turn % 2:
+                torch.randn(1000, device="cuda").sum()
+            torch.cuda.synchronize()
+            for got, expected in zip(a.results(), ref):
+                assert torch.equal(got, expected)
+        # new inputs in the same memory
+        if turn == 1:
+            for a in (L, M):
+                a.X.copy_(torch.randn(a.X.shape, generator=a.g, device="cuda"))
+                a.forward()
+                a.backward()
+            want = [L.results(), M.results()]
+
+
+@gpu
+def test_two_streams_at_once():
+    layers = [Layer(500, 384, 12, 3, torch.bfloat16, seed=s) for s in (3, 4)]
+    want = []
+    for a in layers:
+        a.forward()
+        a.backward()
+        want.append(a.results())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(5):
+        for a, s in zip(layers, streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                a.forward()
+                a.backward()
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        for a, ref in zip(layers, want):
+            for got, expected in zip(a.results(), ref):
+                assert torch.equal(got, expected)
+    # and by the argument, with torch's own scratch of that stream
+    a, s = layers[0], streams[0]
+    s.wait_stream(torch.cuda.current_stream())
+    c, gate, off, place, bal = (torch.empty_like(t) for t in (a.choice, a.gate, a.offsets, a.place, a.balance))
+    nmf.nmf_route(a.logits, a.rows, a.groups, a.k, True, c, gate, off, place, bal, stream=s)
+    s.synchronize()
+    assert torch.equal(c, a.choice) and torch.equal(gate, a.gate) and torch.equal(place, a.place) and torch.equal(off, a.offsets) and torch.equal(bal, a.balance)
+
+
+@gpu
+def test_rows_beyond_32_bits():
+    """Rows, codes and places whose distances in memory pass 2^31 and 2^32 bytes."""
+    rows, m, ld = 260, 128, 1 << 24
+    mem = torch.empty(rows * ld, dtype=torch.uint8, device="cuda")          # 4.4 GB
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.randn(rows, m, generator=g, device="cuda").to(torch.bfloat16)
+    far = mem.view(torch.bfloat16).as_strided((rows, m), (ld // 2, 1))
+    far.copy_(x)
+    Y, Z = torch.empty_like(x), torch.empty_like(x)
+    nmf.nmf_rms_norm(far, rows, m, 1e-6, Y=Y)
+    nmf.nmf_rms_norm(x, rows, m, 1e-6, Y=Z)
+    assert torch.equal(Y, Z)
+    place = torch.randperm(rows, generator=g, device="cuda").int()[:, None]
+    nmf.nmf_collect_rows(far, rows, 1, place, None, m, Y)
+    assert torch.equal(Y, x[place[:, 0].long()])
+    nmf.nmf_spread_rows(Y, rows, 1, place, m, far)
+    assert torch.equal(far, x)
+    X8, s = mem.as_strided((rows, m), (ld, 1)), torch.empty(rows, 1, device="cuda")
+    nmf.nmf_round_blocks(x, rows, m, 1, X8, s)
+    near8 = X8.contiguous()
+    B8, bs = torch.randint(0, 120, (1, m, m), generator=g, device="cuda").to(torch.uint8), torch.ones(1, 1, 1, device="cuda")
+    off = torch.tensor([0, rows], device="cuda")
+    nmf.nmf_grouped_product8(X8, s, off, 1, rows, B8, bs, False, m, m, Y)
+    nmf.nmf_grouped_product8(near8, s, off, 1, rows, B8, bs, False, m, m, Z)
+    # (tiles that pass registers add the same numbers in the same order)
+    assert torch.equal(Y, Z)

@@ -1,0 +1,341 @@
+"""The norm, the rounding to 8 bits and the rows' way to their groups against their definitions in 64 bits.
+
+Bounds, entry by entry: a result in a type is off by half a step of it, HALF of its magnitude (f16: 2^-25 at least, below its
+normal range), and by what its floats lost before: each addition, product, division or root at most 2^-24 of its result, a sum of n
+terms at most n 2^-24 of the sum of their magnitudes.  A code of e4m3 is off by 2^-4 of its magnitude or by 2^-10, half of its
+smallest step.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2202_09518_amd as nmf
+
+gpu = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+E8 = torch.float8_e4m3fn
+U = 2.0 ** -24
+
+
+def near(got, want, typ, lost):
+    """got (of a type) against want (64 bits), whose floats may have lost `lost` (a tensor or a number) on their way."""
+    off, bound = (got.double() - want).abs(), HALF[typ] * (want.abs() + lost) + lost + (2.0 ** -25 if typ == "f16" else 0.0) + 2.0 ** -149
+    bad = ~(off <= bound)
+    assert not bool(bad.any()), (int(bad.sum()), float((off / bound).nan_to_num(1e30).max()))
+
+
+def view(rows, cols, dtype, pad, fill=None, first=0):
+    """A rows x cols view with leading dimension cols + pad, `first` entries into memory that is full of 77."""
+    mem = torch.full(((rows + 1) * (cols + pad) + first,), 77.0, dtype=torch.float32, device="cuda").to(dtype)
+    v = mem.as_strided((rows, cols), (cols + pad, 1), first)
+    if fill is not None:
+        v.copy_(fill)
+    return v, mem
+
+
+def rest_is_kept(mem, v):
+    keep = mem.clone()
+    keep.as_strided(v.shape, v.stride(), v.storage_offset()).copy_(torch.full(v.shape, 77.0, device="cuda").to(mem.dtype))
+    assert bool((keep.float() == torch.tensor(77.0).to(mem.dtype).float().item()).all())
+
+
+def normal(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def codes_are_right(codes, scale, want, block, lost):
+    """Codes and scales against what they stand for, want (rows x m, 64 bits), known to `lost` of its magnitude."""
+    rows, m = want.shape
+    R, M = -(-rows // block), -(-m // 128)
+    full = torch.zeros(R * block, M * 128, dtype=torch.float64, device="cuda")
+    full[:rows, :m] = want
+    most = full.view(R, block, M, 128).abs().amax(dim=(1, 3))
+    exact = (most / 448).clamp_min(2.0 ** -126)
+    assert scale.shape == (R, M)
+    assert bool(((scale.double() - exact).abs() <= exact * (2 * U + lost)).all())
+    s = scale.double().repeat_interleave(block, 0)[:rows].repeat_interleave(128, 1)[:, :m]
+    off = (codes.float().double() * s - want).abs()
+    bound = torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -10 * s) * (1 + 2.0 ** -20) + lost * want.abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
+
+
+# ---- norm ----------------------------------------------------------------------------------
+
+WIDTHS = [1, 7, 8, 100, 128, 129, 512, 520, 1000, 1024, 1500, 2048, 2049, 4096, 4100, 8192, 9000, 16384, 16390, 32768]
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m", WIDTHS)
+def test_norm_and_gradient(typ, m):
+    dt = TYPES[typ]
+    for rows, pad, first, residual, weighted in ((1, 0, 0, True, True), (5, 3, 1, False, True), (67, 8, 8, True, False)):
+        g = torch.Generator(device="cuda").manual_seed(rows + m)
+        X, _ = view(rows, m, dt, pad, normal(g, rows, m), first)
+        R = view(rows, m, dt, pad, 3 * normal(g, rows, m), first)[0] if residual else None
+        w = (1 + 0.3 * normal(g, m)).to(dt) if weighted else None
+        H, hm = view(rows, m, dt, pad, None, first)
+        Y, ym = view(rows, m, dt, pad + 1, None, first)
+        Y8, cm = view(rows, m, E8, pad, None, first)
+        scale, sm = view(rows, -(-m // 128), torch.float32, pad)
+        rstd = torch.empty(rows, device="cuda")
+        nmf.nmf_rms_norm(X, rows, m, 1e-5, weight=w, R=R, H=H, Y=Y, Y8=Y8, scale=scale, rstd=rstd)
+        torch.cuda.synchronize()
+        for mem, v in ((hm, H), (ym, Y), (cm, Y8), (sm, scale)):
+            rest_is_kept(mem, v)
+        h = X if R is None else (X.float() + R.float()).to(dt)
+        assert torch.equal(H, h)
+        h, wd = h.double(), torch.ones(m, dtype=torch.float64, device="cuda") if w is None else w.double()
+        s = 1 / (h.square().mean(dim=1, keepdim=True) + 1e-5).sqrt()
+        # s: half the error of the mean (m squares and sums, a division, an addition), a root and a division
+        lost = (m / 2 + 4) * U
+        assert bool(((rstd.double() - s.squeeze(1)).abs() <= lost * s.squeeze(1)).all())
+        y = h * s * wd
+        near(Y, y, typ, (lost + 2 * U) * y.abs())
+        codes_are_right(Y8, scale, y, 1, lost + 2 * U)
+        # each output by itself is the same
+        Z, Z8, z = torch.empty_like(Y), torch.empty(rows, m, dtype=torch.uint8, device="cuda"), torch.empty(rows, -(-m // 128), device="cuda")
+        nmf.nmf_rms_norm(X, rows, m, 1e-5, weight=w, R=R, Y=Z)
+        nmf.nmf_rms_norm(X, rows, m, 1e-5, weight=w, R=R, Y8=Z8, scale=z)
+        assert torch.equal(Z, Y) and torch.equal(Z8, Y8.contiguous().view(torch.uint8)) and torch.equal(z, scale)
+
+        # gradients
+        dY, _ = view(rows, m, dt, pad, normal(g, rows, m), first)
+        dH = view(rows, m, dt, pad, normal(g, rows, m), first)[0] if residual else None
+        dX, dm = view(rows, m, dt, pad, None, first)
+        dw = torch.full((m,), 5.0, device="cuda").to(dt)
+        nmf.nmf_rms_norm_gradient(H, rstd, dY, rows, m, dX, weight=w, dH=dH, dweight=dw)
+        torch.cuda.synchronize()
+        rest_is_kept(dm, dX)
+        s, dy = rstd.double()[:, None], dY.double()
+        z, x = dy * wd, h * s
+        d = s * (z - x * (z * x).mean(dim=1, keepdim=True))
+        size = s * (z.abs() + x.abs() * (z * x).abs().mean(dim=1, keepdim=True))
+        if dH is not None:
+            d, size = d + dH.double(), size + dH.double().abs()
+        near(dX, d, typ, (m + 12) * U * size)
+        near(dw, (dy * x).sum(0), typ, (rows + 3) * U * (dy * x).abs().sum(0))
+        # without the weight's gradient, with less scratch than wanted and with none, dX in the place of dH or dY
+        for work in (0, 4 * m * 2, None):
+            again, dw2 = torch.empty_like(dX), torch.empty_like(dw)
+            nmf.nmf_rms_norm_gradient(H, rstd, dY, rows, m, again, weight=w, dH=dH, dweight=dw2,
+                                      work=None if work is None else torch.empty(work, dtype=torch.uint8, device="cuda"))
+            assert torch.equal(again, dX)
+            near(dw2, (dy * x).sum(0), typ, (rows + 3) * U * (dy * x).abs().sum(0))
+        again = dY.clone()
+        nmf.nmf_rms_norm_gradient(H, rstd, again, rows, m, again, weight=w, dH=dH)
+        assert torch.equal(again, dX)
+        if dH is not None:
+            again = dH.clone()
+            nmf.nmf_rms_norm_gradient(H, rstd, dY, rows, m, again, weight=w, dH=again)
+            assert torch.equal(again, dX)
+
+
+@gpu
+def test_norm_gradient_against_differences():
+    """Of sum(dY Y) + sum(dH H) in one direction, in floats: the loss in 64 bits of Y in floats is known to about 2^-22 of its terms."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows, m, step = 9, 700, 2.0 ** -6
+    X, w, dY, dH, D, dW = (normal(g, rows, m), 1 + 0.2 * normal(g, m), normal(g, rows, m), normal(g, rows, m), normal(g, rows, m), normal(g, m))
+    dX, dw, rstd = torch.empty_like(X), torch.empty_like(w), torch.empty(rows, device="cuda")
+
+    def loss(x, w):
+        Y, H = torch.empty_like(X), torch.empty_like(X)
+        nmf.nmf_rms_norm(x, rows, m, 1e-6, weight=w, H=H, Y=Y, rstd=rstd)
+        return float((dY.double() * Y.double()).sum() + (dH.double() * H.double()).sum())
+
+    loss(X, w)
+    nmf.nmf_rms_norm_gradient(X, rstd, dY, rows, m, dX, weight=w, dH=dH, dweight=dw)
+    # fourth order in the step; the losses' own error is below 2 rows m 2^-22 (of terms of about one) over the step
+    four = (8 * (loss(X + step * D, w) - loss(X - step * D, w)) - (loss(X + 2 * step * D, w) - loss(X - 2 * step * D, w))) / (12 * step)
+    size = float(dX.norm() * D.norm())
+    assert abs(four - float((dX.double() * D.double()).sum())) < 1e-4 * size
+    two = (loss(X, w + step * dW) - loss(X, w - step * dW)) / (2 * step)
+    assert abs(two - float((dw.double() * dW.double()).sum())) < 1e-4 * float(dw.norm() * dW.norm())
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_norm_rows_stand_alone_and_in_place(typ):
+    dt, rows, m = TYPES[typ], 40, 300
+    g = torch.Generator(device="cuda").manual_seed(5)
+    X, R, w = normal(g, rows, m).to(dt), normal(g, rows, m).to(dt), normal(g, m).to(dt)
+
+    def run(X, R, **more):
+        H, Y, c, s, q = torch.empty_like(X), torch.empty_like(X), torch.empty(rows, m, dtype=torch.uint8, device="cuda"), torch.empty(rows, 3, device="cuda"), torch.empty(rows, device="cuda")
+        nmf.nmf_rms_norm(X, rows, m, 1e-6, weight=w, R=R, H=more.get("H", H), Y=Y, Y8=c, scale=s, rstd=q)
+        return more.get("H", H), Y, c, s, q
+
+    want = run(X, R)
+    bad = X.clone()
+    bad[7, 200], bad[20, 0], bad[21, 299] = math.nan, math.inf, -math.inf
+    got = run(bad, R)
+    ok = torch.ones(rows, dtype=torch.bool, device="cuda")
+    ok[[7, 20, 21]] = False
+    for a, b in zip(want, got):
+        assert torch.equal(a[ok], b[ok])
+    assert bool(got[1][7].isnan().all()) and bool(got[3][7].isnan().all()) and not bool(got[2][7].any())
+    # s is 0 beside an infinity: its own entry is NaN, the others' 0
+    assert bool(got[1][20, 0].isnan()) and bool((got[1][20, 1:] == 0).all()) and bool(got[3][20, 0].isnan()) and bool((got[3][20, 1:] == 2.0 ** -126).all())
+    # a row of zeros
+    zero = X.clone()
+    zero[3] = 0
+    r0 = R.clone()
+    r0[3] = 0
+    got = run(zero, r0)
+    assert bool((got[1][3] == 0).all()) and bool((got[3][3] == 2.0 ** -126).all()) and not bool(got[2][3].any())
+    # H in the place of R, and of X
+    r, x = R.clone(), X.clone()
+    for a, b in zip(want, run(X, r, H=r)):
+        assert torch.equal(a, b)
+    for a, b in zip(want, run(x, R, H=x)):
+        assert torch.equal(a, b)
+
+
+# ---- 8 bits ----------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("count,rows,m", [(1, 1, 1), (1, 1, 128), (2, 127, 130), (1, 128, 128), (3, 129, 255), (1, 300, 1000), (5, 256, 64), (1, 1000, 7)])
+def test_round_blocks(count, rows, m, block, typ):
+    dt = TYPES[typ]
+    g = torch.Generator(device="cuda").manual_seed(rows + m)
+    for pad, first in ((0, 0), (5, 3)):
+        ld = m + pad
+        mem = torch.empty(count * (rows + 1) * ld + first, dtype=dt, device="cuda")
+        X = mem.as_strided((count, rows, m), ((rows + 1) * ld, ld, 1), first)
+        X.copy_(normal(g, count, rows, m) * torch.exp(2 * normal(g, count, rows, 1)))
+        cm = torch.full((count * (rows + 1) * ld + first,), 77, dtype=torch.uint8, device="cuda")
+        C = cm.as_strided(X.shape, X.stride(), first)
+        R, M = -(-rows // block), -(-m // 128)
+        sm = torch.full((count * (R + 1) * (M + 1),), 77.0, device="cuda")
+        S = sm.as_strided((count, R, M), ((R + 1) * (M + 1), M + 1, 1), 0)
+        nmf.nmf_round_blocks(X, rows, m, block, C, S)
+        torch.cuda.synchronize()
+        rest_is_kept(cm, C)
+        rest_is_kept(sm, S)
+        for i in range(count):
+            codes_are_right(C[i].contiguous().view(E8), S[i], X[i].double(), block, 0.0)
+        # one matrix of the stack is the same
+        c, s = torch.empty(rows, m, dtype=E8, device="cuda"), torch.empty(R, M, device="cuda")
+        nmf.nmf_round_blocks(X[count - 1], rows, m, block, c, s)
+        assert torch.equal(c.view(torch.uint8), C[count - 1]) and torch.equal(s, S[count - 1])
+
+
+@gpu
+@pytest.mark.parametrize("block", [1, 128])
+def test_round_blocks_at_the_ends_of_the_range(block):
+    rows, m = 256, 384
+    g = torch.Generator(device="cuda").manual_seed(9)
+    X = normal(g, rows, m)
+    X[:128, :128] = 0
+    X[:128, 128:256] *= 2.0 ** -140                         # below the smallest scale: codes lose bits, nothing overflows
+    X[:128, 256:] *= 2.0 ** 124
+    X[130, 5], X[131, 130], X[140, 300] = math.nan, math.inf, -math.inf
+    C, S = torch.empty(rows, m, dtype=E8, device="cuda"), torch.empty(-(-rows // block), 3, device="cuda")
+    nmf.nmf_round_blocks(X, rows, m, block, C, S)
+    torch.cuda.synchronize()
+    codes_are_right(C[:128], S[:128 // block], X[:128].double(), block, 0.0)
+    assert bool((S[:128 // block, 0] == 2.0 ** -126).all())
+    bad = S.isnan().repeat_interleave(block, 0).repeat_interleave(128, 1)
+    want = torch.zeros_like(bad)
+    for r, c in ((130, 0), (131, 128), (140, 256)):
+        want[(r if block == 1 else 128):(r + 1 if block == 1 else 256), c:c + 128] = True
+    assert torch.equal(bad, want) and not bool(C.view(torch.uint8)[bad].any())
+
+
+# ---- rows to their places and back -----------------------------------------------------------
+
+def places(g, rows, k, sorted_rows, share):
+    """Distinct places for some of the choices, -1 and numbers out of range for the others."""
+    there = torch.rand(rows * k, generator=g, device="cuda") < share
+    free = torch.randperm(sorted_rows, generator=g, device="cuda")
+    which = there.nonzero().squeeze(1)[:sorted_rows]
+    place = torch.full((rows * k,), -1, dtype=torch.int32, device="cuda")
+    place[which] = free[:which.numel()].int()
+    out = (place < 0).nonzero().squeeze(1)
+    place[out[::3]] = sorted_rows
+    place[out[1::3]] = -2 ** 31
+    return place.view(rows, k)
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,k,m", [(1, 1, 1), (3, 2, 7), (24, 4, 128), (50, 3, 1000), (7, 16, 1025), (33, 8, 4096), (5, 5, 9001)])
+def test_spread_and_collect(rows, k, m, typ):
+    dt = TYPES[typ]
+    for pad, first, share in ((0, 0, 1.1), (3, 1, 0.7), (8, 0, 0.0)):
+        g = torch.Generator(device="cuda").manual_seed(rows + m)
+        count = rows * k + 2
+        place = places(g, rows, k, count, share)
+        there = (place >= 0) & (place < count)
+        t, j = there.nonzero(as_tuple=True)
+        z = place[there].long()
+        gate = torch.rand(rows, k, generator=g, device="cuda")
+        gate[~there] = math.nan                              # not used
+        X, _ = view(rows, m, dt, pad, normal(g, rows, m), first)
+        S, sm = view(count, m, dt, pad, None, first)
+        nmf.nmf_spread_rows(X, rows, k, place, m, S)
+        keep = torch.full((count, m), 77.0, device="cuda").to(dt)
+        want = keep.clone()
+        want[z] = X[t]
+        torch.cuda.synchronize()
+        assert torch.equal(S, want)
+        rest_is_kept(sm, S)
+
+        Z, _ = view(count, m, dt, pad, normal(g, count, m), first)
+        unused = torch.ones(count, dtype=torch.bool, device="cuda")
+        unused[z] = False
+        Z[unused] = math.nan                                 # rows that no place names
+        weight = torch.where(there, gate, torch.zeros_like(gate)).double()
+        at = place.clamp(0, count - 1).long()
+        rows_z = torch.where(there[:, :, None], Z.double()[at], torch.zeros((), dtype=torch.float64, device="cuda"))
+        for w in (gate, None):
+            Y, ym = view(rows, m, dt, pad, None, first)
+            nmf.nmf_collect_rows(Z, rows, k, place, w, m, Y)
+            torch.cuda.synchronize()
+            rest_is_kept(ym, Y)
+            terms = rows_z * (weight if w is not None else there.double())[:, :, None]
+            near(Y, terms.sum(1), typ, (k + 1) * U * terms.abs().sum(1))
+
+        dY, _ = view(rows, m, dt, pad, normal(g, rows, m), first)
+        for w in (gate, None):
+            dZ, zm = view(count, m, dt, pad, None, first)
+            dgate = torch.full((rows, k), 5.0, device="cuda")
+            nmf.nmf_collect_gradient(dY, rows, k, place, w, m, dZ, X=Z, dgate=dgate)
+            torch.cuda.synchronize()
+            rest_is_kept(zm, dZ)
+            d = dY.double()[t] * (gate.double()[t, j][:, None] if w is not None else 1.0)
+            near(dZ[z], d, typ, U * d.abs())
+            assert bool((dZ[unused] == torch.tensor(77.0).to(dt).item()).all())
+            terms = dY.double()[:, None, :] * rows_z
+            near(dgate, terms.sum(2), "f32", (m + 1) * U * terms.abs().sum(2))
+            assert bool((dgate[~there] == 0).all())
+            again, _ = view(count, m, dt, pad, None, first)
+            nmf.nmf_collect_gradient(dY, rows, k, place, w, m, again)
+            assert torch.equal(again.nan_to_num(), dZ.nan_to_num())
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 16, 100, 128, 4097])
+def test_spread_of_codes_takes_the_scales_along(m):
+    g = torch.Generator(device="cuda").manual_seed(m)
+    rows, k, M = 19, 3, -(-m // 128)
+    count = rows * k
+    place = places(g, rows, k, count, 0.8)
+    C = torch.randint(0, 256, (rows, m), generator=g, device="cuda").to(torch.uint8)
+    s = torch.rand(rows, M, generator=g, device="cuda")
+    D, dm = view(count, m, torch.uint8, 3)
+    z, zm = view(count, M, torch.float32, 2)
+    nmf.nmf_spread_rows(C, rows, k, place, m, D, scale=s, Yscale=z)
+    torch.cuda.synchronize()
+    there = (place >= 0) & (place < count)
+    t, _ = there.nonzero(as_tuple=True)
+    want, ws = torch.full_like(D, 77), torch.full((count, M), 77.0, device="cuda")
+    want[place[there].long()], ws[place[there].long()] = C[t], s[t]
+    assert torch.equal(D, want) and torch.equal(z, ws)
+    rest_is_kept(dm, D)
+    rest_is_kept(zm, z)
