@@ -128,7 +128,8 @@ int nmf_collect_gradient(int32_t type, const void *dY, int64_t ldy, int64_t rows
 
 /*
  * Scratch of the fastest plan, in bytes (0: none needed, or invalid sizes).  kind: 0 nmf_route (m: groups), 1
- * nmf_rms_norm_gradient with dweight, 2 nmf_grouped_product8 (parts: groups; kind 2 alone takes n and parts).
+ * nmf_rms_norm_gradient with dweight, 2 nmf_grouped_product8 (parts: groups; kind 2 alone takes n and parts, and, added to
+ * it as in nmf_ragged_work_bytes, NMF_ODD_X, NMF_ODD_B and NMF_ONE_B).
  */
 size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts);
 

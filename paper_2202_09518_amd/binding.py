@@ -572,7 +572,10 @@ def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transpos
     b, ldb, stride_b = _stack_of(B8, _codes(B8, "B8"), d, groups, *((n, m) if transposed else (m, n)), "B8")
     bs, ldbs, stride_bs = _stack_of(bscale, torch.float32, d, groups, *((N, M) if transposed else (M, N)), "bscale")
     y, ldy = _rows_of(Y, Y.dtype, d, rows, n, "Y")
-    w, nbytes, _keep = _scratch(_need_routed(2, rows, m, n, groups), work, d, stream)
+    odd = (NMF_ODD_X if (x | ldx) & 15 else 0) | (NMF_ODD_B if (b | ldb | (stride_b if groups > 1 else 0)) & 15 else 0)
+    if stride_b == 0:
+        odd |= NMF_ONE_B
+    w, nbytes, _keep = _scratch(_need_routed(2 | odd, rows, m, n, groups) if work is None else 0, work, d, stream)
     _check(lib().nmf_grouped_product8(typ, x, ldx, xs, ldxs, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
                                       bs, ldbs, stride_bs, int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))
 

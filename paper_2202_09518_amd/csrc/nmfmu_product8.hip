@@ -36,6 +36,8 @@ __device__ __forceinline__ i32x8 both(u32x4 a, u32x4 b)
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
+__device__ __forceinline__ f32x4 fma4(f32x4 x, float s, f32x4 y) { return __builtin_elementwise_fma(x, f32x4{s, s, s, s}, y); }
+
 // Codes 8 i to 8 i + 7 of a lane as bf16.
 __device__ __forceinline__ bf16x8 codes_in_bf16(i32x8 v, int i)
 {
@@ -60,23 +62,24 @@ struct Scales {
     int64_t step;            // from block to block
 };
 
-// The scales of a tile's rows for one block, 256 bytes to each wave: lane l of wave w brings that of row RW w + l.
+// The scales of a tile's rows for one block: lane l of wave w brings that of row RW w + l.
 template <int BM, int WAVES, bool DMA> struct RowScales {
     static constexpr int RW = BM / WAVES;
-    static constexpr int kBytes = WAVES * 256;
+    static constexpr int kBytes = BM * 4;
     static_assert(RW <= 64 && BM % WAVES == 0, "a lane to a row");
 
     const char *base;
     unsigned off;
     int64_t far;
-    bool is;
+    bool mine, is;           // the lane has a row, and it is there
     float reg;
 
     __device__ __forceinline__ void open(const Scales &s, int64_t count)
     {
         const int lane = threadIdx.x & 63, row = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * RW + lane;
         base = (const char *)s.x;
-        is = lane < RW && row < count;
+        mine = lane < RW;
+        is = mine && row < count;
         far = row * s.ldx * 4;
         off = is ? (unsigned)far : kOutside;
     }
@@ -86,17 +89,23 @@ template <int BM, int WAVES, bool DMA> struct RowScales {
         if (DMA) {
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
             typedef __attribute__((address_space(3))) char lds_char;
-            const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds) + wave * 256;
+            const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds) + wave * (RW * 4);
             const u32x4 r = {(unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)at),
                              (unsigned)__builtin_amdgcn_readfirstlane((int)((uintptr_t)at >> 32)) & 0xffffu, 0x7fffffffu, (unsigned)kBufferFlags};
             const unsigned o = block < end ? off : kOutside;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(r) : "memory", "m0");
+            // by the lanes that have a row: all of a wave's are at work here, and the others would write behind its rows
+            constexpr unsigned long long lanes = RW < 64 ? (1ull << (RW % 64)) - 1 : ~0ull;
+            asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tbuffer_load_dword %1, %2, 0 offen lds\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(o),
+                         "s"(r), "s"(lanes)
+                         : "memory", "m0");
         } else {
             reg = is && block < end ? *reinterpret_cast<const float *>(at + far) : 0.f;
         }
     }
-    __device__ __forceinline__ void put(char *lds) { *reinterpret_cast<float *>(lds + threadIdx.x * 4) = reg; }
-    static __device__ __forceinline__ int place(int row) { return ((row / RW) * 64 + row % RW) * 4; }
+    __device__ __forceinline__ void put(char *lds)
+    {
+        if (mine) *reinterpret_cast<float *>(lds + (threadIdx.x / 64 * RW + (threadIdx.x & 63)) * 4) = reg;
+    }
 };
 
 template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool EXACT> struct Tile8 : Tile<e8_t, BM, BN, WM, WN, STAGES_, false, QRC, DMA> {
@@ -113,7 +122,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
     using Rows = RowScales<BM, WM * WN, DMA>;
     static constexpr int kStage = Base::kLdsStage + Rows::kBytes;
     static constexpr int kLds = STAGES * kStage;
-    static_assert(BN / WN <= 128 && 16 * WM % Rows::RW == 0, "a wave's columns lie in one block, its rows' scales at even distances");
+    static_assert(BN / WN <= 128, "a wave's columns lie in one block");
 
     // acc += the product of one stage, a block of the contraction.
     static __device__ __forceinline__ void step(const char *lds, const ReadP &rp, const ReadQ &rq, int at, float sb, Acc &acc)
@@ -122,9 +131,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
         float s[2];
         auto add = [&](int i) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[i & 1][j][v], s[i & 1], acc[i][j][v]);
+            for (int j = 0; j < TN; ++j) acc[i][j] = fma4(t[i & 1][j], s[i & 1], acc[i][j]);
         };
         constexpr int N = EXACT ? 4 : 1;
         std::conditional_t<EXACT, bf16x8, i32x8> q[TN][N];
@@ -142,7 +149,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const i32x8 p = both(rp.read(lds, i, 0), rp.read(lds, i, 1));
-            s[i & 1] = *reinterpret_cast<const float *>(lds + Base::kLdsStage + at + i * (16 * WM / Rows::RW * 256)) * sb;
+            s[i & 1] = *reinterpret_cast<const float *>(lds + Base::kLdsStage + at + i * (64 * WM)) * sb;
             if constexpr (EXACT) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
@@ -160,9 +167,129 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
         add(TM - 1);
     }
 
+    // Scales of the wave's columns in up to 64 blocks from `block` on, one to a lane.
+    static __device__ __forceinline__ float columns_scales(const Scales &s, int64_t block, int count)
+    {
+        const int lane = threadIdx.x & 63;
+        float x = lane < count ? s.b[(block + lane) * s.step] : 0.f;
+        asm volatile("" : "+v"(x));                  // waited for here, not in every stage
+        return x;
+    }
+    static __device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+
+    // Stages of the large tile.  Its products of 16 x 16 follow each other in slots; two slots after a product it joins the sums.  While
+    // a row of them runs, the next row's operand is read.  Before the last row all reads of the stage are done and the next stage has
+    // arrived: the columns' operands of that are read as the last products of this one let go of them, and the stage's buffer is
+    // loaded again, a load or a read between every two products.
+    static constexpr bool kAhead = DMA && !EXACT && STAGES == 2 && TM * TN >= 32;
+    static __device__ __forceinline__ void ahead(LoadP &lp, LoadQ &lq, Rows &ls, const ReadP &rp, const ReadQ &rq, int at, int64_t b0, int64_t b1, int64_t k1,
+                                                 int64_t rows, const Scales &scales, char *lds, Acc &acc)
+    {
+        constexpr int L = LoadP::kJobs + LoadQ::kJobs + 1, D = 2;      // loads of a stage; slots from a product to its sum
+        const int steps = (int)(b1 - b0);
+        auto load = [&](int n, int s) {
+            char *stage = lds + (s & 1) * kStage;
+            const int64_t k0 = (b0 + s) * 128;
+            const int left = k1 - k0 < 128 ? (int)(k1 - k0) : 128;
+            if (n < LoadQ::kJobs) lq.bring(n, lq.base + (QRC ? k0 * lq.ld : k0), left, stage + kLdsP);
+            else if (n < L - 1) lp.bring(n - LoadQ::kJobs, lp.base + k0, left, stage);
+            else ls.fetch(b0 + s, b1, stage + Base::kLdsStage);
+        };
+#pragma unroll
+        for (int n = 0; n < L; ++n) load(n, 0);
+        auto run = [&](auto live) {
+            constexpr int LIVE = live.value;
+            static_assert(LIVE % 2 == 0 && TN % 4 == 0, "turns of registers end with the stage");
+            constexpr int E = (L + LIVE * TN - 1) / (LIVE * TN), FIRST = TN * E < L ? TN * E : L;      // loads of a slot, and of the last row's
+#pragma unroll
+            for (int n = 0; n < FIRST; ++n) load(n, 1);
+            wait_loads<FIRST>();
+            meet();
+            i32x8 q[TN], p[2];
+            f32x4 t[4];
+            float sa[2], scale[2] = {0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) t[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto read_q = [&](int j, const char *stage) { q[j] = both(rq.read(stage + kLdsP, j, 0), rq.read(stage + kLdsP, j, 1)); };
+            auto read_p = [&](int i, const char *stage) {
+                p[i & 1] = both(rp.read(stage, i, 0), rp.read(stage, i, 1));
+                sa[i & 1] = *reinterpret_cast<const float *>(stage + Base::kLdsStage + at + i * (64 * WM));
+            };
+            auto join = [&](auto slot) {             // of the product in this slot
+                constexpr int n = (slot.value + LIVE * TN) % (LIVE * TN), i = n / TN, j = n % TN;
+                acc[i][j] = fma4(t[n & 3], scale[i & 1], acc[i][j]);
+            };
+#pragma unroll
+            for (int j = 0; j < TN; ++j) read_q(j, lds);
+            read_p(0, lds);
+            // (without branches in a stage: the compiler would move the sums behind them)
+            for (int s = 0, till = 0; till < steps;) {
+              till = till + 64 < steps ? till + 64 : steps;
+              const float columns = columns_scales(scales, b0 + s, till - s);
+              const int first = s;
+              for (; s < till; ++s) {
+                const char *now = lds + (s & 1) * kStage, *next = lds + (~s & 1) * kStage;
+                const float sb = lane_of(columns, s - first);
+                each<LIVE>([&](auto row) {
+                    constexpr int i = row.value;
+                    constexpr bool last = i == LIVE - 1;
+                    if constexpr (last) {
+                        wait_loads<0>();
+                        meet();
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    each<TN>([&](auto col) {
+                        constexpr int j = col.value, n = i * TN + j;
+                        if constexpr (j == D - 1) scale[i & 1] = sa[i & 1] * sb;
+                        t[n & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q[j], p[i & 1], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                        join(std::integral_constant<int, n - D>{});
+                        if constexpr (last) {
+                            read_q(j, next);
+                            if constexpr (j == TN - 1) read_p(0, next);
+                        } else if constexpr (j == 0) {
+                            read_p(i + 1, now);
+                        }
+                        constexpr int l = (last ? j : (i + 1) * TN + j) * E;
+                        each<E>([&](auto e) {
+                            if constexpr (l + e.value < L) load(l + e.value, last ? s + 2 : s + 1);
+                        });
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                });
+              }
+            }
+            each<D>([&](auto d) { join(std::integral_constant<int, d.value - D>{}); });
+        };
+        // the waves' rows lie in turn: of a tile with fewer rows each one leaves out as many
+        run(std::integral_constant<int, TM>{});
+        wait_loads<0>();
+        meet();
+    }
+
+    // Order of the blocks: of each 64 of them every workgroup begins with another one.  Tiles of few rows read B once, each for itself, and
+    // where k is contiguous they would all read the same part of their lines of 128 bytes, rows apart, at once: 512 rows over 64 groups
+    // of 4096 x 2048, transposed, 109 us in one order, 88 in turns.  Larger tiles share what they read and keep one order (6000 x 4096 x
+    // 2048, float32: 127 us and 141).
+    struct Turn {
+        int first, base, count, at;
+        __device__ __forceinline__ int block(int s, int steps)      // for s = 0, 1, ...; from `steps` on s
+        {
+            if (BM > 32 || QRC || s >= steps) return s;
+            if (s % 64 == 0) {
+                base = s;
+                count = steps - s < 64 ? steps - s : 64;
+                at = first % count;
+            } else {
+                at = at + 1 == count ? 0 : at + 1;
+            }
+            return base + at;
+        }
+    };
+
     // acc += the product over blocks [b0, b1) of the contraction of K.  Leaves LDS free for other use.
-    static __device__ __forceinline__ void multiply(const Operand &P, const Operand &Q, const Scales &scales, int64_t b0, int64_t b1, int64_t K, char *lds,
-                                                    Acc &acc)
+    static __device__ __forceinline__ void multiply(const Operand &P, const Operand &Q, const Scales &scales, int64_t b0, int64_t b1, int64_t K, int turn,
+                                                    char *lds, Acc &acc)
     {
         LoadP lp;
         LoadQ lq;
@@ -174,23 +301,26 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
         ReadQ rq;
         rp.open(Base::wave_row());
         rq.open(Base::wave_col());
-        const int at = Rows::place(Base::row_of(0));
+        const int at = Base::row_of(0) * 4;
         const int64_t k1 = b1 * 128 < K ? b1 * 128 : K;
-        const int steps = (int)(b1 - b0), lane = threadIdx.x & 63;
-        float sb = 0.f;                              // of 64 blocks, one to a lane
+        const int steps = (int)(b1 - b0);
+        float columns = 0.f;
+        Turn fetched = {turn, 0, 0, 0}, used = {turn, 0, 0, 0};
         auto scale_of_columns = [&](int s) {
-            if (s % 64 == 0) {
-                sb = s + lane < steps ? scales.b[(b0 + s + lane) * scales.step] : 0.f;
-                asm volatile("" : "+v"(sb));         // waited for here, not in every stage
-            }
-            return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb), s % 64));
+            if (s % 64 == 0) columns = columns_scales(scales, b0 + s, steps - s);
+            return lane_of(columns, used.block(s, steps) % 64);
         };
         auto fetch = [&](int s, int to) {
             char *stage = lds + to * kStage;
-            lq.fetch((b0 + s) * 128, k1, stage + kLdsP);
-            lp.fetch((b0 + s) * 128, k1, stage);
-            ls.fetch(b0 + s, b1, stage + Base::kLdsStage);
+            const int64_t block = b0 + fetched.block(s, steps);
+            lq.fetch(block * 128, k1, stage + kLdsP);
+            lp.fetch(block * 128, k1, stage);
+            ls.fetch(block, b1, stage + Base::kLdsStage);
         };
+        if constexpr (kAhead) {
+            ahead(lp, lq, ls, rp, rq, at, b0, b1, k1, P.count, scales, lds, acc);
+            return;
+        }
         if (DMA) {
             constexpr int L = LoadP::kJobs + LoadQ::kJobs + 1;
 #pragma unroll
@@ -251,7 +381,7 @@ template <class C, class O> __global__ __launch_bounds__(C::THREADS) void produc
     const int64_t blocks = blocks_of(a.m), b0 = split * a.k_split, b1 = b0 + a.k_split < blocks ? b0 + a.k_split : blocks;
     typename C::Acc acc;
     C::clear(acc);
-    C::multiply(P, Q, scales, b0, b1, a.m, lds, acc);
+    C::multiply(P, Q, scales, b0, b1, a.m, id, lds, acc);
     if (a.splits > 1) {
         const int64_t n4 = up4(a.n);
         C::store(acc, a.part + ((int64_t)split * a.rows + f.r0) * n4 + c0, n4, f.r1 - f.r0, a.n - c0, true, lds);
@@ -275,6 +405,15 @@ template <class O> __global__ __launch_bounds__(256) void join8_kernel(Product8 
         if (col + e < a.n) out[e] = Type<O>::round(y[e]);
 }
 
+__global__ __launch_bounds__(256) void whole_rows_kernel(const char *src, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t count, char *dst, int64_t ldo)
+{
+    const int64_t per = ldo / 16, all = count * rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t line = i / per, c = (i - line * per) * 16, g = line / rows, r = line - g * rows;
+        *reinterpret_cast<u32x4 *>(dst + i * 16) = keep_first<e8_t>(chunk_at<e8_t>(src + g * stride + r * ld + c, cols - c), cols - c);
+    }
+}
+
 template <class O, bool QRC, bool DMA> void launch_shape(const Product8 &p, hipStream_t st)
 {
     auto go = [&](auto tile) {
@@ -290,7 +429,7 @@ template <class O, bool QRC, bool DMA> void launch_shape(const Product8 &p, hipS
     case k128x128: go(Tile8<128, 128, 2, 2, 2, QRC, DMA, E>{}); break;
     case k64x64: go(Tile8<64, 64, 2, 2, 3, QRC, DMA, E>{}); break;
     case k64x128: go(Tile8<64, 128, 1, 4, 3, QRC, DMA, E>{}); break;
-    default: go(Tile8<32, 128, 1, 4, 4, QRC, DMA, E>{}); break;
+    default: go(Tile8<32, 128, 1, 4, 3, QRC, DMA, E>{}); break;
     }
 }
 
@@ -307,6 +446,14 @@ template <class O> void launch_type(const Product8 &p, hipStream_t st)
 }
 
 }  // namespace
+
+hipError_t launch_whole_rows(const void *src, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t count, void *dst, int64_t ldo, hipStream_t st)
+{
+    const int64_t blocks = (count * rows * (ldo / 16) + 255) / 256;
+    hipLaunchKernelGGL(whole_rows_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, (const char *)src, ld, stride, rows, cols, count,
+                       (char *)dst, ldo);
+    return hipGetLastError();
+}
 
 hipError_t launch_product8(const Product8 &p, hipStream_t st)
 {

@@ -241,6 +241,18 @@ template <class T, int R, bool RC, int THREADS, bool DMA, int PLANES> struct Loa
             reg[j] = v;
         }
     }
+    // The same straight to LDS from a stage that begins at `at`, with `left` k from there on: fewer registers.
+    __device__ __forceinline__ void bring(int j, const char *at, int left, char *lds) const
+    {
+        static_assert(DMA && PLANES == 1, "");
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        typedef __attribute__((address_space(3))) char lds_char;
+        const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)(lds + j * THREADS * 16)) + wave * 1024;
+        const u32x4 r = {(unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)at),
+                         (unsigned)__builtin_amdgcn_readfirstlane((int)((uintptr_t)at >> 32)) & 0xffffu, 0x7fffffffu, (unsigned)kBufferFlags};
+        const unsigned o = (RC ? line >= left - j * kRowStep : k_of(j) >= left) ? kOutside : off[j];
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(r) : "memory", "m0");
+    }
     __device__ __forceinline__ void fetch(int64_t k0, int64_t K, char *lds)
     {
 #pragma unroll

@@ -60,25 +60,29 @@ struct Plan {
 };
 
 // Time of `tiles` tiles of a shape: those of the busiest compute unit, by their size and by what share of the large tile's rate
-// they reach.
+// they reach.  us, bf16 results: 8192 x 4096 x 4096 takes 131 in tiles of 256 x 256, 190 in 128 x 128, 230 in 64 x 128, 270 to 300 in
+// 64 x 64; 1024 x 4096 x 4096 49, 32.1, 31.9, 39.3; 2000 x 2048 x 2048 28, 19.0, 18.7, 23.2; 4096 rows in 8 groups, 4096 x 2048, 52, 68, 75, 77.
 double tile_time(int shape, int64_t tiles)
 {
-    static const double rate[] = {1.0, 0.72, 0.5};
-    return (double)ceil_div(tiles, kComputeUnits) * kTileRows[shape] * kTileCols[shape] / rate[std::min(shape, 2)];
+    const double rate = shape == k256x256 ? 1.0 : shape == k128x128 ? 0.7 : shape == k64x128 ? 0.5 : 0.45;
+    return (double)ceil_div(tiles, kComputeUnits) * kTileRows[shape] * kTileCols[shape] / rate;
 }
 
-// large: the 256 x 256 tile can be had.
+// Tile shape and parts of the contraction.  Groups end inside a tile, half a tile each on average.  large: the 256 x 256 tile can be had.
 Plan product_plan(int64_t rows, int64_t groups, int64_t m, int64_t n, bool large)
 {
     groups = std::max<int64_t>(1, std::min(groups, rows));
     const int64_t avg = ceil_div(rows, groups);
-    auto tiles = [&](int shape) { return groups * ceil_div(avg, kTileRows[shape]) * ceil_div(n, kTileCols[shape]); };
+    auto tiles = [&](int shape) {
+        const int64_t up = groups > 1 ? ceil_div(rows, kTileRows[shape]) + groups / 2 : ceil_div(rows, kTileRows[shape]);
+        return up * ceil_div(n, kTileCols[shape]);
+    };
     Plan p;
     if (avg <= 32) p.shape = k32x128;
     else if (avg <= 64) p.shape = k64x128;
     else {
         p.shape = large ? k256x256 : k128x128;
-        for (int shape : {k128x128, k64x64})
+        for (int shape : {k128x128, k64x128, k64x64})
             if (tile_time(shape, tiles(shape)) < tile_time(p.shape, tiles(p.shape))) p.shape = shape;
     }
     const int64_t want = kComputeUnits / std::max<int64_t>(tiles(p.shape), 1), have = m / (4 * 128);
@@ -87,6 +91,19 @@ Plan product_plan(int64_t rows, int64_t groups, int64_t m, int64_t n, bool large
     return p;
 }
 size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (size_t)splits * rows * up4(n) * 4 : 0; }
+
+// Codes whose rows do not begin and end on 16-byte borders pass registers on their way to LDS, which takes 2 to 3.5 times as long;
+// where the product is long enough they are copied once per call into rows that do, if the scratch has room.
+// PLACEHOLDER
+struct Codes {
+    const void *p;
+    int64_t ld, stride, rows, cols, count;
+    // (distances of a tile's rows go into 32 bits)
+    bool bad() const { return !aligned(p, 16) || (ld | (count > 1 ? stride : 0) | cols) % 16 != 0 || ld >= (1 << 22); }
+    int64_t whole() const { return ceil_div(cols, 16) * 16; }
+    size_t bytes() const { return (size_t)count * rows * whole(); }
+};
+bool worth_copies(size_t bytes, double flops) { return 5e-6 + 2.0 * bytes / 4.5e12 < flops / 0.9e15; }
 
 // A matrix of entries of e bytes: rows x cols, ld from row to row.
 int check_matrix(const void *p, int64_t ld, int64_t rows, int64_t cols, int e)
@@ -190,24 +207,38 @@ int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float 
     if (!aligned(offsets, 8)) return bad(kMisaligned);
     if (stride_b < 0 || stride_bs < 0) return bad("negative stride");
     if (rows == 0) return NMF_OK;
-    // chunks of 16 bytes go to LDS without passing registers where rows begin and end on 16-byte borders, and distances fit 32 bits
-    const int64_t far = (int64_t)1 << 30;
-    const bool dma = aligned(X8, 16) && aligned(B8, 16) && (ldx | ldb | (groups > 1 ? stride_b : 0) | m | (transposed ? 0 : n)) % 16 == 0 &&
-                     ldx * 256 < far && ldb * 256 < far && ldxs * 4 * 256 < far;
+    // (tiles of the smallest shapes, in as many parts as there can be; the parts' joins)
+    const int64_t most = std::max((ceil_div(rows, 32) + groups) * ceil_div(n, 64), kMaxSplits * (groups + ceil_div(rows, 32)) + rows * ceil_div(n, 1024));
+    if (most > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
+    Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, b_rows, b_cols, stride_b ? groups : 1};
+    Codes *const operands[] = {&x, &b};
+    const size_t copies = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
+    char *scratch = static_cast<char *>(work);
+    bool dma = copies == 0 && ldxs < (1 << 20);
+    if (copies && copies <= work_bytes && ldxs < (1 << 20) && worth_copies(copies, 2.0 * rows * m * n)) {
+        for (Codes *c : operands) {
+            if (!c->bad()) continue;
+            if ((rc = launched(launch_whole_rows(c->p, c->ld, c->stride, c->rows, c->cols, c->count, scratch, c->whole(), static_cast<hipStream_t>(stream))))) return rc;
+            c->p = scratch;
+            c->ld = c->whole();
+            c->stride = c->count > 1 ? c->whole() * c->rows : 0;
+            scratch += c->bytes();
+            work_bytes -= c->bytes();
+        }
+        dma = true;
+    }
     const Plan plan = product_plan(rows, groups, m, n, dma && type != NMF_F32);
     Product8 p = {};
-    p.x = X8; p.ldx = ldx; p.xs = xscale; p.ldxs = ldxs; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
-    p.b = B8; p.ldb = ldb; p.stride_b = stride_b; p.bs = bscale; p.ldbs = ldbs; p.stride_bs = stride_bs; p.transposed = transposed != 0;
+    p.x = x.p; p.ldx = x.ld; p.xs = xscale; p.ldxs = ldxs; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
+    p.b = b.p; p.ldb = b.ld; p.stride_b = b.stride; p.bs = bscale; p.ldbs = ldbs; p.stride_bs = stride_bs; p.transposed = transposed != 0;
     p.type = type; p.y = Y; p.ldy = ldy;
     p.dma = dma;
     p.shape = plan.shape;
     p.splits = plan.splits;
     while (p.splits > 1 && product_part(rows, n, p.splits) > work_bytes) --p.splits;
-    p.part = static_cast<float *>(work);
+    p.part = reinterpret_cast<float *>(scratch);
     p.k_split = ceil_div(blocks_of(m), p.splits);
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;
-    const int64_t grid = (ceil_div(rows, kTileRows[p.shape]) + groups) * ceil_div(n, kTileCols[p.shape]) * p.splits;
-    if (std::max(grid, p.splits > 1 ? rows * ceil_div(n, 1024) : 0) > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
     return launched(launch_product8(p, static_cast<hipStream_t>(stream)));
 }
 
@@ -316,11 +347,18 @@ int nmf_collect_gradient(int32_t type, const void *dY, int64_t ldy, int64_t rows
 
 size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts)
 {
+    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ONE_B);
+    kind &= ~odd;
     if (!size_ok(rows) || !size_ok(m)) return 0;
     if (kind == 0) return rows > kRouteAlone && m <= NMF_ROUTE_MAX_GROUPS ? route_bytes(ceil_div(rows, kRouteRows), m) : 0;
     if (kind == 1) return m <= NMF_NORM_MAX_M ? norm_bytes(norm_parts(rows, m), m) : 0;
     if (kind != 2 || !size_ok(n) || parts < 1) return 0;
-    return std::max(product_part(rows, n, product_plan(rows, parts, m, n, true).splits), product_part(rows, n, product_plan(rows, parts, m, n, false).splits));
+    const int64_t count = odd & NMF_ONE_B ? 1 : parts;
+    size_t copies = 0;
+    if (m % 16 || (odd & NMF_ODD_X)) copies += (size_t)rows * ceil_div(m, 16) * 16;
+    if (m % 16 || n % 16 || (odd & NMF_ODD_B)) copies += (size_t)count * std::max(m * ceil_div(n, 16), n * ceil_div(m, 16)) * 16;
+    if (!worth_copies(copies, 2.0 * rows * m * n)) copies = 0;
+    return copies + std::max(product_part(rows, n, product_plan(rows, parts, m, n, true).splits), product_part(rows, n, product_plan(rows, parts, m, n, false).splits));
 }
 
 }  // extern "C"

@@ -130,6 +130,8 @@ struct Product8 {
     float *part;                            // splits x rows x (n rounded up to 4), where there are several
     bool vec;                               // rows of y begin on 16-byte borders
 };
+// `count` matrices of codes with rows of ldo, a multiple of 16, zero behind their ends.
+hipError_t launch_whole_rows(const void *src, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t count, void *dst, int64_t ldo, hipStream_t st);
 hipError_t launch_product8(const Product8 &p, hipStream_t st);
 
 }  // namespace routed

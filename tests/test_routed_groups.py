@@ -390,3 +390,29 @@ def test_balance_is_one_where_all_groups_are_equal():
     l = torch.zeros(64, groups, device="cuda")
     l[:, 0] = 50.0                                            # all rows to the first group
     assert abs(float(route(l, 1, False)[4]) - groups) < 1e-4
+
+
+@gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("what", ["widths", "x", "b", "one"])
+def test_product8_copies_rows_that_are_not_whole(what, transposed):
+    """Long products of rows that do not begin or end on 16 bytes, with the scratch that copies take, with less, and with none."""
+    g = torch.Generator(device="cuda").manual_seed(14)
+    rows, groups, m, n = 3000, 2, 1500 if what in ("widths", "one") else 1504, 1501 if what in ("widths", "one") else 1504
+    cut = torch.tensor([3, 1700, 2990])
+    inside = (torch.arange(rows, device="cuda") >= 3) & (torch.arange(rows, device="cuda") < 2990)
+    shape = (n, m) if transposed else (m, n)
+    x, b = codes(g, 1, rows, m), codes(g, 1 if what == "one" else groups, *shape)
+    xs, bs = torch.rand(rows, 12, generator=g, device="cuda"), torch.rand(b.shape[0], 12, 12, generator=g, device="cuda") / 1e4
+    X, B = strided(x, 1 if what == "x" else 0, 0)[0], strided(b, 0, 5 if what == "b" else 0)
+    if what == "one":
+        B, bs = B.expand(groups, *shape), bs.expand(groups, 12, 12)
+    want, size = product(x[0], xs, b.expand(groups, *shape), bs, cut, transposed)
+    need = nmf.nmf_routed_work_bytes(2 | {"x": nmf.NMF_ODD_X, "b": nmf.NMF_ODD_B, "one": nmf.NMF_ONE_B, "widths": 0}[what], rows, m, n, groups)
+    assert need >= rows * m if what == "x" else need >= m * n
+    for work in (None, need, need - 16, 0):
+        Y = torch.full((rows, n), 77.0, dtype=torch.bfloat16, device="cuda")
+        nmf.nmf_grouped_product8(X, xs, cut.cuda(), groups, rows, B, bs, transposed, m, n, Y,
+                                 work=None if work is None else torch.full((work,), 255, dtype=torch.uint8, device="cuda"))
+        holds(Y, want, size, m, "bf16", inside)
+        assert bool((Y[~inside] == 77).all())
