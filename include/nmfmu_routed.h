@@ -14,7 +14,8 @@
  *   - Codes are e4m3 (one sign, four exponent, three fraction bits; largest 448, no infinities), one byte each.  A block of
  *     codes stands for code * scale.  Rows have a scale for each 128 columns: float, rows x ceil(m / 128).  Matrices have one
  *     for each 128 x 128: ceil(m / 128) x ceil(n / 128) for an m x n matrix, in the layout that the matrix has.
- *     scale = max(largest magnitude / 448, 2^-126); a block with an entry that is not finite has the scale NaN and codes 0.
+ *     scale = max(largest magnitude / 448, 2^-126), and codes are the nearest ones to entry / scale, the even one of two; a block
+ *     with an entry that is not finite has the scale NaN and codes 0.
  *   - place: device, int32[rows x k]: where choice j of row r lies among the sorted rows, at [r k + j]; places are distinct.
  *     A place outside [0, sorted rows) stands for no choice (nmf_route writes -1).  Sorted rows that no place names are not
  *     written.

@@ -495,14 +495,6 @@ def _codes(t, what):
     return t.dtype
 
 
-def _maybe_rows(t, dtype, device, rows, cols, what):
-    return (None, 0) if t is None else _rows_of(t, dtype, device, rows, cols, what)
-
-
-def _maybe_list(t, dtype, device, count, what):
-    return None if t is None else _list(t, dtype, device, count, what)
-
-
 @functools.lru_cache(maxsize=1024)
 def _need_routed(kind, rows, m, n, parts) -> int:
     return int(lib().nmf_routed_work_bytes(kind, rows, m, n, parts))
@@ -518,13 +510,13 @@ def nmf_rms_norm(X, rows, m, eps, weight=None, R=None, H=None, Y=None, Y8=None, 
     if d != _current_device():
         return _call_on(d, nmf_rms_norm, X, rows, m, eps, weight, R, H, Y, Y8, scale, rstd, stream)
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
-    r, ldr = _maybe_rows(R, dt, d, rows, m, "R")
-    h, ldh = _maybe_rows(H, dt, d, rows, m, "H")
-    y, ldy = _maybe_rows(Y, dt, d, rows, m, "Y")
+    r, ldr = (None, 0) if R is None else _rows_of(R, dt, d, rows, m, "R")
+    h, ldh = (None, 0) if H is None else _rows_of(H, dt, d, rows, m, "H")
+    y, ldy = (None, 0) if Y is None else _rows_of(Y, dt, d, rows, m, "Y")
     y8, ldy8 = (None, 0) if Y8 is None else _rows_of(Y8, _codes(Y8, "Y8"), d, rows, m, "Y8")
-    s, lds = _maybe_rows(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
-    _check(lib().nmf_rms_norm(typ, x, ldx, r, ldr, _maybe_list(weight, dt, d, m, "weight"), rows, m, eps, h, ldh, y, ldy, y8, ldy8, s, lds,
-                              _maybe_list(rstd, torch.float32, d, rows, "rstd"), _stream_at(d, stream)))
+    s, lds = (None, 0) if scale is None else _rows_of(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
+    _check((_lib or lib()).nmf_rms_norm(typ, x, ldx, r, ldr, None if weight is None else _list(weight, dt, d, m, "weight"), rows, m, eps, h, ldh, y, ldy, y8, ldy8, s, lds,
+                              None if rstd is None else _list(rstd, torch.float32, d, rows, "rstd"), _stream_at(d, stream)))
 
 
 def nmf_rms_norm_gradient(H, rstd, dY, rows, m, dX, weight=None, dH=None, dweight=None, work=None, stream=None) -> None:
@@ -534,11 +526,11 @@ def nmf_rms_norm_gradient(H, rstd, dY, rows, m, dX, weight=None, dH=None, dweigh
         return _call_on(d, nmf_rms_norm_gradient, H, rstd, dY, rows, m, dX, weight, dH, dweight, work, stream)
     h, ldh = _rows_of(H, dt, d, rows, m, "H")
     dy, ldy = _rows_of(dY, dt, d, rows, m, "dY")
-    dh, lddh = _maybe_rows(dH, dt, d, rows, m, "dH")
+    dh, lddh = (None, 0) if dH is None else _rows_of(dH, dt, d, rows, m, "dH")
     dx, ldx = _rows_of(dX, dt, d, rows, m, "dX")
     w, nbytes, _keep = _scratch(0 if dweight is None else _need_routed(1, rows, m, 0, 0), work, d, stream)
-    _check(lib().nmf_rms_norm_gradient(typ, h, ldh, _list(rstd, torch.float32, d, rows, "rstd"), _maybe_list(weight, dt, d, m, "weight"), dy, ldy,
-                                       dh, lddh, rows, m, dx, ldx, _maybe_list(dweight, dt, d, m, "dweight"), w, nbytes, _stream_at(d, stream)))
+    _check((_lib or lib()).nmf_rms_norm_gradient(typ, h, ldh, _list(rstd, torch.float32, d, rows, "rstd"), None if weight is None else _list(weight, dt, d, m, "weight"), dy, ldy,
+                                       dh, lddh, rows, m, dx, ldx, None if dweight is None else _list(dweight, dt, d, m, "dweight"), w, nbytes, _stream_at(d, stream)))
 
 
 def nmf_round_blocks(X, rows, m, block, X8, scale, stream=None) -> None:
@@ -558,7 +550,7 @@ def nmf_round_blocks(X, rows, m, block, X8, scale, stream=None) -> None:
         x, ldx = _rows_of(X, dt, d, rows, m, "X")
         x8, ldx8 = _rows_of(X8, codes, d, rows, m, "X8")
         s, lds = _rows_of(scale, torch.float32, d, lines, M, "scale")
-    _check(lib().nmf_round_blocks(typ, x, ldx, stride, count, rows, m, block, x8, ldx8, stride8, s, lds, stride_s, _stream_at(d, stream)))
+    _check((_lib or lib()).nmf_round_blocks(typ, x, ldx, stride, count, rows, m, block, x8, ldx8, stride8, s, lds, stride_s, _stream_at(d, stream)))
 
 
 def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transposed, m, n, Y, work=None, stream=None) -> None:
@@ -576,7 +568,7 @@ def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transpos
     if stride_b == 0:
         odd |= NMF_ONE_B
     w, nbytes, _keep = _scratch(_need_routed(2 | odd, rows, m, n, groups) if work is None else 0, work, d, stream)
-    _check(lib().nmf_grouped_product8(typ, x, ldx, xs, ldxs, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
+    _check((_lib or lib()).nmf_grouped_product8(typ, x, ldx, xs, ldxs, _list(offsets, torch.int64, d, groups + 1, "offsets"), groups, rows, b, ldb, stride_b,
                                       bs, ldbs, stride_bs, int(bool(transposed)), m, n, y, ldy, w, nbytes, _stream_at(d, stream)))
 
 
@@ -587,7 +579,7 @@ def nmf_route(logits, rows, groups, k, normalise, choice, gate, offsets, place, 
         return _call_on(d, nmf_route, logits, rows, groups, k, normalise, choice, gate, offsets, place, balance, work, stream)
     l, ldl = _rows_of(logits, logits.dtype, d, rows, groups, "logits")
     w, nbytes, _keep = _scratch(_need_routed(0, rows, groups, 0, 0), work, d, stream)
-    _check(lib().nmf_route(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
+    _check((_lib or lib()).nmf_route(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
                            _list(gate, torch.float32, d, rows * k, "gate"), _list(offsets, torch.int64, d, groups + 1, "offsets"),
                            _list(place, torch.int32, d, rows * k, "place"), _list(balance, torch.float32, d, 1, "balance"), w, nbytes,
                            _stream_at(d, stream)))
@@ -600,9 +592,9 @@ def nmf_route_gradient(logits, rows, groups, k, normalise, choice, offsets, dgat
         return _call_on(d, nmf_route_gradient, logits, rows, groups, k, normalise, choice, offsets, dgate, dbalance, dlogits, stream)
     l, ldl = _rows_of(logits, logits.dtype, d, rows, groups, "logits")
     dl, lddl = _rows_of(dlogits, logits.dtype, d, rows, groups, "dlogits")
-    _check(lib().nmf_route_gradient(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
-                                    _list(offsets, torch.int64, d, groups + 1, "offsets"), _maybe_list(dgate, torch.float32, d, rows * k, "dgate"),
-                                    _maybe_list(dbalance, torch.float32, d, 1, "dbalance"), dl, lddl, _stream_at(d, stream)))
+    _check((_lib or lib()).nmf_route_gradient(typ, l, ldl, rows, groups, k, int(bool(normalise)), _list(choice, torch.int32, d, rows * k, "choice"),
+                                    _list(offsets, torch.int64, d, groups + 1, "offsets"), None if dgate is None else _list(dgate, torch.float32, d, rows * k, "dgate"),
+                                    None if dbalance is None else _list(dbalance, torch.float32, d, 1, "dbalance"), dl, lddl, _stream_at(d, stream)))
 
 
 def nmf_spread_rows(X, rows, k, place, m, Y, scale=None, Yscale=None, stream=None) -> None:
@@ -614,9 +606,9 @@ def nmf_spread_rows(X, rows, k, place, m, Y, scale=None, Yscale=None, stream=Non
     x, ldx = _rows_of(X, dt, d, rows, m, "X")
     count = Y.shape[0]
     y, ldy = _rows_of(Y, dt, d, count, m, "Y")
-    xs, ldxs = _maybe_rows(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
-    ys, ldys = _maybe_rows(Yscale, torch.float32, d, count, (m + 127) // 128, "Yscale")
-    _check(lib().nmf_spread_rows(typ, x, ldx, rows, k, _list(place, torch.int32, d, rows * k, "place"), m, y, ldy, count, xs, ldxs, ys, ldys,
+    xs, ldxs = (None, 0) if scale is None else _rows_of(scale, torch.float32, d, rows, (m + 127) // 128, "scale")
+    ys, ldys = (None, 0) if Yscale is None else _rows_of(Yscale, torch.float32, d, count, (m + 127) // 128, "Yscale")
+    _check((_lib or lib()).nmf_spread_rows(typ, x, ldx, rows, k, _list(place, torch.int32, d, rows * k, "place"), m, y, ldy, count, xs, ldxs, ys, ldys,
                                  _stream_at(d, stream)))
 
 
@@ -627,8 +619,8 @@ def nmf_collect_rows(X, rows, k, place, gate, m, Y, stream=None) -> None:
         return _call_on(d, nmf_collect_rows, X, rows, k, place, gate, m, Y, stream)
     x, ldx = _rows_of(X, dt, d, X.shape[0], m, "X")
     y, ldy = _rows_of(Y, dt, d, rows, m, "Y")
-    _check(lib().nmf_collect_rows(typ, x, ldx, X.shape[0], rows, k, _list(place, torch.int32, d, rows * k, "place"),
-                                  _maybe_list(gate, torch.float32, d, rows * k, "gate"), m, y, ldy, _stream_at(d, stream)))
+    _check((_lib or lib()).nmf_collect_rows(typ, x, ldx, X.shape[0], rows, k, _list(place, torch.int32, d, rows * k, "place"),
+                                  None if gate is None else _list(gate, torch.float32, d, rows * k, "gate"), m, y, ldy, _stream_at(d, stream)))
 
 
 def nmf_collect_gradient(dY, rows, k, place, gate, m, dX, X=None, dgate=None, stream=None) -> None:
@@ -639,7 +631,7 @@ def nmf_collect_gradient(dY, rows, k, place, gate, m, dX, X=None, dgate=None, st
     dy, ldy = _rows_of(dY, dt, d, rows, m, "dY")
     count = dX.shape[0]
     dx, lddx = _rows_of(dX, dt, d, count, m, "dX")
-    x, ldx = _maybe_rows(X, dt, d, count, m, "X")
-    _check(lib().nmf_collect_gradient(typ, dy, ldy, rows, k, _list(place, torch.int32, d, rows * k, "place"),
-                                      _maybe_list(gate, torch.float32, d, rows * k, "gate"), m, dx, lddx, count, x, ldx,
-                                      _maybe_list(dgate, torch.float32, d, rows * k, "dgate"), _stream_at(d, stream)))
+    x, ldx = (None, 0) if X is None else _rows_of(X, dt, d, count, m, "X")
+    _check((_lib or lib()).nmf_collect_gradient(typ, dy, ldy, rows, k, _list(place, torch.int32, d, rows * k, "place"),
+                                      None if gate is None else _list(gate, torch.float32, d, rows * k, "gate"), m, dx, lddx, count, x, ldx,
+                                      None if dgate is None else _list(dgate, torch.float32, d, rows * k, "dgate"), _stream_at(d, stream)))

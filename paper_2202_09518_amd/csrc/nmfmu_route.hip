@@ -9,7 +9,8 @@ namespace routed {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 1024;      // of a block of rows: a compute unit's worth, as choices follow each other and wait for lanes
+constexpr int kFew = 256;           // of what comes behind
 
 // Logits as integers in the order that rows choose by: larger first, then the lower group.  0: never chosen.
 __device__ __forceinline__ unsigned order_of(float x)
@@ -49,8 +50,7 @@ template <class T, int W, int C> struct Logits {
         float most = x[0];
 #pragma unroll
         for (int c = 1; c < C; ++c) most = __builtin_fmaxf(most, x[c]);
-#pragma unroll
-        for (int d = 1; d < W; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+        most = most_of<W>(most);
         float sum = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -61,26 +61,25 @@ template <class T, int W, int C> struct Logits {
     }
 };
 
-// Choices of up to kRouteRows rows from `base` on: choice and gate to memory, which rows chose a group to `mask` (a bit for
-// each row, zeroed before), c_r p_rg summed over the thread's rows to share[].
+// Choices of up to kRouteRows rows from `base` on: choice and gate to memory, choice to `picked` too, which rows chose a group to
+// `mask` (a bit for each row, zeroed before), c_r p_rg summed over the thread's rows to share[].
 template <class T, int W, int C>
-__device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned long long *mask, float (&share)[C])
+__device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned long long *mask, int *picked, float (&share)[C])
 {
     constexpr int ROWS = kThreads / W;
     const int lane = threadIdx.x % W;
 #pragma unroll
-    for (int r = 0; r < kRouteRows / ROWS; ++r) {
+    for (int r = 0; r < (kRouteRows + ROWS - 1) / ROWS; ++r) {
         const int in = r * ROWS + threadIdx.x / W;
         const int64_t row = base + in;
-        const bool is = row < a.rows;
+        const bool is = row < a.rows && in < kRouteRows;
         if (base + r * ROWS >= a.rows) break;
         Logits<T, W, C> l;
         l.load((const T *)a.logits + row * a.ldl, a.groups, is);
         unsigned key[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) key[c] = order_of(l.x[c]);
-        const float sum = l.exponents();
-        // the largest key of all that is left, and of equals the lowest group
+        const float one = 1.f / l.exponents();
         int mine = 0;
         float total = 0.f;
         constexpr int N = W < NMF_ROUTE_MAX_K ? NMF_ROUTE_MAX_K / W : 1;      // lane j % W keeps choice j
@@ -89,24 +88,22 @@ __device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned lo
 #pragma unroll
         for (int n = 0; n < N; ++n) gate[n] = 0.f, choice[n] = -1;
         for (int j = 0; j < a.k; ++j) {
-            unsigned best = key[0];
-            int at = 0;
+            // the largest key of all that is left, and the lowest group that has it
+            unsigned best = key[0], at = ~0u;
 #pragma unroll
-            for (int c = 1; c < C; ++c)
-                if (key[c] > best) best = key[c], at = c;
-            int group = l.first + at;
-#pragma unroll
-            for (int d = 1; d < W; d <<= 1) {
-                const unsigned o = (unsigned)__shfl_xor((int)best, d);
-                const int g = __shfl_xor(group, d);
-                if (o > best || (o == best && g < group)) best = o, group = g;
-            }
+            for (int c = 1; c < C; ++c) best = key[c] > best ? key[c] : best;
+            best = most_of<W>(best);
             if (best == 0) break;
+#pragma unroll
+            for (int c = C - 1; c >= 0; --c) at = key[c] == best ? (unsigned)(l.first + c) : at;
+            const int group = (int)least_of<W>(at);
             float e = 0.f;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (l.first + c == group) key[c] = 0, e = l.x[c];
-            const float p = __shfl(e, group / C, W) / sum;
+            for (int c = 0; c < C; ++c) {
+                e = l.first + c == group ? l.x[c] : e;
+                key[c] = l.first + c == group ? 0 : key[c];
+            }
+            const float p = __shfl(e, group / C, W) * one;
             total += p;
             ++mine;
 #pragma unroll
@@ -119,12 +116,13 @@ __device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned lo
                 const int j = lane + n * W, g = choice[n];
                 if (j >= a.k) continue;
                 a.choice[row * a.k + j] = g;
+                picked[in * a.k + j] = g;
                 a.gate[row * a.k + j] = g >= 0 && a.normalise ? gate[n] / total : gate[n];
                 if (g >= 0) atomicOr(&mask[g], 1ull << in);
             }
             if (mine) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) share[c] += (float)mine * (l.x[c] / sum);
+                for (int c = 0; c < C; ++c) share[c] += (float)mine * (l.x[c] * one);
             }
         }
     }
@@ -146,9 +144,9 @@ template <int W, int C> __device__ __forceinline__ void add_share(const float (&
 }
 
 // Sums before each entry of `count` (up to 1024) to `before`, by the whole workgroup; returns the sum of all.
-__device__ __forceinline__ int64_t sums_before(const int64_t *count, int n, int64_t *before, int64_t *meet)
+template <int THREADS> __device__ __forceinline__ int64_t sums_before(const int64_t *count, int n, int64_t *before, int64_t *meet)
 {
-    constexpr int E = NMF_ROUTE_MAX_GROUPS / kThreads;
+    constexpr int E = NMF_ROUTE_MAX_GROUPS / THREADS;
     int64_t x[E], sum = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -165,7 +163,7 @@ __device__ __forceinline__ int64_t sums_before(const int64_t *count, int n, int6
     if ((threadIdx.x & 63) == 63) meet[threadIdx.x / 64] = up;
     __syncthreads();
     int64_t base = up - sum, all = 0;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < (int)(threadIdx.x / 64)) base += meet[w];
         all += meet[w];
     }
@@ -180,22 +178,26 @@ __device__ __forceinline__ int64_t sums_before(const int64_t *count, int n, int6
 }
 
 // groups * sum of count / C * mass / C, by the whole workgroup.
-template <class M> __device__ __forceinline__ double balance_of(const int64_t *count, const M *mass, int groups, int64_t all, double *meet)
+template <int THREADS> __device__ __forceinline__ double balance_of(const int64_t *count, const double *mass, int groups, int64_t all, double *meet)
 {
     double x = 0.;
-    for (int g = threadIdx.x; g < groups; g += kThreads) x += (double)count[g] * (double)mass[g];
+    for (int g = threadIdx.x; g < groups; g += THREADS) x += (double)count[g] * mass[g];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
     if ((threadIdx.x & 63) == 0) meet[threadIdx.x / 64] = x;
     __syncthreads();
     x = 0.;
-    for (int w = 0; w < kThreads / 64; ++w) x += meet[w];
+    for (int w = 0; w < THREADS / 64; ++w) x += meet[w];
     return all ? x * groups / ((double)all * (double)all) : 0.;
 }
 
 }  // namespace
 
-// All rows by one workgroup: for few rows, and for calls without scratch.  Places are first those within the group.
+// Place of choice i of a block within the block's part of its group.
+__device__ __forceinline__ int place_in(const unsigned long long *mask, int g, int row) { return __popcll(mask[g] & ((1ull << row) - 1)); }
+
+// All rows by one workgroup: for few rows, and for calls without scratch.  With more than one block of rows, places are first those
+// within the group.
 template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void route_one_kernel(Route a)
 {
     constexpr int G = W * C;
@@ -203,6 +205,8 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
     __shared__ int64_t count[G], before[G], meet[kThreads / 64];
     __shared__ double mass[G], meet_d[kThreads / 64];
     __shared__ float lds[kThreads * C], part[G];
+    __shared__ int picked[kRouteRows * NMF_ROUTE_MAX_K];
+    const bool several = a.rows > kRouteRows;
     for (int g = threadIdx.x; g < a.groups; g += kThreads) count[g] = 0, mass[g] = 0.;
     for (int64_t base = 0; base < a.rows; base += kRouteRows) {
         for (int g = threadIdx.x; g < a.groups; g += kThreads) mask[g] = 0;
@@ -210,13 +214,14 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
         float share[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) share[c] = 0.f;
-        choose<T, W, C>(a, base, mask, share);
-        __syncthreads();
+        choose<T, W, C>(a, base, mask, picked, share);
         add_share<W, C>(share, a.groups, lds, part);
-        const int64_t here = std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
-        for (int64_t i = threadIdx.x; i < here; i += kThreads) {
-            const int g = a.choice[base * a.k + i];
-            a.place[base * a.k + i] = g < 0 ? -1 : (int)(count[g] + __popcll(mask[g] & ((1ull << (i / a.k)) - 1)));
+        if (several) {
+            const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
+            for (int i = threadIdx.x; i < here; i += kThreads) {
+                const int g = picked[i];
+                a.place[base * a.k + i] = g < 0 ? -1 : (int)count[g] + place_in(mask, g, i / a.k);
+            }
         }
         __syncthreads();
         for (int g = threadIdx.x; g < a.groups; g += kThreads) {
@@ -225,13 +230,14 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
         }
     }
     __syncthreads();
-    const int64_t all = sums_before(count, a.groups, before, meet);
+    const int64_t all = sums_before<kThreads>(count, a.groups, before, meet);
     for (int64_t i = threadIdx.x; i < a.rows * a.k; i += kThreads) {
-        const int g = a.choice[i];
-        if (g >= 0) a.place[i] += (int)before[g];
+        const int g = several ? a.choice[i] : picked[i];
+        if (!several) a.place[i] = g < 0 ? -1 : (int)before[g] + place_in(mask, g, (int)i / a.k);
+        else if (g >= 0) a.place[i] += (int)before[g];
     }
     for (int g = threadIdx.x; g < a.groups; g += kThreads) a.offsets[g] = before[g];
-    const double b = balance_of(count, mass, a.groups, all, meet_d);
+    const double b = balance_of<kThreads>(count, mass, a.groups, all, meet_d);
     if (threadIdx.x == 0) {
         a.offsets[a.groups] = all;
         a.balance[0] = (float)b;
@@ -243,33 +249,35 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
 {
     __shared__ unsigned long long mask[W * C];
     __shared__ float lds[kThreads * C];
+    __shared__ int picked[kRouteRows * NMF_ROUTE_MAX_K];
     for (int g = threadIdx.x; g < a.groups; g += kThreads) mask[g] = 0;
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kRouteRows;
     float share[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) share[c] = 0.f;
-    choose<T, W, C>(a, base, mask, share);
-    __syncthreads();
+    choose<T, W, C>(a, base, mask, picked, share);
     add_share<W, C>(share, a.groups, lds, a.share + (int64_t)blockIdx.x * a.groups);
-    const int64_t here = std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
-    for (int64_t i = threadIdx.x; i < here; i += kThreads) {
-        const int g = a.choice[base * a.k + i];
-        a.place[base * a.k + i] = g < 0 ? -1 : __popcll(mask[g] & ((1ull << (i / a.k)) - 1));
+    const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
+    for (int i = threadIdx.x; i < here; i += kThreads) {
+        const int g = picked[i];
+        a.place[base * a.k + i] = g < 0 ? -1 : place_in(mask, g, i / a.k);
     }
     for (int g = threadIdx.x; g < a.groups; g += kThreads) a.count[(int64_t)blockIdx.x * a.groups + g] = __popcll(mask[g]);
 }
 
-// Counts of a group in all blocks to sums before each block: a group to each column of 16 threads' rows.
-__global__ __launch_bounds__(kThreads) void route_sums_kernel(Route a)
+// Counts of a group in all blocks to the sums before each block: 16 groups to a workgroup, 64 runs of blocks to each.
+__global__ __launch_bounds__(1024) void route_sums_kernel(Route a)
 {
-    __shared__ int64_t sums[16][17];
-    __shared__ double masses[16][17];
+    constexpr int RUNS = 64;
+    __shared__ int sums[RUNS][17];
+    __shared__ double masses[RUNS][17];
     const int c = threadIdx.x & 15, r = threadIdx.x >> 4, g = blockIdx.x * 16 + c;
-    const int64_t each = (a.blocks + 15) / 16, b0 = r * each, b1 = std::min<int64_t>(b0 + each, a.blocks);
-    int64_t sum = 0;
+    const int64_t each = (a.blocks + RUNS - 1) / RUNS, b0 = r * each, b1 = std::min<int64_t>(b0 + each, a.blocks);
+    int sum = 0;
     double mass = 0.;
     if (g < a.groups)
+#pragma unroll 4
         for (int64_t b = b0; b < b1; ++b) {
             sum += a.count[b * a.groups + g];
             mass += (double)a.share[b * a.groups + g];
@@ -278,39 +286,74 @@ __global__ __launch_bounds__(kThreads) void route_sums_kernel(Route a)
     masses[r][c] = mass;
     __syncthreads();
     if (g >= a.groups) return;
-    int64_t before = 0, all = 0;
-    mass = 0.;
-    for (int i = 0; i < 16; ++i) {
-        if (i < r) before += sums[i][c];
-        all += sums[i][c];
-        mass += masses[i][c];
+    int before = 0;
+    for (int i = 0; i < r; ++i) before += sums[i][c];
+    if (r == RUNS - 1) {
+        mass = 0.;
+        for (int i = 0; i < RUNS; ++i) mass += masses[i][c];
+        a.total[g] = before + sum;
+        a.mass[g] = mass;
     }
+#pragma unroll 4
     for (int64_t b = b0; b < b1; ++b) {
         const int64_t at = b * a.groups + g;
         const int n = a.count[at];
-        a.count[at] = (int)before;
+        a.count[at] = before;
         before += n;
-    }
-    if (r == 0) {
-        a.total[g] = all;
-        a.mass[g] = mass;
     }
 }
 
-__global__ __launch_bounds__(kThreads) void route_place_kernel(Route a)
+// 512 rows to 4 of 64 groups: 11.0 us, 13.7 with the launch in between; 2048 rows, 32 blocks to add up: 17.0 and 13.9.
+constexpr int kFewBlocks = 8;
+
+// Places among all rows.  SUMS: of few blocks, whose counts each workgroup adds up itself instead of a launch in between.
+template <bool SUMS> __global__ __launch_bounds__(kFew) void route_place_kernel(Route a)
 {
-    __shared__ int64_t before[NMF_ROUTE_MAX_GROUPS], meet[kThreads / 64];
-    __shared__ double meet_d[kThreads / 64];
-    const int64_t all = sums_before(a.total, a.groups, before, meet);
+    __shared__ int64_t before[NMF_ROUTE_MAX_GROUPS], meet[kFew / 64];
+    __shared__ double meet_d[kFew / 64];
+    __shared__ int64_t totals[SUMS ? NMF_ROUTE_MAX_GROUPS : 1];
+    __shared__ double masses[SUMS ? NMF_ROUTE_MAX_GROUPS : 1];
+    __shared__ int earlier[SUMS ? NMF_ROUTE_MAX_GROUPS : 1];
+    constexpr int E = kRouteRows * NMF_ROUTE_MAX_K / kFew;      // choices of a thread
     const int64_t base = (int64_t)blockIdx.x * kRouteRows;
-    const int64_t here = std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
-    for (int64_t i = threadIdx.x; i < here; i += kThreads) {
-        const int g = a.choice[base * a.k + i];
-        if (g >= 0) a.place[base * a.k + i] += (int)before[g] + a.count[(int64_t)blockIdx.x * a.groups + g];
+    const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
+    int group[E], in[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int i = threadIdx.x + e * kFew;
+        group[e] = i < here ? a.choice[base * a.k + i] : -1;
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (group[e] >= 0) {
+            in[e] = a.place[base * a.k + threadIdx.x + e * kFew];
+            if (!SUMS) in[e] += a.count[(int64_t)blockIdx.x * a.groups + group[e]];
+        }
+    if constexpr (SUMS) {
+        for (int g = threadIdx.x; g < a.groups; g += kFew) {
+            int sum = 0, mine = 0;
+            double mass = 0.;
+#pragma unroll 8
+            for (int b = 0; b < (int)a.blocks; ++b) {
+                const int n = a.count[b * a.groups + g];
+                if (blockIdx.x == 0) mass += (double)a.share[b * a.groups + g];
+                sum += n;
+                mine += b < (int)blockIdx.x ? n : 0;
+            }
+            totals[g] = sum;
+            masses[g] = mass;
+            earlier[g] = mine;
+        }
+        __syncthreads();
+    }
+    const int64_t *total = SUMS ? totals : a.total;
+    const int64_t all = sums_before<kFew>(total, a.groups, before, meet);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (group[e] >= 0) a.place[base * a.k + threadIdx.x + e * kFew] = in[e] + (int)before[group[e]] + (SUMS ? earlier[group[e]] : 0);
     if (blockIdx.x) return;
-    for (int g = threadIdx.x; g < a.groups; g += kThreads) a.offsets[g] = before[g];
-    const double b = balance_of(a.total, a.mass, a.groups, all, meet_d);
+    for (int g = threadIdx.x; g < a.groups; g += kFew) a.offsets[g] = before[g];
+    const double b = balance_of<kFew>(total, SUMS ? masses : a.mass, a.groups, all, meet_d);
     if (threadIdx.x == 0) {
         a.offsets[a.groups] = all;
         a.balance[0] = (float)b;
@@ -323,8 +366,8 @@ template <class F> void by_groups(int groups, F f)
     using std::integral_constant;
     if (groups <= 32) f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
     else if (groups <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-    else if (groups <= 128) f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
-    else if (groups <= 256) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (groups <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    else if (groups <= 256) f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
     else if (groups <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
     else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
@@ -338,91 +381,104 @@ template <class T> hipError_t launch_route(const Route &a, hipStream_t st)
             return;
         }
         hipLaunchKernelGGL((route_rows_kernel<T, W, C>), dim3((unsigned)a.blocks), dim3(kThreads), 0, st, a);
-        hipLaunchKernelGGL(route_sums_kernel, dim3((unsigned)((a.groups + 15) / 16)), dim3(kThreads), 0, st, a);
-        hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.blocks), dim3(kThreads), 0, st, a);
+        if (a.blocks <= kFewBlocks) {
+            hipLaunchKernelGGL((route_place_kernel<true>), dim3((unsigned)a.blocks), dim3(kFew), 0, st, a);
+        } else {
+            hipLaunchKernelGGL(route_sums_kernel, dim3((unsigned)((a.groups + 15) / 16)), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((route_place_kernel<false>), dim3((unsigned)a.blocks), dim3(kFew), 0, st, a);
+        }
     });
     return hipGetLastError();
 }
 
 // ---- gradient of the logits ------------------------------------------------------------------
-template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void route_gradient_kernel(RouteGradient a)
+template <class T, int W, int C> __global__ __launch_bounds__(kFew) void route_gradient_kernel(RouteGradient a)
 {
-    constexpr int ROWS = kThreads / W;
+    constexpr int ROWS = kFew / W;
     const int first = (int)(threadIdx.x % W) * C;
     float q[C];                                   // d balance / d p_rg, but for c_r
     {
         const int64_t all = a.offsets[a.groups];
         const float up = a.dbalance && all > 0 ? a.dbalance[0] : 0.f;
+        const double unit = all > 0 ? (double)a.groups / ((double)all * (double)all) : 0.;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            q[c] = 0.f;
-            if (a.dbalance && all > 0 && first + c < a.groups)
-                q[c] = up * (float)((double)a.groups * (double)(a.offsets[first + c + 1] - a.offsets[first + c]) / ((double)all * (double)all));
-        }
+        for (int c = 0; c < C; ++c)
+            q[c] = a.dbalance && first + c < a.groups ? up * (float)(unit * (double)(a.offsets[first + c + 1] - a.offsets[first + c])) : 0.f;
     }
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < a.rows; base += (int64_t)gridDim.x * ROWS) {
         const int64_t row = base + threadIdx.x / W;
         const bool is = row < a.rows;
         Logits<T, W, C> l;
         l.load((const T *)a.logits + row * a.ldl, a.groups, is);
-        const float sum = l.exponents();
+        // the lane's own groups among the row's choices, and their gates' gradients
         float d[C];
+        unsigned own = 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            l.x[c] /= sum;                        // p
-            d[c] = 0.f;
-        }
-        // the lane's own groups among the row's choices
+        for (int c = 0; c < C; ++c) d[c] = 0.f;
         int mine = 0;
-        float total = 0.f, dot = 0.f;             // sums over the choices of p and of p dgate
-        for (int j = 0; j < a.k; ++j) {
-            const int g = is ? a.choice[row * a.k + j] : -1;
-            if (g < 0 || g >= a.groups) continue;
-            ++mine;
-            const float dg = a.dgate ? a.dgate[row * a.k + j] : 0.f;
+        for (int j0 = 0; j0 < a.k; j0 += 4) {
+            int g[4];
+            float dg[4];
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (first + c == g) {
-                    total += l.x[c];
-                    dot = __builtin_fmaf(l.x[c], dg, dot);
-                    d[c] = 1.f;
-                }
-        }
-        total = sum_of<W>(total);
-        dot = sum_of<W>(dot);
-        float mean = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) mean = __builtin_fmaf(l.x[c], q[c], mean);
-        mean = sum_of<W>(mean);
-        if (!is) continue;
-        // p_i ([i chosen] dg_i - dot), or, normalised, p_i / total (dg_i - dot / total) of the chosen
-        const float share = a.normalise ? 1.f / total : 1.f, less = a.normalise ? dot / total : dot;
-        float out[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            out[c] = (float)mine * (q[c] - mean);
-            if (!a.normalise) out[c] -= less;
-            else if (d[c] != 0.f) out[c] -= less * share;
-        }
-        if (a.dgate)
-            for (int j = 0; j < a.k; ++j) {
-                const int g = a.choice[row * a.k + j];
-                const float dg = a.dgate[row * a.k + j];
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (first + c == g) out[c] = __builtin_fmaf(dg, share, out[c]);
+            for (int j = 0; j < 4; ++j) {
+                const bool there = is && j0 + j < a.k;
+                g[j] = there ? a.choice[row * a.k + j0 + j] : -1;
+                dg[j] = there && a.dgate ? a.dgate[row * a.k + j0 + j] : 0.f;
             }
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (first + c < a.groups) ((T *)a.dlogits)[row * a.lddl + first + c] = Type<T>::round(mine ? l.x[c] * out[c] : 0.f);
+            for (int j = 0; j < 4; ++j) {
+                if (g[j] < 0 || g[j] >= a.groups) continue;
+                ++mine;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (first + c == g[j]) {
+                        d[c] = dg[j];
+                        own |= 1u << c;
+                    }
+            }
+        }
+        const float one = 1.f / l.exponents();
+        float total = 0.f, dot = 0.f, mean = 0.f;      // sums of p and of p dgate over the choices, of p q over all groups
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            l.x[c] *= one;                        // p
+            if (own >> c & 1) {
+                total += l.x[c];
+                dot = __builtin_fmaf(l.x[c], d[c], dot);
+            }
+            mean = __builtin_fmaf(l.x[c], q[c], mean);
+        }
+        dot = sum_of<W>(dot);
+        mean = sum_of<W>(mean);
+        if (a.normalise) total = sum_of<W>(total);
+        if (!is) continue;
+        // p_i ([i chosen] dg_i - dot), or, normalised, p_i / total (dg_i - dot / total) of the chosen
+        const float share = a.normalise ? 1.f / total : 1.f, less = dot * share;
+        T out[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const bool chosen = own >> c & 1;
+            float x = chosen ? d[c] : 0.f;
+            if (chosen || !a.normalise) x -= less;
+            x = __builtin_fmaf((float)mine, q[c] - mean, x * share);
+            out[c] = Type<T>::round(mine ? l.x[c] * x : 0.f);
+        }
+        T *to = (T *)a.dlogits + row * a.lddl + first;
+        if (first + C <= a.groups) {
+            __builtin_memcpy(to, out, sizeof(out));
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (first + c < a.groups) to[c] = out[c];
+        }
     }
 }
 
 template <class T> hipError_t launch_route_gradient(const RouteGradient &a, hipStream_t st)
 {
     by_groups(a.groups, [&](auto w, auto c) {
-        constexpr int W = w.value, C = c.value, rows = kThreads / W;
-        hipLaunchKernelGGL((route_gradient_kernel<T, W, C>), dim3((unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, 2048)), dim3(kThreads), 0, st, a);
+        constexpr int W = w.value, C = c.value, rows = kFew / W;
+        hipLaunchKernelGGL((route_gradient_kernel<T, W, C>), dim3((unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, 2048)), dim3(kFew), 0, st, a);
     });
     return hipGetLastError();
 }

@@ -73,36 +73,69 @@ template <class T> struct Eight {
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 struct Scale {
-    float scale, inverse;
+    float scale, most, up, back;      // scale is most / 448; up: 1 / scale, back: 512 / most
     bool finite;
 };
-__device__ __forceinline__ Scale scale_of(unsigned most)
+__device__ __forceinline__ Scale scale_of(unsigned bits)
 {
     Scale s;
-    s.finite = most < 0x7f800000u;
-    s.scale = __builtin_fmaxf(__uint_as_float(most) / 448.f, 0x1p-126f);
-    s.inverse = 1.f / s.scale;
-    if (!s.finite) s.scale = __builtin_nanf("");
+    s.finite = bits < 0x7f800000u;
+    s.most = __builtin_fmaxf(__uint_as_float(bits), 0x1.cp-118f);      // 448 2^-126
+    // most / 448 and its inverse, each with its error taken back once
+    constexpr float part = 1.f / 448.f;
+    const float near = s.most * part, scale = __builtin_fmaf(__builtin_fmaf(-near, 448.f, s.most), part, near);
+    const float inverse = __builtin_amdgcn_rcpf(scale);
+    s.up = __builtin_fmaf(__builtin_fmaf(-scale, inverse, 1.f), inverse, inverse);
+    s.back = s.up * (8.f / 7.f);
+    s.scale = s.finite ? scale : __builtin_nanf("");
     return s;
 }
-// Codes of eight entries: x / scale, to the last bit (the quotient's error is taken back once), rounded to nearest even.  No
-// quotient is above 448 by more than 2^-23 of it, so none overflows.
-__device__ __forceinline__ ragged::u32x2 codes_of(const float (&x)[8], const Scale &s)
+__device__ __forceinline__ ragged::u32x2 codes_of(const float (&q)[8], const Scale &s)
 {
     ragged::u32x2 c = {0, 0};
     if (!s.finite) return c;
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        q[i] = x[i] * s.inverse;
-        q[i] = __builtin_fmaf(__builtin_fmaf(-q[i], s.scale, x[i]), s.inverse, q[i]);
-    }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * n], q[4 * n + 1], 0, false);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * n], q[4 * n + 1], 0, false);
         c[n] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * n + 2], q[4 * n + 3], w, true);
     }
     return c;
+}
+// Codes of eight floats: x / scale to its last places, rounded to nearest even.  (At most 448 (1 + 2^-22), which is 448.)
+__device__ __forceinline__ ragged::u32x2 near_codes(const float (&x)[8], const Scale &s)
+{
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = x[i] * s.up;
+    return codes_of(q, s);
+}
+// The same of entries as they are, to the nearest code: the quotient's error, from x 7 / 8 and most quotient / 512 so that nothing
+// overflows, is taken back.  Of 16-bit entries the quotient lies on a border between two codes or 2^-16 away from it.  Of floats it
+// can be nearer than its own last place, so there what is left of it sets that to odd, which no border has; it is looked at only
+// where some quotient of the wave is within four last places of where borders are, multiples of 2^19 of them.
+template <class T> __device__ __forceinline__ ragged::u32x2 exact_codes(const float (&x)[8], const Scale &s)
+{
+    float q[8];
+    bool near = sizeof(T) == 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        q[i] = x[i] * s.up;
+        near |= ((__float_as_uint(q[i]) + 4) & 0x7ffff) <= 8;
+    }
+    if (sizeof(T) == 2 || __any(near)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float part = x[i] * 0.875f, rest = sizeof(T) == 4 ? __builtin_fmaf(x[i], 0.875f, -part) : 0.f;
+            q[i] = __builtin_fmaf(__builtin_fmaf(q[i] * -0x1p-9f, s.most, part) + rest, s.back, q[i]);
+            if (sizeof(T) == 4) {
+                const float left = __builtin_fmaf(q[i] * -0x1p-9f, s.most, part) + rest;
+                unsigned b = __float_as_uint(q[i]);
+                if (left != 0.f) b = (b - ((b ^ __float_as_uint(left)) >> 31)) | 1u;
+                q[i] = __uint_as_float(b);
+            }
+        }
+    }
+    return codes_of(q, s);
 }
 __device__ __forceinline__ void store_codes(unsigned char *row, int64_t col, int64_t m, ragged::u32x2 c)
 {
@@ -115,20 +148,41 @@ __device__ __forceinline__ void store_codes(unsigned char *row, int64_t col, int
         if (col + i < m) row[col + i] = (unsigned char)(c[i >> 2] >> (8 * (i & 3)));
 }
 
-template <int W> __device__ __forceinline__ unsigned most_of(unsigned x)      // of W neighbouring lanes
+// f of W neighbouring lanes (a power of two), in all of them: partners are the other one of a pair, the other pair, then mirrored
+// quads and halves of 16, which hold one value each by then, then the other 16 and 32 lanes.  f(a, b) is f(b, a), so all lanes end
+// with the same bits.
+template <int CONTROL> __device__ __forceinline__ unsigned moved(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CONTROL, 0xf, 0xf, true); }
+template <int W, class F> __device__ __forceinline__ unsigned over_lanes(unsigned x, F f)
 {
-#pragma unroll
-    for (int d = 1; d < W; d <<= 1) {
-        const unsigned o = (unsigned)__shfl_xor((int)x, d);
-        x = x > o ? x : o;
+    if constexpr (W >= 2) x = f(x, moved<0xb1>(x));       // quad_perm 1 0 3 2
+    if constexpr (W >= 4) x = f(x, moved<0x4e>(x));       // quad_perm 2 3 0 1
+    if constexpr (W >= 8) x = f(x, moved<0x141>(x));      // row_half_mirror
+    if constexpr (W >= 16) x = f(x, moved<0x140>(x));     // row_mirror
+    if constexpr (W >= 32) {
+        const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = f(y[0], y[1]);
+    }
+    if constexpr (W >= 64) {
+        const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = f(y[0], y[1]);
     }
     return x;
 }
+template <int W> __device__ __forceinline__ unsigned most_of(unsigned x)
+{
+    return over_lanes<W>(x, [](unsigned a, unsigned b) { return a > b ? a : b; });
+}
+template <int W> __device__ __forceinline__ unsigned least_of(unsigned x)
+{
+    return over_lanes<W>(x, [](unsigned a, unsigned b) { return a < b ? a : b; });
+}
+template <int W> __device__ __forceinline__ float most_of(float x)
+{
+    return __uint_as_float(over_lanes<W>(__float_as_uint(x), [](unsigned a, unsigned b) { return __float_as_uint(__builtin_fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
 template <int W> __device__ __forceinline__ float sum_of(float x)
 {
-#pragma unroll
-    for (int d = 1; d < W; d <<= 1) x += __shfl_xor(x, d);
-    return x;
+    return __uint_as_float(over_lanes<W>(__float_as_uint(x), [](unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
 // Sum over the W threads of a row, W / 64 waves of which leave theirs in `meet` (two turns of it, so that one barrier does).
