@@ -12,7 +12,7 @@ namespace {
 constexpr int kThreads = 1024;      // of a block of rows: a compute unit's worth, as choices follow each other and wait for lanes
 constexpr int kFew = 256;           // of what comes behind
 
-// Logits as integers in the order that rows choose by: larger first, then the lower group.  0: never chosen.
+// Logits as integers in the order that rows choose by.  0: never chosen.
 __device__ __forceinline__ unsigned order_of(float x)
 {
     const unsigned b = __float_as_uint(x);
@@ -20,6 +20,53 @@ __device__ __forceinline__ unsigned order_of(float x)
     if (x == 0.f) return 0x80000000u;                        // both zeros are equal
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+
+// The largest key of all that is left in a row, and the lowest group that has it; 0 if nothing is left.  A lane's own groups are
+// first, first + 1, ...  Keys of 16 bits take their group along in the lower half, the lower group above the higher: one maximum
+// over the lanes finds both.
+template <class T, int W, int C> struct Keys {
+    static constexpr bool kBoth = sizeof(T) == 2;
+    unsigned key[C];
+
+    __device__ __forceinline__ void open(const float (&x)[C], int first)
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            key[c] = order_of(x[c]);
+            if (kBoth && key[c]) {
+                unsigned top = key[c];      // of bf16 the upper half is all there is; of a half its own bits are taken the same way
+                if (std::is_same<T, f16_t>::value) {
+                    const unsigned h = (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[c]) << 16;
+                    top = top == 0x80000000u ? top : (h & 0x80000000u ? ~h : h | 0x80000000u);
+                }
+                key[c] = (top & 0xffff0000u) | (unsigned)(0xffff - first - c);
+            }
+        }
+    }
+    __device__ __forceinline__ unsigned most(int first, int &group) const
+    {
+        unsigned best = key[0];
+#pragma unroll
+        for (int c = 1; c < C; ++c) best = key[c] > best ? key[c] : best;
+        best = most_of<W>(best);
+        if (kBoth) {
+            group = 0xffff - (int)(best & 0xffff);
+        } else {
+            unsigned at = ~0u;
+#pragma unroll
+            for (int c = C - 1; c >= 0; --c) at = key[c] == best ? (unsigned)(first + c) : at;
+            group = (int)least_of<W>(at);
+        }
+        return best;
+    }
+    // Whether a lane's group c is the one that was found; it is taken out.
+    __device__ __forceinline__ bool take(int c, unsigned best, int group, int first)
+    {
+        const bool is = kBoth ? key[c] == best : first + c == group;
+        key[c] = is ? 0 : key[c];
+        return is;
+    }
+};
 
 // One row's logits, G of them, C neighbouring ones to each of W lanes.
 template <class T, int W, int C> struct Logits {
@@ -76,9 +123,8 @@ __device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned lo
         if (base + r * ROWS >= a.rows) break;
         Logits<T, W, C> l;
         l.load((const T *)a.logits + row * a.ldl, a.groups, is);
-        unsigned key[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) key[c] = order_of(l.x[c]);
+        Keys<T, W, C> keys;
+        keys.open(l.x, l.first);
         const float one = 1.f / l.exponents();
         int mine = 0;
         float total = 0.f;
@@ -88,21 +134,13 @@ __device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned lo
 #pragma unroll
         for (int n = 0; n < N; ++n) gate[n] = 0.f, choice[n] = -1;
         for (int j = 0; j < a.k; ++j) {
-            // the largest key of all that is left, and the lowest group that has it
-            unsigned best = key[0], at = ~0u;
-#pragma unroll
-            for (int c = 1; c < C; ++c) best = key[c] > best ? key[c] : best;
-            best = most_of<W>(best);
+            int group;
+            const unsigned best = keys.most(l.first, group);
             if (best == 0) break;
-#pragma unroll
-            for (int c = C - 1; c >= 0; --c) at = key[c] == best ? (unsigned)(l.first + c) : at;
-            const int group = (int)least_of<W>(at);
             float e = 0.f;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                e = l.first + c == group ? l.x[c] : e;
-                key[c] = l.first + c == group ? 0 : key[c];
-            }
+            for (int c = 0; c < C; ++c)
+                if (keys.take(c, best, group, l.first)) e = l.x[c];
             const float p = __shfl(e, group / C, W) * one;
             total += p;
             ++mine;

@@ -239,6 +239,7 @@ int norm_parts(int64_t rows, int64_t m)
     by_width(m, [&](auto w, auto) {
         constexpr int W = w.value, threads = W < 256 ? 256 : W, each = threads / W;
         parts = (int)std::min<int64_t>(std::max<int64_t>((rows + each - 1) / each, 1), kNormThreads / threads);
+        if (rows <= 4 * each) parts = 1;
     });
     return parts;
 }
