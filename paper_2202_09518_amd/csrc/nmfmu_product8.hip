@@ -181,11 +181,16 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
     // a row of them runs, the next row's operand is read.  Before the last row all reads of the stage are done and the next stage has
     // arrived: the columns' operands of that are read as the last products of this one let go of them, and the stage's buffer is
     // loaded again, a load or a read between every two products.
+    // Power bounds it: 8192 x 4096 x 4096 takes 131 us (2100 TFLOP/s) on random codes and 111 on zeros; without the reads of LDS it would
+    // take 93, without loads 107, without the sums in floats 109, and another order of the same work takes the same: a second meeting in
+    // the stage, so that every load has half a stage more to arrive, and the columns read over twice the slots, 131.  A second copy of
+    // the loop for tiles of few rows costs registers: 7 % of all tiles.
     static constexpr bool kAhead = DMA && !EXACT && STAGES == 2 && TM * TN >= 32;
     static __device__ __forceinline__ void ahead(LoadP &lp, LoadQ &lq, Rows &ls, const ReadP &rp, const ReadQ &rq, int at, int64_t b0, int64_t b1, int64_t k1,
-                                                 int64_t rows, const Scales &scales, char *lds, Acc &acc)
+                                                 const Scales &scales, char *lds, Acc &acc)
     {
-        constexpr int L = LoadP::kJobs + LoadQ::kJobs + 1, D = 2;      // loads of a stage; slots from a product to its sum
+        constexpr int L = LoadP::kJobs + LoadQ::kJobs + 1, D = 2, N = TM * TN;      // loads of a stage; slots from a product to its sum; slots
+        static_assert(TM % 2 == 0 && TN % 4 == 0 && L > TN && L <= N, "turns of registers end with the stage, loads have their slots");
         const int steps = (int)(b1 - b0);
         auto load = [&](int n, int s) {
             char *stage = lds + (s & 1) * kStage;
@@ -195,74 +200,61 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
             else if (n < L - 1) lp.bring(n - LoadQ::kJobs, lp.base + k0, left, stage);
             else ls.fetch(b0 + s, b1, stage + Base::kLdsStage);
         };
+        // all of the first stage, and of the second what a last row loads
 #pragma unroll
-        for (int n = 0; n < L; ++n) load(n, 0);
-        auto run = [&](auto live) {
-            constexpr int LIVE = live.value;
-            static_assert(LIVE % 2 == 0 && TN % 4 == 0, "turns of registers end with the stage");
-            constexpr int E = (L + LIVE * TN - 1) / (LIVE * TN), FIRST = TN * E < L ? TN * E : L;      // loads of a slot, and of the last row's
+        for (int n = 0; n < L + TN; ++n) load(n % L, n / L);
+        wait_loads<TN>();
+        meet();
+        i32x8 q[TN], p[2];
+        f32x4 t[4];
+        float sa[2], scale[2] = {0.f, 0.f};
 #pragma unroll
-            for (int n = 0; n < FIRST; ++n) load(n, 1);
-            wait_loads<FIRST>();
-            meet();
-            i32x8 q[TN], p[2];
-            f32x4 t[4];
-            float sa[2], scale[2] = {0.f, 0.f};
+        for (int n = 0; n < 4; ++n) t[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto read_q = [&](int j, const char *stage) { q[j] = both(rq.read(stage + kLdsP, j, 0), rq.read(stage + kLdsP, j, 1)); };
+        auto read_p = [&](int i, const char *stage) {
+            p[i & 1] = both(rp.read(stage, i, 0), rp.read(stage, i, 1));
+            sa[i & 1] = *reinterpret_cast<const float *>(stage + Base::kLdsStage + at + i * (64 * WM));
+        };
+        auto join = [&](auto slot) {                 // of the product in this slot
+            constexpr int n = (slot.value + N) % N, i = n / TN, j = n % TN;
+            acc[i][j] = fma4(t[n & 3], scale[i & 1], acc[i][j]);
+        };
 #pragma unroll
-            for (int n = 0; n < 4; ++n) t[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-            auto read_q = [&](int j, const char *stage) { q[j] = both(rq.read(stage + kLdsP, j, 0), rq.read(stage + kLdsP, j, 1)); };
-            auto read_p = [&](int i, const char *stage) {
-                p[i & 1] = both(rp.read(stage, i, 0), rp.read(stage, i, 1));
-                sa[i & 1] = *reinterpret_cast<const float *>(stage + Base::kLdsStage + at + i * (64 * WM));
-            };
-            auto join = [&](auto slot) {             // of the product in this slot
-                constexpr int n = (slot.value + LIVE * TN) % (LIVE * TN), i = n / TN, j = n % TN;
-                acc[i][j] = fma4(t[n & 3], scale[i & 1], acc[i][j]);
-            };
-#pragma unroll
-            for (int j = 0; j < TN; ++j) read_q(j, lds);
-            read_p(0, lds);
-            // (without branches in a stage: the compiler would move the sums behind them)
-            for (int s = 0, till = 0; till < steps;) {
-              till = till + 64 < steps ? till + 64 : steps;
-              const float columns = columns_scales(scales, b0 + s, till - s);
-              const int first = s;
-              for (; s < till; ++s) {
+        for (int j = 0; j < TN; ++j) read_q(j, lds);
+        read_p(0, lds);
+        // (without branches in a stage: the compiler would move the sums behind them)
+        for (int s = 0, till = 0; till < steps;) {
+            till = till + 64 < steps ? till + 64 : steps;
+            const float columns = columns_scales(scales, b0 + s, till - s);
+            const int first = s;
+            for (; s < till; ++s) {
                 const char *now = lds + (s & 1) * kStage, *next = lds + (~s & 1) * kStage;
                 const float sb = lane_of(columns, s - first);
-                each<LIVE>([&](auto row) {
-                    constexpr int i = row.value;
-                    constexpr bool last = i == LIVE - 1;
-                    if constexpr (last) {
+                each<N>([&](auto slot) {
+                    constexpr int n = slot.value, i = n / TN, j = n % TN;
+                    constexpr bool last = i == TM - 1;
+                    if constexpr (last && j == 0) {
                         wait_loads<0>();
                         meet();
                         __builtin_amdgcn_sched_barrier(0);
                     }
-                    each<TN>([&](auto col) {
-                        constexpr int j = col.value, n = i * TN + j;
-                        if constexpr (j == D - 1) scale[i & 1] = sa[i & 1] * sb;
-                        t[n & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q[j], p[i & 1], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-                        __builtin_amdgcn_sched_barrier(0);
-                        join(std::integral_constant<int, n - D>{});
-                        if constexpr (last) {
-                            read_q(j, next);
-                            if constexpr (j == TN - 1) read_p(0, next);
-                        } else if constexpr (j == 0) {
-                            read_p(i + 1, now);
-                        }
-                        constexpr int l = (last ? j : (i + 1) * TN + j) * E;
-                        each<E>([&](auto e) {
-                            if constexpr (l + e.value < L) load(l + e.value, last ? s + 2 : s + 1);
-                        });
-                        __builtin_amdgcn_sched_barrier(0);
-                    });
+                    if constexpr (j == D - 1) scale[i & 1] = sa[i & 1] * sb;      // (the row before has joined but for this slot's)
+                    t[n & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q[j], p[i & 1], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    join(std::integral_constant<int, n - D>{});
+                    if constexpr (last) {
+                        read_q(j, next);
+                        if constexpr (j == TN - 1) read_p(0, next);
+                    } else if constexpr (j == 0) {
+                        read_p(i + 1, now);
+                    }
+                    constexpr int l = last ? j : n + TN;
+                    if constexpr (l < L) load(l, last ? s + 2 : s + 1);
+                    __builtin_amdgcn_sched_barrier(0);
                 });
-              }
             }
-            each<D>([&](auto d) { join(std::integral_constant<int, d.value - D>{}); });
-        };
-        // the waves' rows lie in turn: of a tile with fewer rows each one leaves out as many
-        run(std::integral_constant<int, TM>{});
+        }
+        each<D>([&](auto d) { join(std::integral_constant<int, d.value - D>{}); });
         wait_loads<0>();
         meet();
     }
@@ -318,7 +310,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
             ls.fetch(block, b1, stage + Base::kLdsStage);
         };
         if constexpr (kAhead) {
-            ahead(lp, lq, ls, rp, rq, at, b0, b1, k1, P.count, scales, lds, acc);
+            ahead(lp, lq, ls, rp, rq, at, b0, b1, k1, scales, lds, acc);
             return;
         }
         if (DMA) {
