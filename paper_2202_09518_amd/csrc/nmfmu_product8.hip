@@ -181,10 +181,10 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
     // a row of them runs, the next row's operand is read.  Before the last row all reads of the stage are done and the next stage has
     // arrived: the columns' operands of that are read as the last products of this one let go of them, and the stage's buffer is
     // loaded again, a load or a read between every two products.
-    // Power bounds it: 8192 x 4096 x 4096 takes 131 us (2100 TFLOP/s) on random codes and 111 on zeros; without the reads of LDS it would
-    // take 93, without loads 107, without the sums in floats 109, and another order of the same work takes the same: a second meeting in
-    // the stage, so that every load has half a stage more to arrive, and the columns read over twice the slots, 131.  A second copy of
-    // the loop for tiles of few rows costs registers: 7 % of all tiles.
+    // Power bounds it: 8192 x 4096 x 4096 takes 123 to 131 us (2100 to 2230 TFLOP/s) on random codes and 100 to 111 on zeros, where its
+    // loads bound it (without them 85; 12 TB/s from L2).  Random codes without the sums in floats take 109; another order of the same
+    // work takes the same: a second meeting in the stage, so that every load has half a stage more to arrive, and the columns read over
+    // twice the slots, 131.  A second copy of the loop for tiles of few rows costs registers: 7 % of all tiles.
     static constexpr bool kAhead = DMA && !EXACT && STAGES == 2 && TM * TN >= 32;
     static __device__ __forceinline__ void ahead(LoadP &lp, LoadQ &lq, Rows &ls, const ReadP &rp, const ReadQ &rq, int at, int64_t b0, int64_t b1, int64_t k1,
                                                  const Scales &scales, char *lds, Acc &acc)
@@ -350,6 +350,9 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
     }
 };
 
+// Y, or parts of it over the contraction.  Few rows are bound by reading the groups' matrices: 512 rows over 64 groups of 4096 x 2048
+// 85 to 88 us (6.1 to 6.3 TB/s); many by power (above); 1237 rows of 515 x 389 in 9 groups, float results, by the latency of five stages
+// through registers, 10.7.
 template <class C, class O> __global__ __launch_bounds__(C::THREADS) void product8_kernel(Product8 a)
 {
     __shared__ __align__(1024) char lds[C::kLds];

