@@ -108,18 +108,17 @@ template <class T, int W, int C> struct Logits {
     }
 };
 
-// Choices of up to kRouteRows rows from `base` on: choice and gate to memory, choice to `picked` too, which rows chose a group to
+// Choices of up to `each` rows from `base` on: choice and gate to memory, choice to `picked` too, which rows chose a group to
 // `mask` (a bit for each row, zeroed before), c_r p_rg summed over the thread's rows to share[].
 template <class T, int W, int C>
-__device__ __forceinline__ void choose(const Route &a, int64_t base, unsigned long long *mask, int *picked, float (&share)[C])
+__device__ __forceinline__ void choose(const Route &a, int64_t base, int each, unsigned long long *mask, int *picked, float (&share)[C])
 {
     constexpr int ROWS = kThreads / W;
     const int lane = threadIdx.x % W;
-#pragma unroll
-    for (int r = 0; r < (kRouteRows + ROWS - 1) / ROWS; ++r) {
+    for (int r = 0; r * ROWS < each; ++r) {
         const int in = r * ROWS + threadIdx.x / W;
         const int64_t row = base + in;
-        const bool is = row < a.rows && in < kRouteRows;
+        const bool is = row < a.rows && in < each;
         if (base + r * ROWS >= a.rows) break;
         Logits<T, W, C> l;
         l.load((const T *)a.logits + row * a.ldl, a.groups, is);
@@ -252,7 +251,7 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
         float share[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) share[c] = 0.f;
-        choose<T, W, C>(a, base, mask, picked, share);
+        choose<T, W, C>(a, base, kRouteRows, mask, picked, share);
         add_share<W, C>(share, a.groups, lds, part);
         if (several) {
             const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
@@ -284,7 +283,7 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
 
 // (16384 rows to 8 of 128 groups, bf16: 9.0 us for the choices, 4.0 for the sums of the blocks, 3.4 for the places; instructions
 // bound the choices, 50 of them for each, and launches the rest.  24 rows of 64 floats to 4 groups, by one workgroup: 5.8 us.)
-// Blocks of kRouteRows rows: choices, gates, places within the block's part of a group, counts and shares of the block.
+// Blocks of a.each rows: choices, gates, places within the block's part of a group, counts and shares of the block.
 template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void route_rows_kernel(Route a)
 {
     __shared__ unsigned long long mask[W * C];
@@ -292,13 +291,13 @@ template <class T, int W, int C> __global__ __launch_bounds__(kThreads) void rou
     __shared__ int picked[kRouteRows * NMF_ROUTE_MAX_K];
     for (int g = threadIdx.x; g < a.groups; g += kThreads) mask[g] = 0;
     __syncthreads();
-    const int64_t base = (int64_t)blockIdx.x * kRouteRows;
+    const int64_t base = (int64_t)blockIdx.x * a.each;
     float share[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) share[c] = 0.f;
-    choose<T, W, C>(a, base, mask, picked, share);
+    choose<T, W, C>(a, base, a.each, mask, picked, share);
     add_share<W, C>(share, a.groups, lds, a.share + (int64_t)blockIdx.x * a.groups);
-    const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
+    const int here = (int)std::min<int64_t>(a.each, a.rows - base) * a.k;
     for (int i = threadIdx.x; i < here; i += kThreads) {
         const int g = picked[i];
         a.place[base * a.k + i] = g < 0 ? -1 : place_in(mask, g, i / a.k);
@@ -343,7 +342,7 @@ __global__ __launch_bounds__(1024) void route_sums_kernel(Route a)
     }
 }
 
-// 512 rows to 4 of 64 groups: 11.0 us, 13.7 with the launch in between; 2048 rows, 32 blocks to add up: 17.0 and 13.9.
+// 512 rows to 4 of 64 groups, 8 blocks: 11.0 us, 13.7 with the launch in between; 1024 of 256, 32 blocks, 19.1 and 15.5.
 constexpr int kFewBlocks = 8;
 
 // Places among all rows.  SUMS: of few blocks, whose counts each workgroup adds up itself instead of a launch in between.
@@ -355,8 +354,8 @@ template <bool SUMS> __global__ __launch_bounds__(kFew) void route_place_kernel(
     __shared__ double masses[SUMS ? NMF_ROUTE_MAX_GROUPS : 1];
     __shared__ int earlier[SUMS ? NMF_ROUTE_MAX_GROUPS : 1];
     constexpr int E = kRouteRows * NMF_ROUTE_MAX_K / kFew;      // choices of a thread
-    const int64_t base = (int64_t)blockIdx.x * kRouteRows;
-    const int here = (int)std::min<int64_t>(kRouteRows, a.rows - base) * a.k;
+    const int64_t base = (int64_t)blockIdx.x * a.each;
+    const int here = (int)std::min<int64_t>(a.each, a.rows - base) * a.k;
     int group[E], in[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -410,6 +409,19 @@ template <class F> void by_groups(int groups, F f)
     else if (groups <= 256) f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
     else if (groups <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
     else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+}
+
+// As many rows to a block as a workgroup takes at once, more where that leaves a block to each compute unit: 174 rows of 292 groups in
+// blocks of 16 rows 13.8 us, of 64 22; 4096 of 512 17.6 and 32.
+int route_each(int64_t rows, int groups)
+{
+    int each = kRouteRows;
+    by_groups(groups, [&](auto w, auto) {
+        const int at_once = std::min(kRouteRows, kThreads / w.value);
+        const int64_t turns = std::min<int64_t>((rows + 256 * at_once - 1) / (256 * at_once), kRouteRows / at_once);
+        each = at_once * (int)std::max<int64_t>(turns, 1);
+    });
+    return each;
 }
 
 template <class T> hipError_t launch_route(const Route &a, hipStream_t st)

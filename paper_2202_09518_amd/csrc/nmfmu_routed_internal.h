@@ -88,13 +88,15 @@ struct Route {
     int32_t *place;
     float *balance;
     // plan: null for one workgroup
-    int64_t blocks;                         // of kRouteRows rows
+    int each;                               // rows of a block, at most kRouteRows
+    int64_t blocks;
     int32_t *count;                         // blocks x groups: choices of each group in a block, then those in the blocks before
     float *share;                           // blocks x groups: sums of c_r p_rg
     int64_t *total;                         // groups
     double *mass;                           // groups
 };
 constexpr int kRouteRows = 64;
+int route_each(int64_t rows, int groups);      // rows of a block
 template <class T> hipError_t launch_route(const Route &a, hipStream_t st);
 
 struct RouteGradient {

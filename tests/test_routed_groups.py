@@ -416,3 +416,19 @@ def test_product8_copies_rows_that_are_not_whole(what, transposed):
                                  work=None if work is None else torch.full((work,), 255, dtype=torch.uint8, device="cuda"))
         holds(Y, want, size, m, "bf16", inside)
         assert bool((Y[~inside] == 77).all())
+
+
+@gpu
+@pytest.mark.parametrize("rows,groups,k", [(16, 1024, 16), (17, 1024, 16), (32, 200, 5), (33, 200, 5), (64, 64, 8), (9000, 700, 4), (17000, 40, 2), (9000, 257, 1)])
+def test_route_in_blocks_of_any_size(rows, groups, k):
+    """Rows at the ends of what one workgroup takes, and so many that blocks have several turns."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    l = (2 * normal(g, rows, groups)).to(torch.bfloat16)
+    l[rows // 3:rows // 2] = -math.inf
+    got = [t.cpu() for t in route(l, k, True)]
+    want = by_definition(l, k, True)
+    for i in (0, 2, 3):
+        assert torch.equal(got[i].long(), want[i]), i
+    lost = (groups + 300) * U
+    assert bool(((got[1].double() - want[1]).abs() <= (2 * lost + k * U) * want[1] + 2.0 ** -126).all())
+    assert abs(float(got[4]) - float(want[4])) <= (lost + (rows + groups) * U) * float(want[4])

@@ -247,6 +247,44 @@ def test_round_blocks_at_the_ends_of_the_range(block):
     assert torch.equal(bad, want) and not bool(C.view(torch.uint8)[bad].any())
 
 
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_codes_are_the_nearest_ones(typ):
+    """Against x 448 / largest in 64 bits, to the code: quotients on borders between two codes (64 bits show them as such: they have few
+    bits), and floats a few last places beside them (there 64 bits have 29 bits more than the floats)."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    rows, m, dt = 4096, 256, TYPES[typ]
+    X = normal(g, rows, m).to(dt).float()
+    most = torch.exp2(torch.randint(-6, 7, (rows, 1), generator=g, device="cuda").float()) * (1 + torch.rand(rows, 1, generator=g, device="cuda"))
+    most[::4] = 1.75 * torch.exp2(torch.randint(-6, 7, (rows // 4, 1), generator=g, device="cuda").float())      # all entries' quotients have few bits
+    most = most.to(dt).float()
+    fraction, exponent = torch.randint(8, 16, (rows, m), generator=g, device="cuda"), torch.randint(-10, 6, (rows, m), generator=g, device="cuda")
+    border = (fraction + 0.5).double() * torch.exp2(exponent.double() - 1)
+    near_it = (border * most.double() / 448).to(dt).float()
+    step = torch.randint(-3, 4, (rows, m), generator=g, device="cuda")
+    if typ == "f32":
+        near_it = (near_it.view(torch.int32) + step.int()).view(torch.float32)
+    X[1::2] = torch.where(near_it.abs() <= most, near_it, most.expand(rows, m))[1::2]
+    X[::2] = (X / X.abs().amax(1, keepdim=True) * most)[::2]
+    X = X.to(dt)
+    X[:, 0], X[:, 128] = most[:, 0].to(dt), -most[:, 0].to(dt)
+    assert bool((X.float().abs() <= most).all())
+    C, S = torch.empty(rows, m, dtype=E8, device="cuda"), torch.empty(rows, 2, device="cuda")
+    nmf.nmf_round_blocks(X, rows, m, 1, C, S)
+    q = X.double() * 448 / most.double()
+    unit = torch.exp2((torch.frexp(q).exponent - 4).clamp_min(-9).double())
+    want = torch.round(q / unit) * unit                      # ties to the even multiple
+    bad = C.float().double() != want
+    assert not bool(bad.any()), (int(bad.sum()), X[bad][:4], q[bad][:4], C.float()[bad][:4])
+    # the largest entry of a block of 128 x 128 alone
+    C2, S2 = torch.empty(rows, m, dtype=E8, device="cuda"), torch.empty(rows // 128, 2, device="cuda")
+    nmf.nmf_round_blocks(X, rows, m, 128, C2, S2)
+    tile = X.double().abs().view(rows // 128, 128, 2, 128).amax(dim=(1, 3))
+    q = X.double() * 448 / tile.repeat_interleave(128, 0).repeat_interleave(128, 1)
+    unit = torch.exp2((torch.frexp(q).exponent - 4).clamp_min(-9).double())
+    assert bool((C2.float().double() == torch.round(q / unit) * unit).all())
+
+
 # ---- rows to their places and back -----------------------------------------------------------
 
 def places(g, rows, k, sorted_rows, share):
