@@ -75,7 +75,9 @@ int nmf_round_blocks(int32_t type, const void *X, int64_t ldx, int64_t stride, i
  *   X8, xscale  rows x m and its scales, ldxs from row to row
  *   B8, bscale  group g at B8 + g * stride_b and bscale + g * stride_bs: m x n, or n x m if `transposed`; stride 0: one for all
  *   Y           rows x n of `type`;  rows outside all groups are not written
- * The gradient dX_g = dY_g B_g^T of rounded dY is the same call with B in its other form.
+ * The gradient dX_g = dY_g B_g^T of rounded dY is the same call with B in its other form; that of B is nmf_grouped_gradient of the
+ * rows before they were rounded.  Rows of codes that begin and end on 16-byte borders are fastest (others are copied, or slower).
+ * Results in 16 bits: of eight neighbouring products of codes what is below 2^-13 of the largest one is left out.
  */
 int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float *xscale, int64_t ldxs, const int64_t *offsets,
                          int32_t groups, int64_t rows, const void *B8, int64_t ldb, int64_t stride_b, const float *bscale, int64_t ldbs,

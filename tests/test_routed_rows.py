@@ -358,6 +358,26 @@ def test_spread_and_collect(rows, k, m, typ):
 
 
 @gpu
+def test_collect_gradient_against_differences():
+    """Of sum(dY Y) in one direction of X and one of the gates: Y is linear in each, so differences over any step are exact but for the
+    floats' own error, some 2^-22 of the terms."""
+    g = torch.Generator(device="cuda").manual_seed(19)
+    rows, k, m = 30, 3, 200
+    place = places(g, rows, k, rows * k, 0.8)
+    gate, X, dY, D, E = torch.rand(rows, k, generator=g, device="cuda"), normal(g, rows * k, m), normal(g, rows, m), normal(g, rows * k, m), normal(g, rows, k)
+    dX, dgate, Y = torch.zeros_like(X), torch.empty_like(gate), torch.empty_like(dY)
+
+    def loss(X, gate):
+        nmf.nmf_collect_rows(X, rows, k, place, gate, m, Y)
+        return float((dY.double() * Y.double()).sum())
+
+    nmf.nmf_collect_gradient(dY, rows, k, place, gate, m, dX, X=X, dgate=dgate)
+    size = rows * k * m * 2.0 ** -22 * 16
+    assert abs(loss(X + D, gate) - loss(X - D, gate) - 2 * float((dX.double() * D.double()).sum())) < size
+    assert abs(loss(X, gate + E) - loss(X, gate - E) - 2 * float((dgate.double() * E.double()).sum())) < size
+
+
+@gpu
 @pytest.mark.parametrize("m", [1, 16, 100, 128, 4097])
 def test_spread_of_codes_takes_the_scales_along(m):
     g = torch.Generator(device="cuda").manual_seed(m)
