@@ -108,11 +108,44 @@ template <int BM, int WAVES, bool DMA> struct RowScales {
     }
 };
 
+// Brings stages of an operand by columns, on any border, through registers.  Where a stage is whole and nothing is read behind the
+// array's end, its chunks are loaded as they lie: what they hold of columns that are not there is in no result that is written.  Else
+// (the last stage) with a look at every chunk, and zeros behind the contraction's end.  us, with a look at every chunk throughout and
+// without: 900 rows in 8 groups of 3001 x 2999 67 and 45, 20 rows of 2047 x 2049 21 and 17, 3000 rows in 5 groups of 1001 x 999, float
+// results, 33 and 28.  (Operands by rows are slower so, 540 and 590 to 630 for 2245 rows in 22 groups of 6196 x 5568, transposed: a
+// row's chunks lie across two lines of memory each, and come twice.)
+template <int R, int THREADS> struct ColumnLoader : Loader<e8_t, R, true, THREADS, false, 1> {
+    using Base = Loader<e8_t, R, true, THREADS, false, 1>;
+    using Base::kJobs;
+    unsigned from[kJobs];      // of a chunk, from the stage's first k on
+
+    __device__ __forceinline__ void open(const Operand &o)
+    {
+        Base::open(o);
+#pragma unroll
+        for (int j = 0; j < kJobs; ++j) this->reg[j] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kJobs; ++j)
+            from[j] = this->chunk(j) * 16 < this->count ? (unsigned)(this->line + j * Base::kRowStep) * (unsigned)o.ld + this->chunk(j) * 16 : kOutside;
+    }
+    __device__ __forceinline__ void fetch(int64_t k0, int64_t K, char *)
+    {
+        if (this->ld < (1 << 22) && K - k0 >= 128 && (k0 + 127) * this->ld + (this->count + 15) / 16 * 16 <= this->bytes) {
+            const char *at = this->base + k0 * this->ld;
+#pragma unroll
+            for (int j = 0; j < kJobs; ++j)
+                if (from[j] != kOutside) __builtin_memcpy(&this->reg[j], at + from[j], 16);
+        } else {
+            Base::fetch(k0, K, nullptr);
+        }
+    }
+};
+
 template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool EXACT> struct Tile8 : Tile<e8_t, BM, BN, WM, WN, STAGES_, false, QRC, DMA> {
     using Base = Tile<e8_t, BM, BN, WM, WN, STAGES_, false, QRC, DMA>;
     using typename Base::Acc;
     using typename Base::LoadP;
-    using typename Base::LoadQ;
+    using LoadQ = std::conditional_t<!DMA && QRC, ColumnLoader<BN, Base::THREADS>, typename Base::LoadQ>;
     using typename Base::ReadP;
     using typename Base::ReadQ;
     using Base::kLdsP;
@@ -313,7 +346,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
             ahead(lp, lq, ls, rp, rq, at, b0, b1, k1, scales, lds, acc);
             return;
         }
-        if (DMA) {
+        if constexpr (DMA) {
             constexpr int L = LoadP::kJobs + LoadQ::kJobs + 1;
 #pragma unroll
             for (int s = 0; s < STAGES - 1; ++s) fetch(s, s);

@@ -432,3 +432,27 @@ def test_route_in_blocks_of_any_size(rows, groups, k):
     lost = (groups + 300) * U
     assert bool(((got[1].double() - want[1]).abs() <= (2 * lost + k * U) * want[1] + 2.0 ** -126).all())
     assert abs(float(got[4]) - float(want[4])) <= (lost + (rows + groups) * U) * float(want[4])
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 5, 17, 63, 65, 129, 200])
+@pytest.mark.parametrize("m", [127, 128, 129, 256, 300])
+def test_product8_reads_nothing_behind_its_arrays(m, n):
+    """Odd widths whose last rows end where the memory that may be read ends: codes behind it are NaN, and would show."""
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+    for rows, typ in ((3, "bf16"), (90, "f32")):
+        x, b = codes(g, 1, rows, m)[0], codes(g, 2, m, n)
+        xs, bs = torch.rand(rows, -(-m // 128), generator=g, device="cuda"), torch.rand(2, -(-m // 128), -(-n // 128), generator=g, device="cuda") / 100
+        cut = torch.tensor([0, rows // 2, rows])
+        memx, memb = (torch.full((t.numel() + 4096,), 127, dtype=torch.uint8, device="cuda") for t in (x, b))
+        X, B = memx[:x.numel()].view(rows, m), memb[:b.numel()].view(2, m, n)
+        X.copy_(x.view(torch.uint8))
+        B.copy_(b.view(torch.uint8))
+        Y = torch.empty(rows, n, dtype=TYPES[typ], device="cuda")
+        nmf.nmf_grouped_product8(X, xs, cut.cuda(), 2, rows, B, bs, False, m, n, Y)
+        want, size = product(x, xs, b, bs, cut, False)
+        holds(Y, want, size, m, typ, torch.ones(rows, dtype=torch.bool, device="cuda"))
+        Bt = memb[:b.numel()].view(2, n, m)
+        Bt.copy_(b.view(torch.uint8).transpose(1, 2))
+        nmf.nmf_grouped_product8(X, xs, cut.cuda(), 2, rows, Bt, bs.transpose(1, 2).contiguous(), True, m, n, Y)
+        holds(Y, want, size, m, typ, torch.ones(rows, dtype=torch.bool, device="cuda"))
