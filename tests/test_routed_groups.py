@@ -456,3 +456,21 @@ def test_product8_reads_nothing_behind_its_arrays(m, n):
         Bt.copy_(b.view(torch.uint8).transpose(1, 2))
         nmf.nmf_grouped_product8(X, xs, cut.cuda(), 2, rows, Bt, bs.transpose(1, 2).contiguous(), True, m, n, Y)
         holds(Y, want, size, m, typ, torch.ones(rows, dtype=torch.bool, device="cuda"))
+
+
+@gpu
+@pytest.mark.parametrize("transposed", [False, True])
+def test_product8_of_long_contractions_in_large_tiles(transposed):
+    """More than 64 blocks, whose scales come 64 at a time, the last one in part."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    rows, m, n = 2100, 8336, 4112
+    M, N = -(-m // 128), -(-n // 128)
+    x, b = codes(g, 1, rows, m)[0], codes(g, 1, *((n, m) if transposed else (m, n)))
+    xs = torch.exp(normal(g, rows, M)) / 1000
+    bs = torch.exp(normal(g, 1, *((N, M) if transposed else (M, N)))) / 60
+    cut = torch.tensor([0, rows])
+    want, size = product(x, xs, b, bs, cut, transposed)
+    for typ in ("bf16", "f32"):
+        Y = torch.empty(rows, n, dtype=TYPES[typ], device="cuda")
+        nmf.nmf_grouped_product8(x, xs, cut.cuda(), 1, rows, b, bs, transposed, m, n, Y)
+        holds(Y, want, size, m, typ, torch.ones(rows, dtype=torch.bool, device="cuda"))
