@@ -48,6 +48,15 @@ int nmfmu_dense_plan(const float *A, int64_t m, int64_t n, int32_t k, float *W, 
                      int32_t *plan, void *stream);
 
 /*
+ * What nmf_grouped_product8 (nmfmu_routed.h) would do with these arguments, by them alone (no pointer is followed, nothing is
+ * launched), in route[0..6] (host): [0] 1 if the codes go straight to LDS, 0 through registers; [1] bytes of the copies that it makes
+ * in its scratch; [2], [3] leading dimensions of X8 and B8 as the tiles read them; [4], [5] rows and columns of a tile; [6] bytes of the
+ * parts of its contraction.
+ */
+int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs, int32_t groups, int64_t rows, const void *B8, int64_t ldb,
+                         int64_t stride_b, int32_t transposed, int64_t m, int64_t n, size_t work_bytes, int64_t *route);
+
+/*
  * nmf_mu_dense with timing, on A as it is (no copy of a misaligned A is made, so such
  * an A takes the slower kernels here): the same launches on `stream`, with a HIP event
  * recorded between them; synchronises `stream` before returning.  On return

@@ -1,6 +1,7 @@
 // C ABI of the norm, routing, the rows' way to their groups and products in 8 bits: argument checks and plans.
 // Public contract: include/nmfmu_routed.h.
 #include "nmfmu_routed.h"
+#include "nmfmu_test.h"
 #include "nmfmu_internal.h"
 #include "nmfmu_routed_internal.h"
 
@@ -96,15 +97,34 @@ size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (
 // Codes whose rows do not begin and end on 16-byte borders pass registers on their way to LDS, which takes 2 to 3.5 times as long;
 // where the product is long enough they are copied once per call into rows that do, if the scratch has room.
 // (us: 6000 x 4095 x 2047 in 4 groups 239, transposed 141, through registers, 94 and 89 with copies)
+constexpr int64_t kFar = 1 << 22;      // straight to LDS, distances inside a tile go into 32 bits: 256 rows below this, copied ones too
+int64_t whole(int64_t cols) { return ceil_div(cols, 16) * 16; }
 struct Codes {
     const void *p;
     int64_t ld, stride, rows, cols, count;
-    // (distances of a tile's rows go into 32 bits)
-    bool bad() const { return !aligned(p, 16) || (ld | (count > 1 ? stride : 0) | cols) % 16 != 0 || ld >= (1 << 22); }
-    int64_t whole() const { return ceil_div(cols, 16) * 16; }
-    size_t bytes() const { return (size_t)count * rows * whole(); }
+    bool bad() const { return !aligned(p, 16) || (ld | (count > 1 ? stride : 0) | cols) % 16 != 0 || ld >= kFar; }
+    bool can_copy() const { return whole(cols) < kFar; }
+    size_t bytes() const { return (size_t)count * rows * whole(cols); }
 };
 bool worth_copies(size_t bytes, double flops) { return 5e-6 + 2.0 * bytes / 4.5e12 < flops / 0.9e15; }
+
+// What a product does: its tiles, whether its codes go straight to LDS, and the bytes of copies that it makes for that.
+struct Route8 {
+    Plan tiles;
+    bool straight;
+    size_t copies;
+};
+Route8 route_of(int32_t type, const Codes &x, const Codes &b, int64_t ldxs, int64_t groups, int64_t m, int64_t n, size_t work_bytes)
+{
+    const bool near = ldxs < (1 << 20), can = (!x.bad() || x.can_copy()) && (!b.bad() || b.can_copy());
+    const size_t odd = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
+    Route8 r;
+    r.copies = odd && near && can && odd <= work_bytes && worth_copies(odd, 2.0 * x.rows * m * n) ? odd : 0;
+    r.straight = near && (odd == 0 || r.copies);
+    r.tiles = product_plan(x.rows, groups, m, n, r.straight && type != NMF_F32);
+    while (r.tiles.splits > 1 && product_part(x.rows, n, r.tiles.splits) > work_bytes - r.copies) --r.tiles.splits;
+    return r;
+}
 
 // A matrix of entries of e bytes: rows x cols, ld from row to row.
 int check_matrix(const void *p, int64_t ld, int64_t rows, int64_t cols, int e)
@@ -209,29 +229,25 @@ int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float 
     if (stride_b < 0 || stride_bs < 0) return bad("negative stride");
     if (rows == 0) return NMF_OK;
     Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, b_rows, b_cols, stride_b ? groups : 1};
-    const bool near = ldxs < (1 << 20);
-    const size_t odd = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
-    const bool copies = odd && near && odd <= work_bytes && worth_copies(odd, 2.0 * rows * m * n), dma = near && (odd == 0 || copies);
+    const Route8 route = route_of(type, x, b, ldxs, groups, m, n, work_bytes);
+    const Plan plan = route.tiles;
     char *scratch = static_cast<char *>(work);
-    if (copies) work_bytes -= odd;
-    Plan plan = product_plan(rows, groups, m, n, dma && type != NMF_F32);
-    while (plan.splits > 1 && product_part(rows, n, plan.splits) > work_bytes) --plan.splits;
     const int64_t grid = (ceil_div(rows, kTileRows[plan.shape]) + groups) * ceil_div(n, kTileCols[plan.shape]) * plan.splits;
     if (std::max(grid, plan.splits > 1 ? rows * ceil_div(n, 1024) : 0) > kMostWorkgroups) return set_error(NMF_EUNSUPPORTED, "more tiles than one launch can have");
-    if (copies)
+    if (route.copies)
         for (Codes *c : {&x, &b}) {
             if (!c->bad()) continue;
-            if ((rc = launched(launch_whole_rows(c->p, c->ld, c->stride, c->rows, c->cols, c->count, scratch, c->whole(), static_cast<hipStream_t>(stream))))) return rc;
+            if ((rc = launched(launch_whole_rows(c->p, c->ld, c->stride, c->rows, c->cols, c->count, scratch, whole(c->cols), static_cast<hipStream_t>(stream))))) return rc;
             c->p = scratch;
-            c->ld = c->whole();
-            c->stride = c->count > 1 ? c->whole() * c->rows : 0;
+            c->ld = whole(c->cols);
+            c->stride = c->count > 1 ? c->ld * c->rows : 0;
             scratch += c->bytes();
         }
     Product8 p = {};
     p.x = x.p; p.ldx = x.ld; p.xs = xscale; p.ldxs = ldxs; p.offsets = offsets; p.groups = groups; p.rows = rows; p.m = m; p.n = n;
     p.b = b.p; p.ldb = b.ld; p.stride_b = b.stride; p.bs = bscale; p.ldbs = ldbs; p.stride_bs = stride_bs; p.transposed = transposed != 0;
     p.type = type; p.y = Y; p.ldy = ldy;
-    p.dma = dma;
+    p.dma = route.straight;
     p.shape = plan.shape;
     p.splits = plan.splits;
     p.part = reinterpret_cast<float *>(scratch);
@@ -344,6 +360,21 @@ int nmf_collect_gradient(int32_t type, const void *dY, int64_t ldy, int64_t rows
     return launched(type, a, stream, launch_collect_gradient<float>, launch_collect_gradient<bf16_t>, launch_collect_gradient<f16_t>);
 }
 
+int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs, int32_t groups, int64_t rows, const void *B8, int64_t ldb,
+                         int64_t stride_b, int32_t transposed, int64_t m, int64_t n, size_t work_bytes, int64_t *route)
+{
+    const Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, transposed ? n : m, transposed ? m : n, stride_b ? groups : 1};
+    const Route8 r = route_of(type, x, b, ldxs, groups, m, n, work_bytes);
+    route[0] = r.straight;
+    route[1] = (int64_t)r.copies;
+    route[2] = r.copies && x.bad() ? whole(x.cols) : ldx;
+    route[3] = r.copies && b.bad() ? whole(b.cols) : ldb;
+    route[4] = kTileRows[r.tiles.shape];
+    route[5] = kTileCols[r.tiles.shape];
+    route[6] = r.tiles.splits > 1 ? (int64_t)product_part(rows, n, r.tiles.splits) : 0;
+    return NMF_OK;
+}
+
 size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts)
 {
     const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ONE_B);
@@ -354,8 +385,9 @@ size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32
     if (kind != 2 || !size_ok(n) || parts < 1) return 0;
     const int64_t count = odd & NMF_ONE_B ? 1 : parts;
     size_t copies = 0;
-    if (m % 16 || (odd & NMF_ODD_X)) copies += (size_t)rows * ceil_div(m, 16) * 16;
-    if (m % 16 || n % 16 || (odd & NMF_ODD_B)) copies += (size_t)count * std::max(m * ceil_div(n, 16), n * ceil_div(m, 16)) * 16;
+    if (m % 16 || (odd & NMF_ODD_X)) copies += (size_t)rows * whole(m);
+    if (m % 16 || n % 16 || (odd & NMF_ODD_B)) copies += (size_t)count * std::max(m * whole(n), n * whole(m));
+    if (whole(std::max(m, n)) >= kFar) copies = 0;
     if (!worth_copies(copies, 2.0 * rows * m * n)) copies = 0;
     return copies + std::max(product_part(rows, n, product_plan(rows, parts, m, n, true).splits), product_part(rows, n, product_plan(rows, parts, m, n, false).splits));
 }
