@@ -133,8 +133,10 @@ int nmf_collect_gradient(int32_t type, const void *dY, int64_t ldy, int64_t rows
 /*
  * Scratch of the fastest plan, in bytes (0: none needed, or invalid sizes).  kind: 0 nmf_route (m: groups), 1
  * nmf_rms_norm_gradient with dweight, 2 nmf_grouped_product8 (parts: groups; kind 2 alone takes n and parts, and, added to
- * it as in nmf_ragged_work_bytes, NMF_ODD_X, NMF_ODD_B and NMF_ONE_B).
+ * it as in nmf_ragged_work_bytes, NMF_ODD_X and NMF_ODD_B, also for leading dimensions of 2^22 and more, NMF_ONE_B, and how B lies:
+ * NMF_B_M_X_N, or NMF_B_N_X_M for `transposed`; with neither there is enough for both).
  */
+enum { NMF_B_M_X_N = 256, NMF_B_N_X_M = 512 };
 size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts);
 
 #ifdef __cplusplus

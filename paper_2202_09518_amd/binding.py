@@ -32,7 +32,8 @@ NMF_MU_MAX_K_SLICED = 1024
 NMF_LOWRANK_MAX_K = 256
 NMF_F32, NMF_BF16, NMF_F16, NMF_E4M3 = range(4)
 NMF_NORM_MAX_M, NMF_ROUTE_MAX_GROUPS, NMF_ROUTE_MAX_K = 32768, 1024, 16
-NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS, NMF_ONE_B = 16, 32, 64, 128
+NMF_ODD_X, NMF_ODD_B, NMF_ODD_FACTORS, NMF_ONE_B, NMF_B_M_X_N, NMF_B_N_X_M = 16, 32, 64, 128, 256, 512
+_FAR = 1 << 22                          # leading dimensions of codes from here on are odd ones too
 
 _lib = None
 
@@ -564,7 +565,11 @@ def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transpos
     b, ldb, stride_b = _stack_of(B8, _codes(B8, "B8"), d, groups, *((n, m) if transposed else (m, n)), "B8")
     bs, ldbs, stride_bs = _stack_of(bscale, torch.float32, d, groups, *((N, M) if transposed else (M, N)), "bscale")
     y, ldy = _rows_of(Y, Y.dtype, d, rows, n, "Y")
-    odd = (NMF_ODD_X if (x | ldx) & 15 else 0) | (NMF_ODD_B if (b | ldb | (stride_b if groups > 1 else 0)) & 15 else 0)
+    odd = NMF_B_N_X_M if transposed else NMF_B_M_X_N
+    if (x | ldx) & 15 or ldx >= _FAR:
+        odd |= NMF_ODD_X
+    if (b | ldb | (stride_b if groups > 1 else 0)) & 15 or ldb >= _FAR:
+        odd |= NMF_ODD_B
     if stride_b == 0:
         odd |= NMF_ONE_B
     w, nbytes, _keep = _scratch(_need_routed(2 | odd, rows, m, n, groups) if work is None else 0, work, d, stream)

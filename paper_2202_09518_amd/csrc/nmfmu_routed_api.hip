@@ -103,10 +103,18 @@ struct Codes {
     const void *p;
     int64_t ld, stride, rows, cols, count;
     bool bad() const { return !aligned(p, 16) || (ld | (count > 1 ? stride : 0) | cols) % 16 != 0 || ld >= kFar; }
-    bool can_copy() const { return whole(cols) < kFar; }
     size_t bytes() const { return (size_t)count * rows * whole(cols); }
 };
 bool worth_copies(size_t bytes, double flops) { return 5e-6 + 2.0 * bytes / 4.5e12 < flops / 0.9e15; }
+
+// Bytes of the copies of a product, of the operands that need them, with scratch enough; 0 if it makes none.
+size_t copies_of(int64_t rows, int64_t m, int64_t n, int64_t count, bool transposed, bool odd_x, bool odd_b)
+{
+    const int64_t wide_x = whole(m), wide_b = whole(transposed ? m : n);
+    if ((odd_x && wide_x >= kFar) || (odd_b && wide_b >= kFar)) return 0;
+    const __int128 bytes = (odd_x ? (__int128)rows * wide_x : 0) + (odd_b ? (__int128)count * (transposed ? n : m) * wide_b : 0);
+    return bytes < ((__int128)1 << 62) && worth_copies((size_t)bytes, 2.0 * rows * m * n) ? (size_t)bytes : 0;
+}
 
 // What a product does: its tiles, whether its codes go straight to LDS, and the bytes of copies that it makes for that.
 struct Route8 {
@@ -114,13 +122,13 @@ struct Route8 {
     bool straight;
     size_t copies;
 };
-Route8 route_of(int32_t type, const Codes &x, const Codes &b, int64_t ldxs, int64_t groups, int64_t m, int64_t n, size_t work_bytes)
+Route8 route_of(int32_t type, const Codes &x, const Codes &b, int64_t ldxs, int64_t groups, bool transposed, int64_t m, int64_t n, size_t work_bytes)
 {
-    const bool near = ldxs < (1 << 20), can = (!x.bad() || x.can_copy()) && (!b.bad() || b.can_copy());
-    const size_t odd = (x.bad() ? x.bytes() : 0) + (b.bad() ? b.bytes() : 0);
+    const bool near = ldxs < (1 << 20);
     Route8 r;
-    r.copies = odd && near && can && odd <= work_bytes && worth_copies(odd, 2.0 * x.rows * m * n) ? odd : 0;
-    r.straight = near && (odd == 0 || r.copies);
+    r.copies = near ? copies_of(x.rows, m, n, b.count, transposed, x.bad(), b.bad()) : 0;
+    if (r.copies > work_bytes) r.copies = 0;
+    r.straight = near && ((!x.bad() && !b.bad()) || r.copies);
     r.tiles = product_plan(x.rows, groups, m, n, r.straight && type != NMF_F32);
     while (r.tiles.splits > 1 && product_part(x.rows, n, r.tiles.splits) > work_bytes - r.copies) --r.tiles.splits;
     return r;
@@ -229,7 +237,7 @@ int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float 
     if (stride_b < 0 || stride_bs < 0) return bad("negative stride");
     if (rows == 0) return NMF_OK;
     Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, b_rows, b_cols, stride_b ? groups : 1};
-    const Route8 route = route_of(type, x, b, ldxs, groups, m, n, work_bytes);
+    const Route8 route = route_of(type, x, b, ldxs, groups, transposed != 0, m, n, work_bytes);
     const Plan plan = route.tiles;
     char *scratch = static_cast<char *>(work);
     const int64_t grid = (ceil_div(rows, kTileRows[plan.shape]) + groups) * ceil_div(n, kTileCols[plan.shape]) * plan.splits;
@@ -364,7 +372,7 @@ int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs
                          int64_t stride_b, int32_t transposed, int64_t m, int64_t n, size_t work_bytes, int64_t *route)
 {
     const Codes x = {X8, ldx, 0, rows, m, 1}, b = {B8, ldb, stride_b, transposed ? n : m, transposed ? m : n, stride_b ? groups : 1};
-    const Route8 r = route_of(type, x, b, ldxs, groups, m, n, work_bytes);
+    const Route8 r = route_of(type, x, b, ldxs, groups, transposed != 0, m, n, work_bytes);
     route[0] = r.straight;
     route[1] = (int64_t)r.copies;
     route[2] = r.copies && x.bad() ? whole(x.cols) : ldx;
@@ -377,19 +385,23 @@ int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs
 
 size_t nmf_routed_work_bytes(int kind, int64_t rows, int64_t m, int64_t n, int32_t parts)
 {
-    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ONE_B);
+    const int odd = kind & (NMF_ODD_X | NMF_ODD_B | NMF_ONE_B | NMF_B_M_X_N | NMF_B_N_X_M);
     kind &= ~odd;
     if (!size_ok(rows) || !size_ok(m)) return 0;
     if (kind == 0) return m <= NMF_ROUTE_MAX_GROUPS && !route_alone(rows, m) ? route_bytes(ceil_div(rows, route_each(rows, (int)m)), m) : 0;
     if (kind == 1) return m <= NMF_NORM_MAX_M ? norm_bytes(norm_parts(rows, m), m) : 0;
     if (kind != 2 || !size_ok(n) || parts < 1) return 0;
     const int64_t count = odd & NMF_ONE_B ? 1 : parts;
-    size_t copies = 0;
-    if (m % 16 || (odd & NMF_ODD_X)) copies += (size_t)rows * whole(m);
-    if (m % 16 || n % 16 || (odd & NMF_ODD_B)) copies += (size_t)count * std::max(m * whole(n), n * whole(m));
-    if (whole(std::max(m, n)) >= kFar) copies = 0;
-    if (!worth_copies(copies, 2.0 * rows * m * n)) copies = 0;
-    return copies + std::max(product_part(rows, n, product_plan(rows, parts, m, n, true).splits), product_part(rows, n, product_plan(rows, parts, m, n, false).splits));
+    size_t most = 0;
+    for (bool transposed : {false, true}) {
+        if ((odd & (NMF_B_M_X_N | NMF_B_N_X_M)) && !(odd & (transposed ? NMF_B_N_X_M : NMF_B_M_X_N))) continue;
+        const bool odd_x = m % 16 || (odd & NMF_ODD_X), odd_b = (transposed ? m : n) % 16 || (odd & NMF_ODD_B);
+        const size_t copies = copies_of(rows, m, n, count, transposed, odd_x, odd_b);
+        size_t joined = product_part(rows, n, product_plan(rows, parts, m, n, false).splits);
+        if (copies || !(odd_x || odd_b)) joined = std::max(joined, product_part(rows, n, product_plan(rows, parts, m, n, true).splits));
+        most = std::max(most, copies + joined);
+    }
+    return most;
 }
 
 }  // extern "C"

@@ -49,7 +49,8 @@ def test_codes_that_go_straight_to_lds_stay_near(odd, transposed, typ):
 
 @pytest.mark.parametrize("m,n,transposed", [(17000001, 450, True), (450, 17000001, False)])
 def test_no_copies_are_asked_for_of_rows_that_far(m, n, transposed):
-    for kind in (2, 2 | nmf.NMF_ONE_B):
+    layout = nmf.NMF_B_N_X_M if transposed else nmf.NMF_B_M_X_N
+    for kind in (2 | layout, 2 | layout | nmf.NMF_ONE_B):
         assert nmf.nmf_routed_work_bytes(kind, 450, m, n, 8) == route(nmf.NMF_BF16, 450, 8, m, n, transposed, bool(kind & nmf.NMF_ONE_B))[6]
 
 
