@@ -73,20 +73,24 @@ template <class T> struct Eight {
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 struct Scale {
-    float scale, most, up, back;      // scale is most / 448; up: 1 / scale, back: 512 / most
+    float scale, up;              // scale: the largest magnitude / 448; up: 1 / scale
+    float most, part, back;       // for exact_codes, where the magnitude is small 2^64 times it: the magnitude; 7 / 8 as many times; 512 / most
     bool finite;
 };
 __device__ __forceinline__ Scale scale_of(unsigned bits)
 {
     Scale s;
     s.finite = bits < 0x7f800000u;
-    s.most = __builtin_fmaxf(__uint_as_float(bits), 0x1.cp-118f);      // 448 2^-126
+    const float most = __builtin_fmaxf(__uint_as_float(bits), 0x1.cp-118f);      // 448 2^-126
     // most / 448 and its inverse, each with its error taken back once
     constexpr float part = 1.f / 448.f;
-    const float near = s.most * part, scale = __builtin_fmaf(__builtin_fmaf(-near, 448.f, s.most), part, near);
+    const float near = most * part, scale = __builtin_fmaf(__builtin_fmaf(-near, 448.f, most), part, near);
     const float inverse = __builtin_amdgcn_rcpf(scale);
     s.up = __builtin_fmaf(__builtin_fmaf(-scale, inverse, 1.f), inverse, inverse);
-    s.back = s.up * (8.f / 7.f);
+    const bool small = most < 0x1p-60f;
+    s.most = small ? most * 0x1p64f : most;
+    s.part = small ? 0.875f * 0x1p64f : 0.875f;
+    s.back = s.up * (8.f / 7.f) * (small ? 0x1p-64f : 1.f);
     s.scale = s.finite ? scale : __builtin_nanf("");
     return s;
 }
@@ -110,7 +114,7 @@ __device__ __forceinline__ ragged::u32x2 near_codes(const float (&x)[8], const S
     return codes_of(q, s);
 }
 // The same of entries as they are, to the nearest code: the quotient's error, from x 7 / 8 and most quotient / 512 so that nothing
-// overflows, is taken back.  Of 16-bit entries the quotient lies on a border between two codes or 2^-16 away from it.  Of floats it
+// overflows, is taken back.  In small blocks both are 2^64 times that, as errors of 2^-48 of an entry would lie below 2^-149.  Of 16-bit entries the quotient lies on a border between two codes or 2^-16 away from it.  Of floats it
 // can be nearer than its own last place, so there what is left of it sets that to odd, which no border has; it is looked at only
 // where some quotient of the wave is within four last places of where borders are, multiples of 2^19 of them.
 template <class T> __device__ __forceinline__ ragged::u32x2 exact_codes(const float (&x)[8], const Scale &s)
@@ -125,7 +129,7 @@ template <class T> __device__ __forceinline__ ragged::u32x2 exact_codes(const fl
     if (sizeof(T) == 2 || __any(near)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float part = x[i] * 0.875f, rest = sizeof(T) == 4 ? __builtin_fmaf(x[i], 0.875f, -part) : 0.f;
+            const float part = x[i] * s.part, rest = sizeof(T) == 4 ? __builtin_fmaf(x[i], s.part, -part) : 0.f;
             q[i] = __builtin_fmaf(__builtin_fmaf(q[i] * -0x1p-9f, s.most, part) + rest, s.back, q[i]);
             if (sizeof(T) == 4) {
                 const float left = __builtin_fmaf(q[i] * -0x1p-9f, s.most, part) + rest;
