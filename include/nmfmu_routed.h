@@ -14,8 +14,9 @@
  *   - Codes are e4m3 (one sign, four exponent, three fraction bits; largest 448, no infinities), one byte each.  A block of
  *     codes stands for code * scale.  Rows have a scale for each 128 columns: float, rows x ceil(m / 128).  Matrices have one
  *     for each 128 x 128: ceil(m / 128) x ceil(n / 128) for an m x n matrix, in the layout that the matrix has.
- *     scale = max(largest magnitude / 448, 2^-126), and codes are the nearest ones to entry / scale, the even one of two; a block
- *     with an entry that is not finite has the scale NaN and codes 0.
+ *     scale = max(largest magnitude / 448, 2^-126), rounded to a float, and codes are the nearest ones to entry * 448 / largest magnitude
+ *     (to entry * 2^126 under the smallest scale), the even one of two: not to entry / scale, which differs by the scale's rounding.  A
+ *     block with an entry that is not finite has the scale NaN and codes 0.
  *   - place: device, int32[rows x k]: where choice j of row r lies among the sorted rows, at [r k + j]; places are distinct.
  *     A place outside [0, sorted rows) stands for no choice (nmf_route writes -1).  Sorted rows that no place names are not
  *     written.
@@ -45,7 +46,8 @@ enum { NMF_E4M3 = 3 };            /* type of nmf_spread_rows alone: codes and th
  * added up in floats: s is 0 where they pass 2^128.)
  *   H       rows x m, or null; it may be X or R itself (the same pointer and leading dimension)
  *   weight  m entries, or null for 1
- *   Y       rows x m, or null;  Y8, scale: the same in codes, rounded from floats, or both null;  one of them at least
+ *   Y       rows x m, or null;  Y8, scale: the floats that Y is rounded from, in codes, or both null;  one of them
+ *           at least.  A code whose quotient is within 2^-22 of itself of the middle between two may be the farther one.
  *   rstd    float[rows]: s, or null
  */
 int nmf_rms_norm(int32_t type, const void *X, int64_t ldx, const void *R, int64_t ldr, const void *weight, int64_t rows, int64_t m,

@@ -50,3 +50,28 @@ def test_codes_are_the_nearest_ones_at_the_ends_of_the_range(low, high, typ):
         want = nearest(X.double(), most)
         bad = C.float().double() != want
         assert not bool(bad.any()), (block, int(bad.sum()), X[bad][:4], want[bad][:4], C.float()[bad][:4])
+
+
+@gpu
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("low,high", [(-124, -112), (-6, 7), (100, 126)])
+@pytest.mark.parametrize("m", [128, 640, 4096, 9088, 32768])
+def test_codes_of_the_norm_are_the_nearest_but_beside_borders(m, low, high, typ):
+    """Rows of 1 and -1, whose norm is one: the weights come out as they are, on borders of codes and beside them.  Within 2^-22 of a border
+    (scale, inverse and product are off by 2^-24 each) either neighbour will do."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    rows, dt = 5, TYPES[typ]
+    w = on_borders(g, 256, low, high, dt).reshape(-1)[:m].contiguous()
+    beside = torch.rand(m, generator=g, device="cuda") < 0.5               # some a little farther off
+    beside[::128] = False
+    w = torch.where(beside, w.double() * (1 - 2.0 ** -7), w.double()).to(dt)
+    X = (2 * torch.randint(0, 2, (rows, m), generator=g, device="cuda") - 1).to(dt)
+    Y, Y8, scale = torch.empty_like(X), torch.empty(rows, m, dtype=E8, device="cuda"), torch.empty(rows, m // 128, device="cuda")
+    nmf.nmf_rms_norm(X, rows, m, 0.0, weight=w, Y=Y, Y8=Y8, scale=scale)
+    assert torch.equal(Y, X * w)
+    most = w.double().abs().view(-1, 128).amax(1)
+    assert bool(((scale.double() * 448 - most).abs() <= most * 2.0 ** -24).all())
+    y, most = Y.double(), most.repeat_interleave(128)[None]
+    low, high = (nearest((y * (1 + s * 2.0 ** -22)).clamp(-most, most), most) for s in (-1, 1))
+    got = Y8.float().double()
+    assert bool(((got == low) | (got == high)).all())
