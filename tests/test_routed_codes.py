@@ -70,7 +70,7 @@ def test_codes_of_the_norm_are_the_nearest_but_beside_borders(m, low, high, typ)
     nmf.nmf_rms_norm(X, rows, m, 0.0, weight=w, Y=Y, Y8=Y8, scale=scale)
     assert torch.equal(Y, X * w)
     most = w.double().abs().view(-1, 128).amax(1)
-    assert bool(((scale.double() * 448 - most).abs() <= most * 2.0 ** -24).all())
+    assert bool(((scale.double() - (most / 448).clamp_min(2.0 ** -126)).abs() <= scale.double() * 2.0 ** -24).all())
     y, most = Y.double(), most.repeat_interleave(128)[None]
     low, high = (nearest((y * (1 + s * 2.0 ** -22)).clamp(-most, most), most) for s in (-1, 1))
     got = Y8.float().double()
