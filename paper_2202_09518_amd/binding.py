@@ -556,11 +556,11 @@ def nmf_round_blocks(X, rows, m, block, X8, scale, stream=None) -> None:
 
 def nmf_grouped_product8(X8, xscale, offsets, groups, rows, B8, bscale, transposed, m, n, Y, work=None, stream=None) -> None:
     """Y_g = X_g B_g from codes and scales; B8: groups x m x n, or groups x n x m if transposed; the result has Y's type."""
-    typ, d = _type(Y, "Y"), X8.get_device()
+    typ, codes, d = _type(Y, "Y"), _codes(X8, "X8"), X8.get_device()
     if d != _current_device():
         return _call_on(d, nmf_grouped_product8, X8, xscale, offsets, groups, rows, B8, bscale, transposed, m, n, Y, work, stream)
     M, N = (m + 127) // 128, (n + 127) // 128
-    x, ldx = _rows_of(X8, _codes(X8, "X8"), d, rows, m, "X8")
+    x, ldx = _rows_of(X8, codes, d, rows, m, "X8")
     xs, ldxs = _rows_of(xscale, torch.float32, d, rows, M, "xscale")
     b, ldb, stride_b = _stack_of(B8, _codes(B8, "B8"), d, groups, *((n, m) if transposed else (m, n)), "B8")
     bs, ldbs, stride_bs = _stack_of(bscale, torch.float32, d, groups, *((N, M) if transposed else (M, N)), "bscale")
@@ -605,6 +605,8 @@ def nmf_route_gradient(logits, rows, groups, k, normalise, choice, offsets, dgat
 def nmf_spread_rows(X, rows, k, place, m, Y, scale=None, Yscale=None, stream=None) -> None:
     """Each row of X to its k places among Y's rows; codes take their scales along (scale to Yscale)."""
     dt, d = X.dtype, X.get_device()
+    if dt in _CODES:
+        _codes(X, "X")
     typ = NMF_E4M3 if dt in _CODES else _type(X, "X")
     if d != _current_device():
         return _call_on(d, nmf_spread_rows, X, rows, k, place, m, Y, scale, Yscale, stream)
