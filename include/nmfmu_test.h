@@ -57,6 +57,13 @@ int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs
                          int64_t stride_b, int32_t transposed, int64_t m, int64_t n, size_t work_bytes, int64_t *route);
 
 /*
+ * Loads of a tile of nmf_grouped_product8 whose B (m x n, ld from row to row) comes through registers as it lies: of `columns` columns from
+ * c0 on and the contraction up to k1, in reads[0..1] (host): [0] stages that are loaded without a look at every chunk, [1] how far from
+ * (0, c0) on they read, in bytes.  What the kernel decides by, on the host.
+ */
+int nmfmu_column_reads(int64_t m, int64_t n, int64_t ld, int64_t c0, int32_t columns, int64_t k1, int64_t *reads);
+
+/*
  * nmf_mu_dense with timing, on A as it is (no copy of a misaligned A is made, so such
  * an A takes the slower kernels here): the same launches on `stream`, with a HIP event
  * recorded between them; synchronises `stream` before returning.  On return

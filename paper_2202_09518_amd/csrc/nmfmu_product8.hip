@@ -126,11 +126,11 @@ template <int R, int THREADS> struct ColumnLoader : Loader<e8_t, R, true, THREAD
         for (int j = 0; j < kJobs; ++j) this->reg[j] = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < kJobs; ++j)
-            from[j] = this->chunk(j) * 16 < this->count ? (unsigned)(this->line + j * Base::kRowStep) * (unsigned)o.ld + this->chunk(j) * 16 : kOutside;
+            from[j] = this->chunk(j) * 16 < this->count ? column_chunk(this->line + j * Base::kRowStep, this->chunk(j), o.ld) : kOutside;
     }
     __device__ __forceinline__ void fetch(int64_t k0, int64_t K, char *)
     {
-        if (this->ld < (1 << 22) && K - k0 >= 128 && (k0 + 127) * this->ld + (this->count + 15) / 16 * 16 <= this->bytes) {
+        if (whole_stage(this->ld, k0, K, this->count, this->bytes)) {
             const char *at = this->base + k0 * this->ld;
 #pragma unroll
             for (int j = 0; j < kJobs; ++j)
@@ -403,7 +403,7 @@ template <class C, class O> __global__ __launch_bounds__(C::THREADS) void produc
     if (!ranges.find(4 * block + in % high, f)) return;
     const Operand P = {(const char *)a.x + f.r0 * a.ldx, a.ldx, f.r1 - f.r0, (a.rows - 1 - f.r0) * a.ldx + a.m};
     const char *b = (const char *)a.b + f.g * a.stride_b;
-    const Operand Q = C::QRC ? Operand{b + c0, a.ldb, a.n - c0, (a.m - 1) * a.ldb + a.n - c0} : Operand{b + c0 * a.ldb, a.ldb, a.n - c0, (a.n - 1 - c0) * a.ldb + a.m};
+    const Operand Q = C::QRC ? Operand{b + c0, a.ldb, a.n - c0, column_bytes(a.m, a.n, a.ldb, c0)} : Operand{b + c0 * a.ldb, a.ldb, a.n - c0, (a.n - 1 - c0) * a.ldb + a.m};
     const int64_t last = (a.n - 1) / 128, mine = (c0 + C::wave_col()) / 128, col = mine < last ? mine : last;
     const Scales scales = {a.xs + f.r0 * a.ldxs, a.ldxs, a.bs + f.g * a.stride_bs + col * (C::QRC ? 1 : a.ldbs), C::QRC ? a.ldbs : 1};
     const int64_t blocks = blocks_of(a.m), b0 = split * a.k_split, b1 = b0 + a.k_split < blocks ? b0 + a.k_split : blocks;

@@ -97,7 +97,7 @@ size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (
 // Codes whose rows do not begin and end on 16-byte borders pass registers on their way to LDS, which takes 2 to 3.5 times as long;
 // where the product is long enough they are copied once per call into rows that do, if the scratch has room.
 // (us: 6000 x 4095 x 2047 in 4 groups 239, transposed 141, through registers, 94 and 89 with copies)
-constexpr int64_t kFar = 1 << 22;      // straight to LDS, distances inside a tile go into 32 bits: 256 rows below this, copied ones too
+constexpr int64_t kFar = kFarRows;      // straight to LDS, distances inside a tile go into 32 bits: 256 rows below this, copied ones too
 int64_t whole(int64_t cols) { return ceil_div(cols, 16) * 16; }
 struct Codes {
     const void *p;
@@ -380,6 +380,20 @@ int nmfmu_product8_route(int32_t type, const void *X8, int64_t ldx, int64_t ldxs
     route[4] = kTileRows[r.tiles.shape];
     route[5] = kTileCols[r.tiles.shape];
     route[6] = r.tiles.splits > 1 ? (int64_t)product_part(rows, n, r.tiles.splits) : 0;
+    return NMF_OK;
+}
+
+int nmfmu_column_reads(int64_t m, int64_t n, int64_t ld, int64_t c0, int32_t columns, int64_t k1, int64_t *reads)
+{
+    const int64_t bytes = column_bytes(m, n, ld, c0);
+    const int count = (int)std::min<int64_t>(n - c0, columns);
+    reads[0] = reads[1] = 0;
+    for (int64_t k0 = 0; k0 < k1; k0 += 128) {
+        if (!whole_stage(ld, k0, k1, count, bytes)) continue;
+        ++reads[0];
+        for (int k = 0; k < 128; ++k)
+            for (int chunk = 0; chunk * 16 < count; ++chunk) reads[1] = std::max(reads[1], k0 * ld + column_chunk(k, chunk, ld) + 16);
+    }
     return NMF_OK;
 }
 

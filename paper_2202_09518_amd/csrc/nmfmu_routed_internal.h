@@ -110,6 +110,16 @@ struct RouteGradient {
 };
 template <class T> hipError_t launch_route_gradient(const RouteGradient &a, hipStream_t st);
 
+// Operands by columns, rows of ld codes from column c0 of m x n on: bytes from their first code to the array's end; whether a stage of 128 k
+// from k0 on, up to k1, is loaded in chunks as they lie, of `count` columns of a tile; and where such a chunk begins.
+constexpr int64_t kFarRows = 1 << 22;      // distances inside a stage go into 32 bits below this
+constexpr int64_t column_bytes(int64_t m, int64_t n, int64_t ld, int64_t c0) { return (m - 1) * ld + n - c0; }
+constexpr bool whole_stage(int64_t ld, int64_t k0, int64_t k1, int count, int64_t bytes)
+{
+    return ld < kFarRows && k1 - k0 >= 128 && (k0 + 127) * ld + (count + 15) / 16 * 16 <= bytes;
+}
+constexpr unsigned column_chunk(int k, int chunk, int64_t ld) { return (unsigned)k * (unsigned)ld + chunk * 16; }
+
 struct Product8 {
     const void *x;
     int64_t ldx;
