@@ -21,9 +21,12 @@
  *     A place outside [0, sorted rows) stands for no choice (nmf_route writes -1).  Sorted rows that no place names are not
  *     written.
  *   - Malformed offsets, places and choices give meaningless results but no access out of range.
- *   - Rows stand alone, but in `balance` and in the gradient of the norm's weight, which are sums over all rows.
+ *   - Rows stand alone, but in `balance` and in the gradient of the norm's weight, which are sums over all rows: what is in one row
+ *     reaches no other one's results.  (The order in which nmf_grouped_product8 sums, and so a row's last bits, goes by the sizes of the
+ *     call and by where the row lies.)
  *   - Results may not overlap operands, except where said.  Streams, capture, work and limits as in nmfmu_ragged.h; the scratch
- *     of a call is nmf_routed_work_bytes(...) bytes, with less it takes a slower plan.  Results are the same bits in every call
+ *     of a call is nmf_routed_work_bytes(...) bytes, with less it takes a slower plan (nmf_route one workgroup for all rows, which is
+ *     for few of them).  Results are the same bits in every call
  *     with the same scratch.
  */
 #ifndef NMFMU_ROUTED_H
@@ -43,7 +46,8 @@ enum { NMF_E4M3 = 3 };            /* type of nmf_spread_rows alone: codes and th
 
 /*
  * H = X + R (rounded to `type`), s = 1 / sqrt(mean over columns of H^2 + eps), Y = H s w.  Without R (null): H = X.  (Squares are
- * added up in floats: s is 0 where they pass 2^128.)
+ * added up in floats: s is 0 where they pass 2^128, and loses bits where they lie below 2^-126 and eps does too; with eps 0 it is
+ * infinite for a row of zeros.)
  *   H       rows x m, or null; it may be X or R itself (the same pointer and leading dimension)
  *   weight  m entries, or null for 1
  *   Y       rows x m, or null;  Y8, scale: the floats that Y is rounded from, in codes, or both null;  one of them
@@ -79,7 +83,9 @@ int nmf_round_blocks(int32_t type, const void *X, int64_t ldx, int64_t stride, i
  *   Y           rows x n of `type`;  rows outside all groups are not written
  * The gradient dX_g = dY_g B_g^T of rounded dY is the same call with B in its other form; that of B is nmf_grouped_gradient of the
  * rows before they were rounded.  Rows of codes that begin and end on 16-byte borders are fastest (others are copied, or slower).
- * Results in 16 bits: of eight neighbouring products of codes what is below 2^-13 of the largest one is left out.
+ * Results in float32 keep all bits of the products of codes.  Those in 16 bits leave out, of eight neighbouring products, what is below
+ * 2^-13 of the largest one: 1.4e-5 of the results' root mean square, which is more than the last place of f16 where a result cancels to a
+ * few hundredths of that.  The scales of two blocks are multiplied first, as floats: their product should be a normal one.
  */
 int nmf_grouped_product8(int32_t type, const void *X8, int64_t ldx, const float *xscale, int64_t ldxs, const int64_t *offsets,
                          int32_t groups, int64_t rows, const void *B8, int64_t ldb, int64_t stride_b, const float *bscale, int64_t ldbs,

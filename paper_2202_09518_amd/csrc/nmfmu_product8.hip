@@ -385,7 +385,7 @@ template <int BM, int BN, int WM, int WN, int STAGES_, bool QRC, bool DMA, bool 
 
 // Y, or parts of it over the contraction.  Few rows are bound by reading the groups' matrices: 512 rows over 64 groups of 4096 x 2048
 // 85 to 88 us (6.1 to 6.3 TB/s); many by power (above); 1237 rows of 515 x 389 in 9 groups, float results, by the latency of five stages
-// through registers, 10.7.
+// through registers, 10.8.
 template <class C, class O> __global__ __launch_bounds__(C::THREADS) void product8_kernel(Product8 a)
 {
     __shared__ __align__(1024) char lds[C::kLds];

@@ -444,7 +444,9 @@ template <class T> hipError_t launch_route(const Route &a, hipStream_t st)
 }
 
 // ---- gradient of the logits ------------------------------------------------------------------
-// All from the logits again, as what the softmax was is not kept.  16384 x 128 bf16: 9.6 us (0.9 TB/s; the exponents' instructions).
+// All from the logits again, as what the softmax was is not kept.  16384 x 128 bf16: 9.6 us (0.9 TB/s).  Instructions bound it, 780
+// of the vector unit for a wave of four rows: eight compares of each lane for each choice, the opening, which each wave does in floats of
+// 64 bits for its only turn, and the exponents, a sixth of them.
 template <class T, int W, int C> __global__ __launch_bounds__(kFew) void route_gradient_kernel(RouteGradient a)
 {
     constexpr int ROWS = kFew / W;

@@ -64,6 +64,7 @@ struct Plan {
 // Time of `tiles` tiles of a shape: those of the busiest compute unit, by their size and by what share of the large tile's rate
 // they reach.  us, bf16 results: 8192 x 4096 x 4096 takes 131 in tiles of 256 x 256, 190 in 128 x 128, 230 in 64 x 128, 270 to 300 in
 // 64 x 64; 1024 x 4096 x 4096 49, 32.1, 31.9, 39.3; 2000 x 2048 x 2048 28, 19.0, 18.7, 23.2; 4096 rows in 8 groups, 4096 x 2048, 52, 68, 75, 77.
+// (Float results and codes that pass registers go by the same shares, which were not measured for them.)
 double tile_time(int shape, int64_t tiles)
 {
     const double rate = shape == k256x256 ? 1.0 : shape == k128x128 ? 0.7 : shape == k64x128 ? 0.5 : 0.45;
@@ -96,7 +97,9 @@ size_t product_part(int64_t rows, int64_t n, int splits) { return splits > 1 ? (
 
 // Codes whose rows do not begin and end on 16-byte borders pass registers on their way to LDS, which takes 2 to 3.5 times as long;
 // where the product is long enough they are copied once per call into rows that do, if the scratch has room.
-// (us: 6000 x 4095 x 2047 in 4 groups 239, transposed 141, through registers, 94 and 89 with copies)
+// (us, bf16 results: 6000 x 4095 x 2047 in 4 groups 239, transposed 141, through registers, 94 and 89 with copies; 2245 rows in 22 groups of
+// 6197 x 5568 425 and 217, 8192 in 64 of 4095 x 4096 605 and 305, where only the rows are copied.  Float results take longer either way and
+// go by the same rate.)
 constexpr int64_t kFar = kFarRows;      // straight to LDS, distances inside a tile go into 32 bits: 256 rows below this, copied ones too
 int64_t whole(int64_t cols) { return ceil_div(cols, 16) * 16; }
 struct Codes {

@@ -119,7 +119,10 @@ template <class T> hipError_t launch_norm(const Norm &a, hipStream_t st)
 // ---- gradients of the norm -------------------------------------------------------------------
 // A thread has the same columns of all its rows, so it adds up the weight's gradient as it goes; the workgroups' sums meet in
 // a second launch, in order.  Few rows are one workgroup's, which writes the weight's gradient itself.
-// 8192 x 4096 bf16 with the residual's gradient: 50 us (5.4 TB/s) and 4.6 for the sums of 1024 workgroups.
+// 8192 x 4096 bf16 with the residual's gradient: 50 us (5.4 TB/s) and 4.6 for the sums of 1024 workgroups.  Wider, both in turn: 8192 x
+// 8192 130 us, 4096 x 16384 109; 2048 x 32768 232 (114 without the weight's gradient), as 1024 threads have 128 registers each, and
+// beyond 16384 columns (8192 in float32, by a few) what they hold does not fit: memory takes the rest.  A wave for each narrow row leaves
+// most of its lanes idle: 524288 x 128 396 us (1.4 TB/s).
 template <class T, int W, int C, bool DW> __global__ __launch_bounds__(W < 256 ? 256 : W) void norm_gradient_kernel(NormGradient a)
 {
     constexpr int ROWS = W < 256 ? 256 / W : 1;
@@ -235,7 +238,8 @@ template <class T> __global__ __launch_bounds__(1024) void norm_weight_kernel(No
     ((T *)a.dw)[col] = Type<T>::round(x);
 }
 
-// Four workgroups of 256 threads to a compute unit: 8192 x 4096 bf16, forward and backward, 104 us; with three 106, with two 115.
+// Four workgroups of 256 threads to a compute unit: 8192 x 4096 bf16, forward and backward, 104 us; with three 106, with two 115.  (The
+// number for all widths, of which only that one was measured; of 4097 to 8192 columns the registers of two fit at once.)
 constexpr int kNormThreads = 256 * 1024;
 int norm_parts(int64_t rows, int64_t m)
 {
